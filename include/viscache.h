@@ -419,6 +419,136 @@ vc_status viscache_decode_step_planned(const vc_decode_shape *shape, const vc_ca
                                        const void *q, float *out, float scale, int64_t max_rows, void *workspace,
                                        size_t workspace_bytes, void *stream);
 
+/* ---- 8-bit cache, quantised as it is written ------------------------------
+ * A decode cache whose rows are kept in 8 bits.  64 consecutive rows of a unit
+ * (layer, sequence, kv head) form a block with one scale for its keys and one
+ * for its values:
+ *   eff = clamp(max |x| over the block's 64 x d values, Q 2^-60, Q 2^60),
+ *   scale = eff / Q (fp32),
+ *   code = Q x / eff, rounded to nearest, ties to even, in the 8-bit type
+ *          (exactly: no intermediate rounding),
+ * Q = 127 (int8) or 448 (e4m3), and a row reads back as code * scale.  A block
+ * is sealed (quantised) when its 64th row arrives; the rows of the open block
+ * (fewer than 64) wait in bf16 in the unit's tail, so the cache's contents
+ * follow from its rows, not from how many were appended at a time. */
+#define VC_Q8_BLOCK 64
+typedef enum { VC_Q8_INT8 = 0, VC_Q8_E4M3 = 1 } vc_q8_format; /* e4m3: finite only, NaN 0x7F / 0xFF */
+
+/* Unit u = (l*B + b)*Hkv + g owns rows [row_off[u], row_off[u] + 64 ceil(cap[u]
+ * / 64)) of the code pools and the entries of those blocks (row / 64) of the
+ * scale arrays, and holds len[u] <= cap[u] rows; row_off[u] must be a multiple
+ * of 64, and units must not overlap.  With block = row_off[u] / 64 + i / 64 and
+ * j = i % 64, row i of a sealed block has its key codes at k_codes + (block*64 +
+ * j)*d (row-major) and the code of value channel c at v_codes + block*64*d +
+ * c*64 + j (channel-major).  Row i of the open block is row j of the unit's tail.
+ * The open block's scale entries hold the power of two that puts the largest
+ * magnitude of its rows into [2^14, 2^15), at least 2^-60.  A cache starts with
+ * len 0 and any other contents.  All pointers DEVICE; code pools and tails
+ * 16-byte aligned. */
+typedef struct {
+  int32_t format;         /* vc_q8_format */
+  void *k_codes, *v_codes; /* 1 byte a value */
+  float *k_scale, *v_scale;
+  void *k_tail, *v_tail;  /* bf16 [L*B*Hkv][64][d] */
+  const int64_t *row_off; /* [L*B*Hkv] */
+  const int32_t *cap;
+  int32_t *len;
+} vc_q8cache;
+
+/* A strided DEVICE tensor of rows of d contiguous values: row (layer l,
+ * sequence b, token i, head h) starts at data + l*layer + b*seq + i*token +
+ * h*head elements.  data must be 16-byte aligned and every stride a multiple of
+ * 16 bytes and not negative (VC_ERR_ARG; the stride of a dimension of size 1 is
+ * not read).  A stride of 0 repeats rows of an
+ * input; the rows of an output must be distinct. */
+typedef struct {
+  void *data;
+  int64_t layer, seq, token, head;
+} vc_rows;
+
+/* Device, asynchronous.  Appends up to n rows to every unit: rows i < c of k
+ * and v (bf16, head index the kv head), c = count[l*B + b] clamped to [0, n], or
+ * n where count is NULL (count: DEVICE int32 [L*B]), as far as cap leaves
+ * room; len grows by the rows appended.  unit_off, if not NULL, is a DEVICE
+ * array [L*B*Hkv] of the element offset of each unit's first row (a multiple
+ * of 8), instead of the layer, seq and head strides: packed rows such as
+ * viscache_prune's outputs.  Tail rows past the open block's are left as they
+ * were.  n = 0 does nothing.  The cache's other arrays must not be in use on
+ * another stream.  VC_ERR_UNSUPPORTED where the launch would take 2^23 or more
+ * workgroups (one per unit for n <= 64, else ceil(n/64) + 1). */
+vc_status viscache_q8_append(const vc_decode_shape *shape, const vc_q8cache *cache, const vc_rows *k,
+                             const vc_rows *v, int32_t n, const int32_t *count, const int64_t *unit_off, void *stream);
+
+/* Device, asynchronous.  Reads the cache back: rows [0, min(len, cap, max_rows)) of
+ * every unit into k and v (token index = row), as bf16 (out_fp32 = 0; rounded
+ * to nearest even) or fp32 values; the rows behind are left as they were.  unit_off as
+ * for viscache_q8_append (a multiple of 16 bytes): for instance the pools of a
+ * vc_cache.  Limits as there, with max_rows for n. */
+vc_status viscache_q8_read(const vc_decode_shape *shape, const vc_q8cache *cache, int32_t max_rows, const vc_rows *k,
+                           const vc_rows *v, const int64_t *unit_off, int32_t out_fp32, void *stream);
+
+/* Host only.  Workspace bytes viscache_q8_attend needs for n queries a
+ * sequence over caches of at most max_rows rows; 0 where it refuses them. */
+size_t viscache_q8_attend_workspace_bytes(const vc_decode_shape *shape, int32_t n, int32_t max_rows);
+
+/* Device, asynchronous.  Attention of n queries per sequence and layer over the
+ * 8-bit cache, which holds their own keys and values already (append first):
+ * query i of sequence b, c = count[b] clamped to [0, n] (DEVICE int32 [B]; NULL:
+ * n), attends rows t < len - c + i + 1 (causal = 1: the c newest rows are the
+ * queries' own) or t < len (causal = 0),
+ *   out = softmax_t(scale * q . K_t) V_t
+ * with K_t and V_t as they read back (before any rounding to bf16).  q: bf16; out:
+ * bf16 (out_fp32 = 0) or fp32; both indexed by the query head.  A query that
+ * sees no row gives zeros; rows i >= c of out are left as they were.  max_rows
+ * bounds every len (rows past it are not attended).  n * Hq/Hkv <= 16 (single
+ * tokens, short drafts) takes one launch, more a launch or two.  n = 0 does nothing.
+ * `workspace`: DEVICE, at least viscache_q8_attend_workspace_bytes bytes,
+ * 256-byte aligned, zero-filled before its first use and not modified by the
+ * caller between calls (its counters are left at zero).  Calls sharing a
+ * workspace, captured ones among them, must be ordered on one stream and agree
+ * in L*B*Hkv; the rest of the shape, n and max_rows may differ.
+ * VC_ERR_UNSUPPORTED for n * Hq/Hkv > 2^24, or 2^23 or more workgroups. */
+vc_status viscache_q8_attend(const vc_decode_shape *shape, const vc_q8cache *cache, const vc_rows *q,
+                             const vc_rows *out, int32_t n, const int32_t *count, int32_t causal, int32_t out_fp32,
+                             float scale, int32_t max_rows, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---- rotary positions with several axes -----------------------------------
+ * Queries and keys of visual tokens turn with their time, height and width,
+ * text tokens with three equal positions.  Frequency i, i < rot/2, is
+ * theta^(-2i/rot) (or inv_freq[i]) and belongs to one axis:
+ *   SECTIONED:   the first sections[0] frequencies to axis 0, the next
+ *                sections[1] to axis 1, the last sections[2] to axis 2;
+ *   INTERLEAVED: i to axis 1 if i % 3 == 1 and i < 3 sections[1], to axis 2 if
+ *                i % 3 == 2 and i < 3 sections[2], else to axis 0.
+ * With a = pos[axis(i)] * frequency i the pair (x1, x2) of i becomes scale *
+ * (x1 cos a - x2 sin a, x2 cos a + x1 sin a); inverse = 1 turns by -a, which is
+ * the gradient (inputs from outputs' gradients).  Channels from rot on are
+ * copied.  Pairs: HALVES (i, i + rot/2), ADJACENT (2i, 2i+1).  The angle is
+ * formed in 64 bits, the rotation in fp32, and rounded once. */
+typedef enum { VC_ROPE_SECTIONED = 0, VC_ROPE_INTERLEAVED = 1 } vc_rope_layout;
+typedef enum { VC_ROPE_HALVES = 0, VC_ROPE_ADJACENT = 1 } vc_rope_pairing;
+typedef struct {
+  int32_t rot;             /* rotated channels: a multiple of 16, at most d */
+  int32_t sections[3];     /* not negative, summing to rot/2 */
+  int32_t layout, pairing; /* vc_rope_layout, vc_rope_pairing */
+  int32_t fp32;            /* element type: 0 bf16, 1 fp32 */
+  int32_t inverse;
+  float scale;             /* finite; 1 for a plain rotation */
+  double theta;            /* > 0; not read with inv_freq */
+  const double *inv_freq;  /* HOST [rot/2], finite, or NULL */
+} vc_rope;
+
+/* Device, asynchronous.  Rotates n tokens of every layer and sequence: queries
+ * from q_in to q_out (head index the query head) and keys from k_in to k_out
+ * (the kv head); either pair may be NULL, not both.  An output may be its
+ * input (the same data and strides); otherwise they must not overlap.  pos:
+ * DEVICE int32 [3][B][n], shared by the layers.  count: DEVICE int32 [B] or
+ * NULL; tokens i >= count[b] are left alone.  n = 0 does nothing.
+ * VC_ERR_UNSUPPORTED for 2^24 or more tokens over all layers and sequences. */
+vc_status viscache_rope(const vc_decode_shape *shape, const vc_rope *rope, int32_t n, const int32_t *pos,
+                        const int32_t *count, const vc_rows *q_in, const vc_rows *q_out, const vc_rows *k_in,
+                        const vc_rows *k_out, void *stream);
+
 /* Static text for a status code. */
 const char *viscache_strerror(vc_status s);
 

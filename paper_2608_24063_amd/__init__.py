@@ -18,6 +18,10 @@ VC_OK, VC_ERR_ARG, VC_ERR_SHAPE, VC_ERR_BUDGET, VC_ERR_WORKSPACE, VC_ERR_UNSUPPO
 VC_RANK_LAYER_HEAD, VC_RANK_GLOBAL = 0, 1
 VC_SCHED_PARABOLIC, VC_SCHED_FIXED, VC_SCHED_ARITHMETIC, VC_SCHED_GEOMETRIC = 0, 1, 2, 3
 VC_SCORE_WINDOW, VC_SCORE_PREFILL = 0, 1
+VC_Q8_BLOCK = 64
+VC_Q8_INT8, VC_Q8_E4M3 = 0, 1
+VC_ROPE_SECTIONED, VC_ROPE_INTERLEAVED = 0, 1
+VC_ROPE_HALVES, VC_ROPE_ADJACENT = 0, 1
 
 P = ctypes.POINTER
 c_i32, c_i64, c_f32, c_f64, c_vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_double, ctypes.c_void_p
@@ -50,6 +54,20 @@ class vc_cache(ctypes.Structure):
 class vc_qcache(ctypes.Structure):
     _fields_ = [("k_codes", c_vp), ("k_meta", c_vp), ("v_codes", c_vp), ("v_meta", c_vp),
                 ("qrow_off", c_vp), ("nq", c_vp)]
+
+
+class vc_q8cache(ctypes.Structure):
+    _fields_ = [("format", c_i32), ("k_codes", c_vp), ("v_codes", c_vp), ("k_scale", c_vp), ("v_scale", c_vp),
+                ("k_tail", c_vp), ("v_tail", c_vp), ("row_off", c_vp), ("cap", c_vp), ("len", c_vp)]
+
+
+class vc_rows(ctypes.Structure):
+    _fields_ = [("data", c_vp), ("layer", c_i64), ("seq", c_i64), ("token", c_i64), ("head", c_i64)]
+
+
+class vc_rope(ctypes.Structure):
+    _fields_ = [("rot", c_i32), ("sections", c_i32 * 3), ("layout", c_i32), ("pairing", c_i32), ("fp32", c_i32),
+                ("inverse", c_i32), ("scale", c_f32), ("theta", c_f64), ("inv_freq", P(c_f64))]
 
 
 class VisCacheError(RuntimeError):
@@ -100,13 +118,24 @@ def lib() -> ctypes.CDLL:
                                                    ctypes.c_size_t, c_vp, c_vp, c_vp, c_vp, c_f32, c_i64, c_vp,
                                                    ctypes.c_size_t, c_vp]
         L.viscache_quantize_rows.argtypes = [c_i32, c_i64, c_vp, c_vp, c_vp, c_vp]
+        L.viscache_q8_append.argtypes = [P(vc_decode_shape), P(vc_q8cache), P(vc_rows), P(vc_rows), c_i32, c_vp,
+                                         c_vp, c_vp]
+        L.viscache_q8_read.argtypes = [P(vc_decode_shape), P(vc_q8cache), c_i32, P(vc_rows), P(vc_rows), c_vp,
+                                       c_i32, c_vp]
+        L.viscache_q8_attend_workspace_bytes.argtypes = [P(vc_decode_shape), c_i32, c_i32]
+        L.viscache_q8_attend_workspace_bytes.restype = ctypes.c_size_t
+        L.viscache_q8_attend.argtypes = [P(vc_decode_shape), P(vc_q8cache), P(vc_rows), P(vc_rows), c_i32, c_vp,
+                                         c_i32, c_i32, c_f32, c_i32, c_vp, ctypes.c_size_t, c_vp]
+        L.viscache_rope.argtypes = [P(vc_decode_shape), P(vc_rope), c_i32, c_vp, c_vp, P(vc_rows), P(vc_rows),
+                                    P(vc_rows), P(vc_rows), c_vp]
         L.viscache_strerror.argtypes = [c_i32]
         L.viscache_strerror.restype = ctypes.c_char_p
         for name in ("viscache_budget", "viscache_out_rows", "viscache_prune", "viscache_prune_score_offsets",
                      "viscache_prune_staged",
                      "viscache_append_kv", "viscache_decode_attn", "viscache_decode_step",
                      "viscache_decode_step_q4", "viscache_decode_step_noalloc", "viscache_decode_plan",
-                     "viscache_decode_step_planned", "viscache_quantize_rows"):
+                     "viscache_decode_step_planned", "viscache_quantize_rows", "viscache_q8_append",
+                     "viscache_q8_read", "viscache_q8_attend", "viscache_rope"):
             getattr(L, name).restype = c_i32
         _lib = L
     return _lib
@@ -304,6 +333,47 @@ def viscache_quantize_rows(d: int, rows: int, src: int, codes: int, meta: int, s
     _check(lib().viscache_quantize_rows(d, rows, src, codes, meta, stream), "viscache_quantize_rows")
 
 
+def _ref(x):
+    return ctypes.byref(x) if x is not None else None
+
+
+def viscache_q8_append(shape: vc_decode_shape, cache: vc_q8cache, k: vc_rows, v: vc_rows, n: int, count: int,
+                       unit_off: int, stream: int) -> None:
+    """count, unit_off: device addresses, 0 for none."""
+    st = lib().viscache_q8_append(_ref(shape), _ref(cache), _ref(k), _ref(v), n, count, unit_off, stream)
+    if st:
+        _check(st, "viscache_q8_append")
+
+
+def viscache_q8_read(shape: vc_decode_shape, cache: vc_q8cache, max_rows: int, k: vc_rows, v: vc_rows, unit_off: int,
+                     out_fp32: int, stream: int) -> None:
+    st = lib().viscache_q8_read(_ref(shape), _ref(cache), max_rows, _ref(k), _ref(v), unit_off, out_fp32, stream)
+    if st:
+        _check(st, "viscache_q8_read")
+
+
+def viscache_q8_attend_workspace_bytes(shape: vc_decode_shape, n: int, max_rows: int) -> int:
+    return int(lib().viscache_q8_attend_workspace_bytes(ctypes.byref(shape), n, max_rows))
+
+
+def viscache_q8_attend(shape: vc_decode_shape, cache: vc_q8cache, q: vc_rows, out: vc_rows, n: int, count: int,
+                       causal: int, out_fp32: int, scale: float, max_rows: int, workspace: int, workspace_bytes: int,
+                       stream: int) -> None:
+    st = lib().viscache_q8_attend(_ref(shape), _ref(cache), _ref(q), _ref(out), n, count, causal, out_fp32, scale,
+                                  max_rows, workspace, workspace_bytes, stream)
+    if st:
+        _check(st, "viscache_q8_attend")
+
+
+def viscache_rope(shape: vc_decode_shape, rope: vc_rope, n: int, pos: int, count: int, q_in, q_out, k_in, k_out,
+                  stream: int) -> None:
+    """q_in ... k_out: vc_rows or None."""
+    st = lib().viscache_rope(_ref(shape), _ref(rope), n, pos, count, _ref(q_in), _ref(q_out), _ref(k_in), _ref(k_out),
+                             stream)
+    if st:
+        _check(st, "viscache_rope")
+
+
 def viscache_strerror(status: int) -> str:
     return strerror(status)
 
@@ -314,4 +384,5 @@ EXPORTED = ("viscache_default_params", "viscache_budget", "viscache_out_rows",
             "viscache_append_kv", "viscache_decode_attn", "viscache_decode_step_workspace_bytes",
             "viscache_decode_step", "viscache_decode_step_q4", "viscache_decode_step_noalloc",
             "viscache_decode_plan_bytes", "viscache_decode_plan", "viscache_decode_step_planned",
-            "viscache_quantize_rows", "viscache_strerror")
+            "viscache_quantize_rows", "viscache_q8_append", "viscache_q8_read",
+            "viscache_q8_attend_workspace_bytes", "viscache_q8_attend", "viscache_rope", "viscache_strerror")

@@ -1,0 +1,289 @@
+// k_q8.hip -- the 8-bit cache as it is written and read back.  64 rows of a
+// (layer, sequence, kv head) share a scale, keys and values apart:
+//   eff = clamp(max |x|, Q 2^-60, Q 2^60), scale = eff / Q, code = Q x / eff
+// rounded to nearest even, Q = 127 (int8) or 448 (e4m3).  A block is sealed
+// (quantised) when its 64th row arrives; until then its rows stay in the
+// unit's bf16 tail, so the cache is a function of its rows, not of how many
+// came at a time.  Keys are stored row-major [64][d]; values channel-major
+// [d][64], which is the order the attention's products take them in, so the
+// transposition is paid once, here.
+//
+// Bound by memory: 2 bytes a value in, 1 out.  A workgroup takes a block's
+// keys with one half of its waves and its values with the other; each half
+// holds its 64 rows in registers between the search for the maximum and the
+// rounding, so the rows are read once.
+#include "vc_q8_device.h"
+
+namespace vc {
+
+namespace {
+
+constexpr int kThreads = 512;  // 256 for keys, 256 for values
+constexpr int kHalf = 256;
+
+template <int D>
+struct WriteSmem {
+  static constexpr int VP = D + 8;  // pitch of the value codes' rows, bytes
+  uint8_t v[kQ8Block * VP] __attribute__((aligned(16)));
+  uint32_t red[2][4];
+};
+
+// Largest over a half's four waves of per-thread packed magnitudes; one
+// barrier (the next use of `red` must come after another one).
+__device__ __forceinline__ uint32_t half_max(uint32_t (&red)[2][4], uint32_t m, int side, int tid) {
+  uint32_t x = max(m & 0xFFFFu, m >> 16);
+#pragma unroll
+  for (int k = 32; k >= 1; k >>= 1) x = max(x, (uint32_t)__shfl_xor((int)x, k, 64));
+  if ((tid & 63) == 0) red[side][(tid >> 6) & 3] = x;
+  __syncthreads();
+  return max(max(red[side][0], red[side][1]), max(red[side][2], red[side][3]));
+}
+
+// Workgroup j of a unit seals block j of those its new rows reach, or leaves
+// it open; workgroup 0 also takes an open last block, since that goes over the
+// tail rows the first block is made of.
+template <int D, int FMT>
+__global__ __launch_bounds__(kThreads) void k_append_rows(Q8Rows p) {
+  __shared__ WriteSmem<D> sm;
+  constexpr int CPR = D / 16;                     // 16-channel chunks per row
+  constexpr int IT = kQ8Block * CPR / kHalf;      // chunks per thread (2 or 1)
+  const int u = (int)(blockIdx.x / (uint32_t)p.nj), j = (int)(blockIdx.x % (uint32_t)p.nj);
+  const int side = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 8), tid = threadIdx.x & 255;
+  const int len0 = max(ldg(p.c.len + u), 0), cap = ldg(p.c.cap + u);
+  const int want = p.count ? min(max(ldg(p.count + u / p.Hkv), 0), p.n) : p.n;
+  const int m = min(want, max(cap - len0, 0));
+  if (m <= 0) return;
+  const int end = len0 + m, b0 = len0 / kQ8Block;
+  const int nblk = (end + kQ8Block - 1) / kQ8Block - b0;
+  const bool open = end % kQ8Block != 0;
+  if (j >= nblk || (j > 0 && open && j == nblk - 1)) return;
+  const int64_t blk0 = ldg(p.c.row_off + u) / kQ8Block + b0;
+  const RowsDesc &rd = side ? p.v : p.k;
+  const uint16_t *src = reinterpret_cast<const uint16_t *>(rd.base) + unit_base(rd, p.unit_off, u, p.B, p.Hkv);
+  uint16_t *tail = (side ? p.c.vt : p.c.kt) + (int64_t)u * kQ8Block * D;
+  float *scales = side ? p.c.vs : p.c.ks;
+
+  auto seal = [&](int jb) {
+    const int lo = jb == 0 ? len0 % kQ8Block : 0;
+    const int64_t r0 = (int64_t)(b0 + jb) * kQ8Block - len0;  // new row of the block's row 0
+    u32x4 x[IT][2];
+    uint32_t mag = 0u;
+#pragma unroll
+    for (int it = 0; it < IT; ++it) {
+      const int e = tid + kHalf * it, row = e / CPR, c = e % CPR;
+      const uint16_t *s = row < lo ? tail + row * D : src + (r0 + row) * rd.token;
+      x[it][0] = ld16(s + 16 * c);
+      x[it][1] = ld16(s + 16 * c + 8);
+    }
+#pragma unroll
+    for (int it = 0; it < IT; ++it)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        mag = max_mag(max_mag(mag, x[it][h].x), x[it][h].y);
+        mag = max_mag(max_mag(mag, x[it][h].z), x[it][h].w);
+      }
+    const float top = __uint_as_float(half_max(sm.red, mag, side, tid) << 16);
+    const float eff = fminf(fmaxf(top, Q8<FMT>::kEffMin), Q8<FMT>::kEffMax);
+    const float inv = __fdiv_rn(Q8<FMT>::kTop, eff);
+    if (tid == 0) stg(scales + blk0 + jb, __fdiv_rn(eff, Q8<FMT>::kTop));
+    uint8_t *dst = (side ? p.c.vc : p.c.kc) + (blk0 + jb) * (kQ8Block * D);
+#pragma unroll
+    for (int it = 0; it < IT; ++it) {
+      const int e = tid + kHalf * it, row = e / CPR, c = e % CPR;
+      uint32_t o[4];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t ws[4] = {x[it][h].x, x[it][h].y, x[it][h].z, x[it][h].w};
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+          o[2 * h + k] = Q8<FMT>::pack4(
+              Q8<FMT>::code_value(bf16_lo(ws[2 * k]), inv), Q8<FMT>::code_value(bf16_hi(ws[2 * k]), inv),
+              Q8<FMT>::code_value(bf16_lo(ws[2 * k + 1]), inv), Q8<FMT>::code_value(bf16_hi(ws[2 * k + 1]), inv));
+      }
+      if (side == 0) {
+        st16(dst + row * D + 16 * c, u32x4{o[0], o[1], o[2], o[3]});
+      } else {
+        u32x2 *t = reinterpret_cast<u32x2 *>(sm.v + row * WriteSmem<D>::VP + 16 * c);
+        t[0] = u32x2{o[0], o[1]};
+        t[1] = u32x2{o[2], o[3]};
+      }
+    }
+    __syncthreads();
+    if (side == 1) {
+      // Thread: channels 4 cq .. 4 cq + 3, rows 8 rg .. 8 rg + 7.
+      const int rg = tid % 8;
+#pragma unroll
+      for (int cq = tid / 8; cq < D / 4; cq += kHalf / 8) {
+        uint32_t w[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+          w[r] = *reinterpret_cast<const uint32_t *>(sm.v + (8 * rg + r) * WriteSmem<D>::VP + 4 * cq);
+        const u32x4 a = transpose4(w[0], w[1], w[2], w[3]), b = transpose4(w[4], w[5], w[6], w[7]);
+        const uint32_t as[4] = {a.x, a.y, a.z, a.w}, bs[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) st8(dst + (4 * cq + k) * kQ8Block + 8 * rg, u32x2{as[k], bs[k]});
+      }
+    }
+  };
+  // Rows lo .. hi - 1 of open block jb into the tail.
+  auto leave_open = [&](int jb) {
+    const int lo = jb == 0 ? len0 % kQ8Block : 0, hi = end % kQ8Block;
+    const int64_t r0 = (int64_t)(b0 + jb) * kQ8Block - len0;
+    uint32_t mag = 0u;
+    for (int e = tid; e < (hi - lo) * CPR; e += kHalf) {
+      const int row = lo + e / CPR, c = e % CPR;
+      const uint16_t *s = src + (r0 + row) * rd.token + 16 * c;
+      const u32x4 a = ld16(s), b = ld16(s + 8);
+      st16(tail + row * D + 16 * c, a);
+      st16(tail + row * D + 16 * c + 8, b);
+      mag = max_mag(max_mag(max_mag(max_mag(mag, a.x), a.y), a.z), a.w);
+      mag = max_mag(max_mag(max_mag(max_mag(mag, b.x), b.y), b.z), b.w);
+    }
+    const float s = open_scale(half_max(sm.red, mag, side, tid));
+    if (tid == 0) stg(scales + blk0 + jb, lo > 0 ? fmaxf(s, ldg(scales + blk0 + jb)) : s);
+  };
+  if (j < nblk - 1 || !open) seal(j);
+  if (j == 0 && open) leave_open(nblk - 1);  // (every tail row of a sealed block 0 was read before a barrier)
+  // One workgroup a unit: every thread has read the length (a barrier ago).
+  if (p.nj == 1 && threadIdx.x == 0) stg(p.c.len + u, end);
+}
+
+// The lengths, where several workgroups of a unit read them.
+__global__ __launch_bounds__(256) void k_append_len(Q8Rows p) {
+  const int u = (int)(blockIdx.x * 256 + threadIdx.x);
+  if (u >= p.units) return;
+  const int len0 = max(ldg(p.c.len + u), 0);
+  const int want = p.count ? min(max(ldg(p.count + u / p.Hkv), 0), p.n) : p.n;
+  const int m = min(want, max(ldg(p.c.cap + u) - len0, 0));
+  if (m > 0) stg(p.c.len + u, len0 + m);
+}
+
+// N values, already read, to a row: bf16 or fp32.
+template <bool F32>
+__device__ __forceinline__ void put8(char *dst, const float (&f)[8]) {
+  if (F32) {
+    st16(dst, u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])});
+    st16(dst + 16, u32x4{__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7])});
+  } else {
+    st16(dst, u32x4{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])});
+  }
+}
+
+// Workgroup (unit, block): the block's rows below the unit's length (and the
+// row bound) as code * scale, or the tail's rows.
+template <int D, int FMT, bool F32>
+__global__ __launch_bounds__(kThreads) void k_read_rows(Q8Rows p) {
+  constexpr int VP = kQ8Block + 4;  // pitch of a channel's codes, bytes
+  constexpr int E = F32 ? 4 : 2;
+  __shared__ uint32_t vt[D * VP / 4];
+  const int u = (int)(blockIdx.x / (uint32_t)p.nj), j = (int)(blockIdx.x % (uint32_t)p.nj);
+  const int side = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 8), tid = threadIdx.x & 255;
+  const int len = max(min(ldg(p.c.len + u), ldg(p.c.cap + u)), 0);
+  const int rows = min(min(len, p.n) - j * kQ8Block, kQ8Block);
+  if (rows <= 0) return;
+  const int64_t blk = ldg(p.c.row_off + u) / kQ8Block + j;
+  const RowsDesc &rd = side ? p.v : p.k;
+  char *out = reinterpret_cast<char *>(rd.base) +
+              E * (unit_base(rd, p.unit_off, u, p.B, p.Hkv) + (int64_t)j * kQ8Block * rd.token);
+  const int64_t pitch = E * rd.token;
+  if (j >= len / kQ8Block) {  // uniform: the open block
+    const uint16_t *tail = (side ? p.c.vt : p.c.kt) + (int64_t)u * kQ8Block * D;
+    for (int e = tid; e < rows * (D / 8); e += kHalf) {
+      const int row = e / (D / 8), c = e % (D / 8);
+      const u32x4 x = ld16(tail + row * D + 8 * c);
+      const float f[8] = {bf16_lo(x.x), bf16_hi(x.x), bf16_lo(x.y), bf16_hi(x.y),
+                          bf16_lo(x.z), bf16_hi(x.z), bf16_lo(x.w), bf16_hi(x.w)};
+      put8<F32>(out + row * pitch + E * 8 * c, f);
+    }
+    return;
+  }
+  const uint8_t *codes = (side ? p.c.vc : p.c.kc) + blk * (kQ8Block * D);
+  const float s = ldg((side ? p.c.vs : p.c.ks) + blk);
+  if (side == 1) {
+#pragma unroll
+    for (int e = tid; e < D * kQ8Block / 16; e += kHalf) {
+      const int ch = e / 4, rg = e % 4;
+      const u32x4 x = ld16(codes + ch * kQ8Block + 16 * rg);
+      uint32_t *t = vt + ch * (VP / 4) + 4 * rg;
+      t[0] = x.x;
+      t[1] = x.y;
+      t[2] = x.z;
+      t[3] = x.w;
+    }
+  }
+  __syncthreads();
+  if (side == 0) {
+#pragma unroll
+    for (int e = tid; e < kQ8Block * D / 16; e += kHalf) {
+      const int row = e / (D / 16), c = e % (D / 16);
+      const u32x4 x = ld16(codes + row * D + 16 * c);
+      const uint32_t ws[4] = {x.x, x.y, x.z, x.w};
+      if (row < rows) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float a[4], b[4];
+          Q8<FMT>::unpack4(ws[2 * h], a);
+          Q8<FMT>::unpack4(ws[2 * h + 1], b);
+          const float f[8] = {a[0] * s, a[1] * s, a[2] * s, a[3] * s, b[0] * s, b[1] * s, b[2] * s, b[3] * s};
+          put8<F32>(out + row * pitch + E * (16 * c + 8 * h), f);
+        }
+      }
+    }
+  } else {
+    // Thread: channels 8 co .. + 7 of rows 4 rq .. + 3.
+#pragma unroll
+    for (int e = tid; e < (D / 8) * 16; e += kHalf) {
+      const int co = e % (D / 8), rq = e / (D / 8);
+      uint32_t w[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) w[k] = vt[(8 * co + k) * (VP / 4) + rq];
+      const u32x4 a = transpose4(w[0], w[1], w[2], w[3]), b = transpose4(w[4], w[5], w[6], w[7]);
+      const uint32_t as[4] = {a.x, a.y, a.z, a.w}, bs[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        if (4 * rq + r >= rows) continue;
+        float x[4], y[4];
+        Q8<FMT>::unpack4(as[r], x);
+        Q8<FMT>::unpack4(bs[r], y);
+        const float f[8] = {x[0] * s, x[1] * s, x[2] * s, x[3] * s, y[0] * s, y[1] * s, y[2] * s, y[3] * s};
+        put8<F32>(out + (4 * rq + r) * pitch + E * 8 * co, f);
+      }
+    }
+  }
+}
+
+template <int FMT>
+hipError_t append(const Q8Rows &p, hipStream_t st) {
+  const dim3 grid((uint32_t)((int64_t)p.units * p.nj)), block(kThreads);
+  if (p.d == 128)
+    hipLaunchKernelGGL((k_append_rows<128, FMT>), grid, block, 0, st, p);
+  else
+    hipLaunchKernelGGL((k_append_rows<64, FMT>), grid, block, 0, st, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.nj == 1) return e;
+  hipLaunchKernelGGL(k_append_len, dim3((uint32_t)((p.units + 255) / 256)), dim3(256), 0, st, p);
+  return hipGetLastError();
+}
+
+template <int FMT, bool F32>
+hipError_t read(const Q8Rows &p, hipStream_t st) {
+  const dim3 grid((uint32_t)((int64_t)p.units * p.nj)), block(kThreads);
+  if (p.d == 128)
+    hipLaunchKernelGGL((k_read_rows<128, FMT, F32>), grid, block, 0, st, p);
+  else
+    hipLaunchKernelGGL((k_read_rows<64, FMT, F32>), grid, block, 0, st, p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_q8_append(const Q8Rows &p, int format, hipStream_t st) {
+  return format == kInt8 ? append<kInt8>(p, st) : append<kE4m3>(p, st);
+}
+
+hipError_t launch_q8_read(const Q8Rows &p, int format, hipStream_t st) {
+  if (format == kInt8) return p.fp32 ? read<kInt8, true>(p, st) : read<kInt8, false>(p, st);
+  return p.fp32 ? read<kE4m3, true>(p, st) : read<kE4m3, false>(p, st);
+}
+
+}  // namespace vc

@@ -1,0 +1,399 @@
+// k_q8_decode.hip -- attention over the 8-bit cache for single tokens (up to
+// 16 (token, query head) columns per kv head).
+//
+// Bound by memory: every code is read once, by one wave, and used for all the
+// columns of its kv head.  The codes enter the matrix cores as fp16, in which
+// int8 and e4m3 are exact; the query's bf16 values are scaled by a power of two
+// per head and are exact there too.  A block's key scale multiplies its
+// logits, its value scale the block's product:
+//   O <- alpha O + vs_b (P_b Vc_b),  P split in two fp16 parts (22 bits),
+// so nothing below fp32 is rounded on the way.
+//
+// Layout: S^T = K Q^T with the rows of a 64-row block dealt to the matrix
+// rows so that a lane ends with the logits of rows 16 lg .. 16 lg + 15 of its
+// column; those are the k-elements of P^T, and the value codes' channel-major
+// order gives the same 16 rows in one 16-byte load, so neither P nor V passes
+// through LDS.  The open block's bf16 rows take the same path, scaled into
+// fp16 by their power of two, their values transposed through LDS.
+#include "vc_q8_device.h"
+
+namespace vc {
+
+namespace {
+
+constexpr float kNegInf = -__builtin_inff();
+
+__device__ __forceinline__ f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+// Eight bf16 values times a power of two, as fp16.
+__device__ __forceinline__ f16x8 half8_of_bf16(u32x4 w, float f) {
+  const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+  f16x8 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    r[2 * i] = (_Float16)(bf16_lo(ws[i]) * f);
+    r[2 * i + 1] = (_Float16)(bf16_hi(ws[i]) * f);
+  }
+  return r;
+}
+
+// Device-coherent accesses for partials that cross XCDs inside a launch.
+__device__ __forceinline__ void st_dev(float *p, float v) {
+  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float ld_dev(const float *p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+template <int D>
+struct Smem {
+  static constexpr int VP = D + 16;  // pitch of the open block's values: conflict-free transposing reads
+  static constexpr size_t kO = sizeof(float) * 4 * 16 * (D + 4);
+  static constexpr size_t kT = sizeof(uint16_t) * kQ8Block * VP;
+  // The open block's values (one wave, in its loop), then the waves' O.
+  uint8_t buf[kO > kT ? kO : kT] __attribute__((aligned(16)));
+  float2 ml[4][16];
+  float2 mlb[16][16];  // (max, sum) of a batch of partials being merged
+  uint32_t last;
+};
+
+// What a wave carries over its blocks, per lane: the column's running maximum
+// and its own rows' sum, and O^T (channels 16 mb + 4 lg + i of column lr).
+template <int D>
+struct State {
+  float m, l;
+  f32x4 O[D / 16];
+};
+
+// One block's logits into the state: S (raw products; row 16 lg + 4 rb + i in
+// S[rb][i]) times c, rows at or past `end` masked, and the products with the
+// values, whose fragments va(mb, x) holds channel 16 mb + lr, rows 16 lg + 8 x.
+template <int D, bool HILO, typename VA>
+__device__ __forceinline__ void absorb(State<D> &st, f32x4 (&S)[4], float c, float vs, int row0, int end, bool mask,
+                                       int lg, VA va) {
+  constexpr int MB = D / 16;
+  c = fmaxf(c, 1e-37f);  // not zero, so that a masked row stays at -inf
+  if (mask) {
+#pragma unroll
+    for (int rb = 0; rb < 4; ++rb)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (row0 + 16 * lg + 4 * rb + i >= end) S[rb][i] = kNegInf;
+  }
+  float mx = S[0][0];
+#pragma unroll
+  for (int k = 1; k < 16; ++k) mx = fmaxf(mx, S[k / 4][k % 4]);
+  mx = fmaxf(mx, swap16(mx));
+  mx = max_halves(mx) * c;
+  const float mn = fmaxf(st.m, mx);
+  const float ref = mn == kNegInf ? 0.f : mn;
+  if (__builtin_amdgcn_ballot_w64(mn != st.m)) {  // some column's maximum moved
+    const float alpha = fast_exp2(st.m - ref);
+    st.l *= alpha;
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) st.O[mb] *= alpha;
+  }
+  st.m = mn;
+  f16x8 hi[2], lo[2];
+  float sum = 0.f;
+#pragma unroll
+  for (int rb = 0; rb < 4; ++rb)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float pr = fast_exp2(fmaf(S[rb][i], c, -ref));
+      sum += pr;
+      // 2^14 keeps the small ones clear of fp16's subnormals.
+      const float ps = pr * 16384.f;
+      const _Float16 h = (_Float16)ps;
+      hi[rb / 2][4 * (rb & 1) + i] = h;
+      if (HILO) lo[rb / 2][4 * (rb & 1) + i] = (_Float16)(ps - (float)h);
+    }
+  st.l += sum;
+#pragma unroll
+  for (int mb = 0; mb < MB; ++mb) {
+    f32x4 t = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const f16x8 v = va(mb, x);
+      t = mfma16(v, hi[x], t);
+      if (HILO) t = mfma16(v, lo[x], t);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) st.O[mb][i] = fmaf(t[i], vs, st.O[mb][i]);
+  }
+}
+
+__device__ __forceinline__ u32x2 lds_read_tr16(const uint16_t *p) {
+  typedef short v4i16 __attribute__((ext_vector_type(4)));
+  const v4i16 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4i16 *)(p));
+  return __builtin_bit_cast(u32x2, v);
+}
+
+// Columns of the products: column c is query c / G, head c % G of its kv head.
+__device__ __forceinline__ int64_t out_row(const Q8Attn &p, const RowsDesc &r, int u, int col) {
+  const int g = u % p.Hkv, lb = u / p.Hkv;
+  const int i = col / p.G, h = col % p.G;
+  return (int64_t)(lb / p.B) * r.layer + (int64_t)(lb % p.B) * r.seq + (int64_t)i * r.token +
+         (int64_t)(g * p.G + h) * r.head;
+}
+
+__device__ __forceinline__ void put(const Q8Attn &p, int64_t at, float v) {
+  if (p.fp32)
+    stg(reinterpret_cast<float *>(p.out.base) + at, v);
+  else
+    stg(reinterpret_cast<uint16_t *>(p.out.base) + at, (uint16_t)pack_bf16(v, 0.f));
+}
+
+// Workgroup (unit, piece): blocks [j piece, (j + 1) piece) of the unit, dealt
+// to the four waves in turn.
+template <int D, int FMT, bool HILO>
+__global__ __launch_bounds__(256, 2) void k_decode8(Q8Attn p) {
+  constexpr int MB = D / 16, CH = D / 64;
+  __shared__ Smem<D> sm;
+  const int u = (int)(blockIdx.x / (uint32_t)p.npmax), j = (int)(blockIdx.x % (uint32_t)p.npmax);
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 15, lg = lane >> 4;
+  const int b = u / p.Hkv % p.B;
+  const int len = max(min(ldg(p.c.len + u), ldg(p.c.cap + u)), 0);
+  const int cnt = p.count ? min(max(ldg(p.count + b), 0), p.n) : p.n;
+  const int cols = cnt * p.G;
+  const int emax = cols > 0 ? min(len, p.max_rows) : 0;  // rows any column sees
+  const int nt = (emax + kQ8Block - 1) / kQ8Block;
+  const int np = max((nt + p.piece - 1) / p.piece, 1);
+  if (j >= np || cols == 0) return;
+  // Rows this lane's column sees, and the fewest any column does.
+  const int qi = min(lr, cols - 1) / p.G;
+  const int lim = p.causal ? len - cnt + 1 : len;
+  const int end = max(min(p.causal ? lim + qi : len, p.max_rows), 0);
+  const int emin = min(lim, p.max_rows);
+  const int64_t blk0 = ldg(p.c.row_off + u) / kQ8Block;
+  const int nsealed = len / kQ8Block;
+
+  // The column's query as fp16 operands, scaled by a power of two.
+  f16x8 q[CH][2];
+  float cq;
+  {
+    const uint16_t *qp = reinterpret_cast<const uint16_t *>(p.q.base) + out_row(p, p.q, u, min(lr, cols - 1));
+    u32x4 x[CH][2];
+    uint32_t mag = 0u;
+#pragma unroll
+    for (int h = 0; h < CH; ++h)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        x[h][k] = ld16(qp + 64 * h + 16 * lg + 8 * k);
+        mag = max_mag(max_mag(max_mag(max_mag(mag, x[h][k].x), x[h][k].y), x[h][k].z), x[h][k].w);
+      }
+    uint32_t mm = max(mag & 0xFFFFu, mag >> 16);
+    mm = max(mm, (uint32_t)__shfl_xor((int)mm, 16, 64));
+    mm = max(mm, (uint32_t)__shfl_xor((int)mm, 32, 64));
+    const float qs = open_scale(mm);
+    cq = p.sc * qs;
+    const float inv = 1.f / qs;  // exact: a power of two
+#pragma unroll
+    for (int h = 0; h < CH; ++h)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) q[h][k] = half8_of_bf16(x[h][k], inv);
+  }
+
+  State<D> st;
+  st.m = kNegInf;
+  st.l = 0.f;
+#pragma unroll
+  for (int mb = 0; mb < MB; ++mb) st.O[mb] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  const int t0 = j * p.piece, t1 = min(nt, t0 + p.piece);
+  const int ts = min(t1, nsealed);  // sealed blocks end
+  const int krow = 16 * (lr >> 2) + (lr & 3);
+  u32x4 kc[4][CH], vcode[MB];
+  float ks = 0.f, vs = 0.f;
+  auto load_k = [&](int t) {
+    const uint8_t *k = p.c.kc + (blk0 + t) * (kQ8Block * D);
+#pragma unroll
+    for (int rb = 0; rb < 4; ++rb)
+#pragma unroll
+      for (int h = 0; h < CH; ++h) kc[rb][h] = ld16(k + (krow + 4 * rb) * D + 64 * h + 16 * lg);
+    ks = ldg(p.c.ks + blk0 + t);
+  };
+  auto load_v = [&](int t) {
+    const uint8_t *v = p.c.vc + (blk0 + t) * (kQ8Block * D);
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) vcode[mb] = ld16(v + (16 * mb + lr) * kQ8Block + 16 * lg);
+    vs = ldg(p.c.vs + blk0 + t);
+  };
+  int t = t0 + w;
+  if (t < ts) {
+    load_k(t);
+    load_v(t);
+  }
+  for (; t < ts; t += 4) {
+    f32x4 S[4];
+#pragma unroll
+    for (int rb = 0; rb < 4; ++rb) {
+      S[rb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int h = 0; h < CH; ++h) {
+        S[rb] = mfma16(Q8<FMT>::half8(kc[rb][h].x, kc[rb][h].y), q[h][0], S[rb]);
+        S[rb] = mfma16(Q8<FMT>::half8(kc[rb][h].z, kc[rb][h].w), q[h][1], S[rb]);
+      }
+    }
+    const float c = cq * ks, v = vs;
+    const int tn = min(t + 4, ts - 1);  // the last block again where there is no next (never used)
+    load_k(tn);
+    absorb<D, HILO>(st, S, c, v, t * kQ8Block, end, (t + 1) * kQ8Block > emin, lg, [&](int mb, int x) {
+      return x == 0 ? Q8<FMT>::half8(vcode[mb].x, vcode[mb].y) : Q8<FMT>::half8(vcode[mb].z, vcode[mb].w);
+    });
+    load_v(tn);
+  }
+  // The open block, if it is in this piece and this wave's turn.
+  if (nsealed >= t0 && nsealed < t1 && (nsealed - t0) % 4 == w) {
+    const int rows = len - nsealed * kQ8Block;  // 1 .. 63
+    const uint16_t *kt = p.c.kt + (int64_t)u * kQ8Block * D, *vt = p.c.vt + (int64_t)u * kQ8Block * D;
+    const float kse = ldg(p.c.ks + blk0 + nsealed), vse = ldg(p.c.vs + blk0 + nsealed);
+    const float kinv = 1.f / kse, vinv = 1.f / vse;  // powers of two
+    uint16_t *lv = reinterpret_cast<uint16_t *>(sm.buf);
+#pragma unroll 4
+    for (int it = 0; it < D / 8; ++it) {
+      const int e = lane + 64 * it;
+      const int row = e / (D / 8), cc = e % (D / 8);
+      // Rows past the end hold anything: zeros meet their zero weights.
+      const u32x4 x = row < rows ? ld16(vt + row * D + 8 * cc) : u32x4{0u, 0u, 0u, 0u};
+      *reinterpret_cast<f16x8 *>(lv + row * Smem<D>::VP + 8 * cc) = half8_of_bf16(x, vinv);
+    }
+    f32x4 S[4];
+#pragma unroll
+    for (int rb = 0; rb < 4; ++rb) {
+      S[rb] = f32x4{0.f, 0.f, 0.f, 0.f};
+      const uint16_t *k = kt + min(krow + 4 * rb, rows - 1) * D + 16 * lg;
+#pragma unroll
+      for (int h = 0; h < CH; ++h)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) S[rb] = mfma16(half8_of_bf16(ld16(k + 64 * h + 8 * x), kinv), q[h][x], S[rb]);
+    }
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): this wave's LDS writes landed
+    __builtin_amdgcn_wave_barrier();
+    absorb<D, HILO>(st, S, cq * kse, vse, nsealed * kQ8Block, end, true, lg, [&](int mb, int x) {
+      const uint16_t *base = lv + (16 * lg + 8 * x + (lr >> 2)) * Smem<D>::VP + 16 * mb + 4 * (lr & 3);
+      const u32x2 a = lds_read_tr16(base), bb = lds_read_tr16(base + 4 * Smem<D>::VP);
+      return __builtin_bit_cast(f16x8, u32x4{a.x, a.y, bb.x, bb.y});
+    });
+    __builtin_amdgcn_s_waitcnt(0xc07f);
+  }
+
+  // The four waves' states.
+  st.l = sum_halves(st.l + swap16(st.l));
+  __syncthreads();  // the open block's values are read
+  float(*wo)[16][D + 4] = reinterpret_cast<float(*)[16][D + 4]>(sm.buf);
+#pragma unroll
+  for (int mb = 0; mb < MB; ++mb)
+    *reinterpret_cast<f32x4 *>(&wo[w][lr][16 * mb + 4 * lg]) = st.O[mb];
+  if (lg == 0) sm.ml[w][lr] = make_float2(st.m, st.l);
+  __syncthreads();
+  const int x = tid % D;
+  const int64_t slot = (int64_t)u * p.npmax + j;
+  for (int col = tid / D; col < cols; col += 256 / D) {
+    float M = kNegInf;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) M = fmaxf(M, sm.ml[k][col].x);
+    float o = 0.f, s = 0.f;
+    if (M != kNegInf) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float f = fast_exp2(sm.ml[k][col].x - M);
+        o += f * wo[k][col][x];
+        s += f * sm.ml[k][col].y;
+      }
+    }
+    o *= 0x1p-14f;
+    if (np == 1) {
+      put(p, out_row(p, p.out, u, col) + x, s > 0.f ? o / s : 0.f);
+    } else {
+      st_dev(p.part_o + (slot * 16 + col) * D + x, o);
+      if (x == 0) {
+        float *ml = reinterpret_cast<float *>(p.part_ml + slot * 16 + col);
+        st_dev(ml, M);
+        st_dev(ml + 1, s);
+      }
+    }
+  }
+  if (np == 1) return;
+  // A unit in several pieces: the last to arrive merges them, in row order.
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+  if (tid == 0)
+    sm.last = __hip_atomic_fetch_add(p.arrive + u, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(np - 1);
+  __syncthreads();
+  if (!sm.last) return;
+  if (tid == 0) __hip_atomic_store(p.arrive + u, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  constexpr int kEl = 16 * D / 256;
+  float M[kEl], o[kEl], s[kEl];
+#pragma unroll
+  for (int k = 0; k < kEl; ++k) {
+    M[k] = kNegInf;
+    o[k] = s[k] = 0.f;
+  }
+  const int64_t slot0 = (int64_t)u * p.npmax;
+  for (int j0 = 0; j0 < np; j0 += 16) {
+    const int nb = min(16, np - j0);
+    __syncthreads();
+    {
+      const int pc = tid >> 4, col = tid & 15;
+      if (pc < nb && col < cols) {
+        const float *ml = reinterpret_cast<const float *>(p.part_ml + (slot0 + j0 + pc) * 16 + col);
+        sm.mlb[pc][col] = make_float2(ld_dev(ml), ld_dev(ml + 1));
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kEl; ++k) {
+      const int col = tid / D + k * (256 / D);
+      if (col >= cols) continue;
+      float Mc = M[k];
+      for (int pc = 0; pc < nb; ++pc) Mc = fmaxf(Mc, sm.mlb[pc][col].x);
+      if (Mc == kNegInf) continue;
+      const float a = fast_exp2(M[k] - Mc);
+      o[k] *= a;
+      s[k] *= a;
+      M[k] = Mc;
+      for (int p0 = 0; p0 < nb; p0 += 8) {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          v[e] = ld_dev(p.part_o + ((slot0 + j0 + min(p0 + e, nb - 1)) * 16 + col) * D + x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          if (p0 + e >= nb) continue;
+          const float2 ml = sm.mlb[p0 + e][col];
+          const float f = fast_exp2(ml.x - Mc);
+          o[k] += f * v[e];
+          s[k] += f * ml.y;
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < kEl; ++k) {
+    const int col = tid / D + k * (256 / D);
+    if (col < cols) put(p, out_row(p, p.out, u, col) + x, s[k] > 0.f ? o[k] / s[k] : 0.f);
+  }
+}
+
+template <int D, int FMT>
+hipError_t launch(const Q8Attn &p, hipStream_t st) {
+  const dim3 grid((uint32_t)((int64_t)p.units * p.npmax)), block(256);
+  if (p.fp32)
+    hipLaunchKernelGGL((k_decode8<D, FMT, true>), grid, block, 0, st, p);
+  else
+    hipLaunchKernelGGL((k_decode8<D, FMT, false>), grid, block, 0, st, p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_q8_decode(const Q8Attn &p, int format, hipStream_t st) {
+  if (p.d == 128) return format == kInt8 ? launch<128, kInt8>(p, st) : launch<128, kE4m3>(p, st);
+  return format == kInt8 ? launch<64, kInt8>(p, st) : launch<64, kE4m3>(p, st);
+}
+
+}  // namespace vc

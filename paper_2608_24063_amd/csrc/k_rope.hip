@@ -1,0 +1,153 @@
+// k_rope.hip -- rotary positions with several axes: the pair (x1, x2) of
+// frequency i turns by a = pos[axis(i)] f_i, so that a visual token's time,
+// height and width each turn their own channels.  The angle is reduced in 64
+// bits, as a number of turns (pos f_i / 2 pi less its nearest whole number):
+// in 32 bits a position of 2^20 would leave 2^-4 of a turn unknown.  Sine and
+// cosine of the reduced angle and the rotation itself are in 32 bits, rounded
+// once to the output's type.  The gradient of the rotation is the rotation by
+// -a (the sign of the sine).
+//
+// Bound by memory: every value is read and written once.  A token's d/2
+// (sine, cosine) pairs serve all of its heads, so they are computed once per
+// token and layer, one per thread, and shared through LDS; a lane then keeps
+// the pairs of its own channels in registers while it walks the heads.
+#include "vc_device.h"
+#include "vc_q8.h"
+
+namespace vc {
+
+namespace {
+
+// 16 bytes of a row as floats, and back.
+template <bool F32>
+struct Chunk {
+  static constexpr int N = F32 ? 4 : 8;
+  static __device__ __forceinline__ void unpack(u32x4 w, float (&f)[N]) {
+    const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (F32) {
+        f[i] = __uint_as_float(ws[i]);
+      } else {
+        f[(2 * i) % N] = bf16_lo(ws[i]);
+        f[(2 * i + 1) % N] = bf16_hi(ws[i]);
+      }
+    }
+  }
+  static __device__ __forceinline__ u32x4 pack(const float (&f)[N]) {
+    if (F32)
+      return u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
+    return u32x4{pack_bf16(f[0], f[1]), pack_bf16(f[2 % N], f[3 % N]), pack_bf16(f[4 % N], f[5 % N]),
+                 pack_bf16(f[6 % N], f[7 % N])};
+  }
+};
+
+// A workgroup takes TPW tokens of one layer, each with 4 / TPW waves.
+template <bool F32, bool ADJ, int TPW>
+__global__ __launch_bounds__(256) void k_rope(RopePlan p) {
+  using C = Chunk<F32>;
+  constexpr int N = C::N;
+  constexpr int kWaves = 4 / TPW;  // waves per token
+  __shared__ float2 cs[TPW][kRopeMaxHalf];
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t toks = (int64_t)p.B * p.n;
+  const int64_t groups = (toks + TPW - 1) / TPW;
+  const int64_t bid = blockIdx.x;
+  const int l = (int)(bid / groups);
+  const int64_t g0 = bid % groups * TPW;
+  const int half = p.rot / 2;
+  // (sine, cosine) of token g0 + t, frequency i.
+  for (int e = tid; e < TPW * kRopeMaxHalf; e += 256) {
+    const int t = e / kRopeMaxHalf, i = e % kRopeMaxHalf;
+    const int64_t g = g0 + t;
+    if (i < half && g < toks) {
+      const int axis = (int)(p.axis1 >> i & 1) + 2 * (int)(p.axis2 >> i & 1);
+      const double a = (double)ldg(p.pos + axis * toks + g) * p.turns[i];
+      float s, c;
+      sincospif(2.f * (float)(a - rint(a)), &s, &c);
+      cs[t][i] = make_float2(c * p.scale, s * p.scale * p.sgn);
+    }
+  }
+  __syncthreads();
+  const int t = w / kWaves, sub = w % kWaves;
+  const int64_t g = g0 + t;
+  if (g >= toks) return;
+  const int b = (int)(g / p.n), i = (int)(g % p.n);
+  if (p.count && i >= ldg(p.count + b)) return;
+  // Lane: chunk pair c of head h.  Halves: channels [Nc, Nc+N) and the same
+  // past rot/2; adjacent: 2N channels in a row.  Lanes past the rotated
+  // channels copy the rest.
+  const int per = p.d / (2 * N);    // chunk pairs per row (a power of two)
+  const int rper = p.rot / (2 * N);  // rotated ones
+  const int c = lane % per, hl = lane / per, hs = 64 / per;
+  const bool turn = c < rper;
+  const int o1 = turn ? (ADJ ? 2 * N * c : N * c) : 2 * N * c;
+  const int o2 = turn ? (ADJ ? 2 * N * c + N : half + N * c) : 2 * N * c + N;
+  float co[N], si[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    // Frequencies of this lane: N of them, for the halves Nc + k, for
+    // adjacent pairs Nc + k as well (2N channels hold N pairs).
+    const float2 v = turn ? cs[t][N * c + k] : make_float2(1.f, 0.f);
+    co[k] = v.x;
+    si[k] = v.y;
+  }
+  const int H = p.Hq + p.Hkv;
+  for (int h = sub * hs + hl; h < H; h += kWaves * hs) {
+    const bool isq = h < p.Hq;
+    const RowsDesc &ri = isq ? p.qi : p.ki;
+    const RowsDesc &ro = isq ? p.qo : p.ko;
+    const int hh = isq ? h : h - p.Hq;
+    const int64_t eb = F32 ? 4 : 2;
+    const char *src = reinterpret_cast<const char *>(ri.base) +
+                      eb * (l * ri.layer + b * ri.seq + i * ri.token + hh * ri.head);
+    char *dst = reinterpret_cast<char *>(ro.base) + eb * (l * ro.layer + b * ro.seq + i * ro.token + hh * ro.head);
+    float x[N], y[N];
+    C::unpack(ld16(src + eb * o1), x);
+    C::unpack(ld16(src + eb * o2), y);
+    if (turn) {
+      if (ADJ) {
+        // Pairs (2m, 2m+1): N/2 of them in x, N/2 in y.
+#pragma unroll
+        for (int m = 0; m < N / 2; ++m) {
+          const float a = x[2 * m], bq = x[2 * m + 1];
+          x[2 * m] = a * co[m] - bq * si[m];
+          x[2 * m + 1] = bq * co[m] + a * si[m];
+          const float e = y[2 * m], f = y[2 * m + 1];
+          y[2 * m] = e * co[N / 2 + m] - f * si[N / 2 + m];
+          y[2 * m + 1] = f * co[N / 2 + m] + e * si[N / 2 + m];
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          const float a = x[k], e = y[k];
+          x[k] = a * co[k] - e * si[k];
+          y[k] = e * co[k] + a * si[k];
+        }
+      }
+    }
+    st16(dst + eb * o1, C::pack(x));
+    st16(dst + eb * o2, C::pack(y));
+  }
+}
+
+template <bool F32, bool ADJ>
+hipError_t launch(const RopePlan &p, hipStream_t st) {
+  const int64_t toks = (int64_t)p.B * p.n;
+  if (toks * p.L >= 4 * 2048) {
+    const int64_t grid = (toks + 3) / 4 * p.L;
+    hipLaunchKernelGGL((k_rope<F32, ADJ, 4>), dim3((uint32_t)grid), dim3(256), 0, st, p);
+  } else {
+    hipLaunchKernelGGL((k_rope<F32, ADJ, 1>), dim3((uint32_t)(toks * p.L)), dim3(256), 0, st, p);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rope(const RopePlan &p, hipStream_t st) {
+  if (p.fp32) return p.adjacent ? launch<true, true>(p, st) : launch<true, false>(p, st);
+  return p.adjacent ? launch<false, true>(p, st) : launch<false, false>(p, st);
+}
+
+}  // namespace vc

@@ -1,0 +1,76 @@
+// vc_q8.h -- plans and host launchers of the 8-bit cache (append, read back,
+// attention) and of the rotary positions.  Internal.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace vc {
+
+constexpr int kQ8Block = 64;  // rows that share a scale (VC_Q8_BLOCK)
+
+// Row (l, b, i, h) of a strided tensor starts at base + l*layer + b*seq +
+// i*token + h*head elements.
+struct RowsDesc {
+  uint64_t base;
+  int64_t layer, seq, token, head;
+};
+
+// The cache, as in vc_q8cache.
+struct Q8Cache {
+  uint8_t *kc, *vc;
+  float *ks, *vs;
+  uint16_t *kt, *vt;
+  const int64_t *row_off;
+  const int32_t *cap;
+  int32_t *len;
+};
+
+struct Q8Rows {  // append (k, v read) and read back (k, v written)
+  Q8Cache c;
+  RowsDesc k, v;
+  const int64_t *unit_off;  // element offset of each unit's first row; null: the strides
+  const int32_t *count;     // append: rows per (layer, sequence); null: n
+  int32_t B, Hkv, d, units;
+  int32_t n;    // append: rows per unit; read: row bound
+  int32_t nj;   // workgroups per unit
+  int32_t fp32; // read: element type
+};
+
+struct Q8Attn {
+  Q8Cache c;
+  RowsDesc q, out;
+  const int32_t *count;  // queries per sequence; null: n
+  int32_t B, Hq, Hkv, G, d, units;
+  int32_t n, cols;       // queries per sequence; cols = n * G
+  int32_t causal, fp32;
+  int32_t max_rows;
+  float sc;              // scale * log2(e)
+  // One token at a time (cols <= 16): pieces of `piece` blocks, at most npmax
+  // a unit.  Prompts: nqt column tiles of qcols columns, each in ns key splits.
+  int32_t piece, npmax;
+  int32_t qcols, nqt, ns;
+  uint32_t *arrive;      // [units], zero between calls
+  float *part_o;
+  float2 *part_ml;
+};
+
+constexpr int kRopeMaxHalf = 64;
+struct RopePlan {
+  RowsDesc qi, qo, ki, ko;
+  const int32_t *pos;    // [3][B][n]
+  const int32_t *count;  // tokens per sequence; null: n
+  int32_t B, L, Hq, Hkv, d, n;  // Hq (Hkv) is 0 where there are no queries (keys)
+  int32_t rot, adjacent, fp32;
+  uint64_t axis1, axis2;  // bit i: frequency i turns with the height / the width
+  float scale, sgn;
+  double turns[kRopeMaxHalf];  // frequency i over 2 pi
+};
+
+hipError_t launch_q8_append(const Q8Rows &p, int format, hipStream_t st);
+hipError_t launch_q8_read(const Q8Rows &p, int format, hipStream_t st);
+hipError_t launch_q8_decode(const Q8Attn &p, int format, hipStream_t st);
+hipError_t launch_q8_prompt(const Q8Attn &p, int format, hipStream_t st);
+hipError_t launch_rope(const RopePlan &p, hipStream_t st);
+
+}  // namespace vc

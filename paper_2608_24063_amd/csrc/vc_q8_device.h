@@ -1,0 +1,113 @@
+// vc_q8_device.h -- the 8-bit types of the cache on gfx950: rounding to them,
+// and their values as fp32 and fp16 (int8 and e4m3 codes are exact in both).
+// Internal to libviscache.
+#pragma once
+#include "vc_device.h"
+#include "vc_q8.h"
+
+namespace vc {
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
+enum { kInt8 = 0, kE4m3 = 1 };
+
+template <int FMT>
+struct Q8 {
+  static constexpr float kTop = FMT == kInt8 ? 127.f : 448.f;
+  static constexpr float kEffMin = kTop * 0x1p-60f, kEffMax = kTop * 0x1p60f;
+
+  // Q x / eff to 20 significant bits, clamped.  x and eff are bf16 values (or
+  // eff a bound that makes inv a power of two), so the exact quotient is
+  // either a midpoint of two codes (at most 8 significant bits) or at least
+  // 2^-17 of itself away from every midpoint: for int8 |254 X 2^i - M A 2^j| >=
+  // 1 with X, A < 2^8 and M odd <= 253, for e4m3 |7 X 2^i - M A 2^j| >= 1 with
+  // M <= 31.  The product with the rounded inverse is off by less than 2^-22
+  // of itself; cutting it to 20 bits puts midpoints back where they are and
+  // moves nothing across one, so ties go to even without a division per value.
+  static __device__ __forceinline__ float code_value(float x, float inv) {
+    const float y = __uint_as_float((__float_as_uint(x * inv) + 8u) & ~15u);
+    return __builtin_amdgcn_fmed3f(y, -kTop, kTop);
+  }
+  // Codes of four values, the first in the low byte.
+  static __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
+    if (FMT == kInt8) {
+      // The sum with 1.5 * 2^23 rounds to a whole number, ties to even, and
+      // holds it in its low byte.
+      const uint32_t ia = __float_as_uint(a + 12582912.f), ib = __float_as_uint(b + 12582912.f);
+      const uint32_t ic = __float_as_uint(c + 12582912.f), id = __float_as_uint(d + 12582912.f);
+      const uint32_t lo = __builtin_amdgcn_perm(ib, ia, 0x0c0c0400u), hi = __builtin_amdgcn_perm(id, ic, 0x04000c0cu);
+      return lo | hi;
+    }
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+  }
+  // The four codes of a word as fp32.
+  static __device__ __forceinline__ void unpack4(uint32_t w, float (&f)[4]) {
+    if (FMT == kInt8) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) f[i] = (float)(int)(int8_t)(w >> (8 * i));
+      return;
+    }
+    const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+    f[0] = a[0];
+    f[1] = a[1];
+    f[2] = b[0];
+    f[3] = b[1];
+  }
+  // The four codes of a word as fp16: e4m3 by the converting instruction;
+  // int8, moved to 0..255, as the low bits of 1024 + u, less 1152.
+  static __device__ __forceinline__ u32x2 half4(uint32_t w) {
+    f16x2 a, b;
+    if (FMT == kInt8) {
+      const uint32_t u = w ^ 0x80808080u;
+      const f16x2 off = {(_Float16)-1152.f, (_Float16)-1152.f};
+      a = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) + off;
+      b = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) + off;
+    } else {
+      a = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.f, false));
+      b = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.f, true));
+    }
+    return u32x2{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)};
+  }
+  static __device__ __forceinline__ f16x8 half8(uint32_t w0, uint32_t w1) {
+    const u32x2 a = half4(w0), b = half4(w1);
+    return __builtin_bit_cast(f16x8, u32x4{a.x, a.y, b.x, b.y});
+  }
+};
+
+// Largest magnitude of packed bf16 pairs, as bf16 bits (unsigned compare of
+// the bits without the sign).
+__device__ __forceinline__ uint32_t max_mag(uint32_t m, uint32_t w) {
+  const u16x2 a = __builtin_bit_cast(u16x2, m), b = __builtin_bit_cast(u16x2, w & 0x7FFF7FFFu);
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(a, b));
+}
+
+// The power of two that puts a largest magnitude (bf16 bits) into [2^14,
+// 2^15), at least 2^-60: with it a row's bf16 values are exact in fp16 down to
+// 2^-28 of the largest.
+__device__ __forceinline__ float open_scale(uint32_t mag) {
+  const int e = max((int)(mag >> 7) - 14, 127 - 60);
+  return __uint_as_float((uint32_t)e << 23);
+}
+
+// 4 x 4 bytes transposed: byte j of word i becomes byte i of word j.
+__device__ __forceinline__ u32x4 transpose4(uint32_t w0, uint32_t w1, uint32_t w2, uint32_t w3) {
+  const uint32_t t0 = __builtin_amdgcn_perm(w1, w0, 0x05010400u), t1 = __builtin_amdgcn_perm(w3, w2, 0x05010400u);
+  const uint32_t t2 = __builtin_amdgcn_perm(w1, w0, 0x07030602u), t3 = __builtin_amdgcn_perm(w3, w2, 0x07030602u);
+  return u32x4{__builtin_amdgcn_perm(t1, t0, 0x05040100u), __builtin_amdgcn_perm(t1, t0, 0x07060302u),
+               __builtin_amdgcn_perm(t3, t2, 0x05040100u), __builtin_amdgcn_perm(t3, t2, 0x07060302u)};
+}
+
+// First element of row i of unit u = (l*B + b)*Hkv + g in a strided tensor.
+__device__ __forceinline__ int64_t unit_base(const RowsDesc &r, const int64_t *unit_off, int u, int B, int Hkv) {
+  if (unit_off) return ldg(unit_off + u);
+  const int g = u % Hkv, lb = u / Hkv;
+  return (int64_t)(lb / B) * r.layer + (int64_t)(lb % B) * r.seq + (int64_t)g * r.head;
+}
+
+}  // namespace vc

@@ -3,15 +3,18 @@ workspace that the C ABI asks for and passes device addresses and the current
 stream.  No computation happens here."""
 from __future__ import annotations
 
+import ctypes
+
 import torch
 
-from . import (VC_PRUNE_EVENTS, VC_RANK_GLOBAL, make_params, make_prune_io, make_shape, prune_with_io, vc_cache,
-               vc_decode_shape, vc_qcache, viscache_append_kv, viscache_budget, viscache_decode_attn,
+from . import (VC_PRUNE_EVENTS, VC_Q8_BLOCK, VC_Q8_E4M3, VC_Q8_INT8, VC_RANK_GLOBAL, make_params, make_prune_io, make_shape, prune_with_io, vc_cache,
+               vc_decode_shape, vc_q8cache, vc_qcache, vc_rope, vc_rows, viscache_append_kv, viscache_budget, viscache_decode_attn,
                viscache_decode_plan, viscache_decode_step, viscache_decode_step_noalloc,
                viscache_decode_step_planned, viscache_decode_step_q4,
                viscache_decode_step_workspace_bytes,
                viscache_decode_workspace_bytes, viscache_out_rows, viscache_prune_workspace_bytes,
-               viscache_quantize_rows)
+               viscache_q8_append, viscache_q8_attend, viscache_q8_attend_workspace_bytes, viscache_q8_read,
+               viscache_quantize_rows, viscache_rope)
 
 
 def _stream() -> int:
@@ -223,4 +226,249 @@ class DecodeCache:
                                 _stream())
 
 
-__all__ = ["PruneCall", "DecodeCache", "make_params"]
+def _rows(t: torch.Tensor, head_major: bool = False) -> vc_rows:
+    """The vc_rows of a tensor [L, B, n, H, d] ([L, B, H, n, d] with head_major)."""
+    sl, sb, s2, s3, sd = t.stride()
+    if sd != 1 and t.shape[-1] != 1:
+        raise ValueError("rows must be contiguous")
+    return vc_rows(t.data_ptr(), sl, sb, s3, s2) if head_major else vc_rows(t.data_ptr(), sl, sb, s2, s3)
+
+
+def _expect(t: torch.Tensor, name: str, shape, dtypes, device) -> None:
+    if t.shape != shape or t.dtype not in dtypes or t.device != device:
+        raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype} on {t.device}, need {tuple(shape)} "
+                         f"{' or '.join(str(x) for x in dtypes)} on {device}")
+
+
+def _expect_ints(t, name: str, shape, device) -> int:
+    """Address of a contiguous int32 tensor (0 for None)."""
+    if t is None:
+        return 0
+    _expect(t, name, shape, (torch.int32,), device)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _device(device) -> torch.device:
+    d = torch.device(device)
+    return torch.device(d.type, torch.cuda.current_device()) if d.type == "cuda" and d.index is None else d
+
+
+class _On:
+    """The device as the current one, for as long as a call is enqueued."""
+
+    def __init__(self, device: torch.device):
+        self.device = device
+
+    def __enter__(self):
+        self.prev = torch.cuda.current_device()
+        if self.prev != self.device.index:
+            torch.cuda.set_device(self.device)
+        return torch.cuda.current_stream().cuda_stream
+
+    def __exit__(self, *exc):
+        if self.prev != self.device.index:
+            torch.cuda.set_device(self.prev)
+
+
+_BF16 = (torch.bfloat16,)
+_OUT = (torch.bfloat16, torch.float32)
+
+
+class Rope:
+    """Rotary positions with several axes (viscache_rope): head dim d, `rot`
+    rotated channels (all by default), `sections` frequencies for time, height
+    and width (one axis by default)."""
+
+    def __init__(self, d: int, rot: int | None = None, theta: float = 1e6, sections=None, layout: int = 0,
+                 pairing: int = 0, scale: float = 1.0, inv_freq=None):
+        self.d, rot = int(d), int(d if rot is None else rot)
+        sections = (rot // 2, 0, 0) if sections is None else tuple(int(x) for x in sections)
+        self._freq = None
+        if inv_freq is not None:
+            if len(inv_freq) != rot // 2:
+                raise ValueError(f"inv_freq: {len(inv_freq)} frequencies, need {rot // 2}")
+            self._freq = (ctypes.c_double * (rot // 2))(*[float(x) for x in inv_freq])
+        self._params = {}
+        for fp32 in (0, 1):
+            for inverse in (0, 1):
+                self._params[fp32, inverse] = vc_rope(rot, (ctypes.c_int32 * 3)(*sections), layout, pairing, fp32,
+                                                      inverse, scale, theta, self._freq)
+
+    def apply(self, pos, q=None, k=None, q_out=None, k_out=None, inverse: bool = False, count=None):
+        """Rotates q [L, B, n, Hq, d] and k [L, B, n, Hkv, d] (either may be
+        None; both bf16 or fp32) by pos int32 [3, B, n] into q_out and k_out, by
+        default in place, on the current stream of their device.  `inverse`
+        turns back, which is the gradient.  Returns (q_out, k_out)."""
+        ref = q if q is not None else k
+        if ref is None:
+            raise ValueError("nothing to rotate")
+        L, B, n, _, d = ref.shape
+        Hq = q.shape[3] if q is not None else k.shape[3]
+        Hkv = k.shape[3] if k is not None else Hq
+        if q is not None and q_out is None:
+            q_out = q
+        if k is not None and k_out is None:
+            k_out = k
+        dev, typ = ref.device, ref.dtype
+        if typ not in _OUT or d != self.d or dev.type != "cuda":
+            raise ValueError(f"rows of {d} {typ} on {dev}, need {self.d} bf16 or fp32 on a GPU")
+        for t, name, H in ((q, "q", Hq), (q_out, "q_out", Hq), (k, "k", Hkv), (k_out, "k_out", Hkv)):
+            if t is not None:
+                _expect(t, name, (L, B, n, H, d), (typ,), dev)
+        cnt = _expect_ints(count, "count", (B,), dev)
+        at = _expect_ints(pos, "pos", (3, B, n), dev)
+        if ref.numel() == 0:
+            return q_out, k_out
+        r = [None if t is None else _rows(t) for t in (q, q_out, k, k_out)]
+        with _On(dev) as stream:
+            viscache_rope(vc_decode_shape(B, L, Hq, Hkv, d), self._params[int(typ == torch.float32), int(inverse)], n,
+                          at, cnt, r[0], r[1], r[2], r[3], stream)
+        return q_out, k_out
+
+
+_Q8_BUFFERS = ("k_codes", "v_codes", "k_scale", "v_scale", "k_tail", "v_tail", "row_off", "cap", "len")
+
+
+class Q8Cache:
+    """A decode cache in 8 bits (viscache_q8_*) over L layers x B sequences x
+    Hkv heads: unit u = (l*B + b)*Hkv + g has room for caps[u] rows.  format:
+    "int8" or "e4m3".  `buffers`: the cache's tensors by name (k_codes, v_codes,
+    k_scale, v_scale, k_tail, v_tail, row_off, cap, len), laid out as vc_q8cache
+    has them, where a program keeps them itself.
+
+    Calls go to the current stream of the cache's device.  Calls that attend
+    share one workspace and must be ordered on one stream."""
+
+    FORMATS = {"int8": (VC_Q8_INT8, torch.int8), "e4m3": (VC_Q8_E4M3, torch.float8_e4m3fn)}
+
+    def __init__(self, L, B, Hq, Hkv, d, caps, device, format: str = "e4m3", buffers=None):
+        self.L, self.B, self.Hq, self.Hkv, self.d = L, B, Hq, Hkv, d
+        self.shape = vc_decode_shape(B, L, Hq, Hkv, d)
+        self.device = _device(device)
+        self.units = L * B * Hkv
+        caps = [int(c) for c in caps]
+        if len(caps) != self.units or min(caps, default=0) < 0:
+            raise ValueError(f"{len(caps)} capacities, need {self.units}, none negative")
+        code, typ = self.FORMATS[format]
+        self.format = format
+        self.max_cap = max(caps)
+        offs, o = [], 0
+        for c in caps:
+            offs.append(o)
+            o += (c + VC_Q8_BLOCK - 1) // VC_Q8_BLOCK
+        nblk = max(o, 1)
+        need = {"k_codes": ((nblk, VC_Q8_BLOCK, d), typ), "v_codes": ((nblk, d, VC_Q8_BLOCK), typ),
+                "k_scale": ((nblk,), torch.float32), "v_scale": ((nblk,), torch.float32),
+                "k_tail": ((self.units, VC_Q8_BLOCK, d), torch.bfloat16),
+                "v_tail": ((self.units, VC_Q8_BLOCK, d), torch.bfloat16),
+                "row_off": ((self.units,), torch.int64), "cap": ((self.units,), torch.int32),
+                "len": ((self.units,), torch.int32)}
+        if buffers is None:
+            buffers = {name: torch.zeros(shape, dtype=t, device=self.device) for name, (shape, t) in need.items()}
+            buffers["row_off"] = torch.tensor(offs, dtype=torch.int64, device=self.device) * VC_Q8_BLOCK
+            buffers["cap"] = torch.tensor(caps, dtype=torch.int32, device=self.device)
+        for name, (shape, t) in need.items():
+            _expect(buffers[name], name, shape, (t,), self.device)
+            if not buffers[name].is_contiguous():
+                raise ValueError(f"{name} must be contiguous")
+            setattr(self, name, buffers[name])
+        self.c = vc_q8cache(code, *[buffers[name].data_ptr() for name in _Q8_BUFFERS])
+        self._ws, self._ws_bytes, self._kept = None, {}, []
+
+    def _workspace(self, n: int, max_rows: int):
+        """The workspace, grown when a call needs more than any before it (a
+        call that is captured into a graph must have run once before)."""
+        key = (n, max_rows)
+        need = self._ws_bytes.get(key)
+        if need is None:
+            need = self._ws_bytes[key] = viscache_q8_attend_workspace_bytes(self.shape, n, max_rows)
+        if self._ws is None or self._ws.numel() < need:
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("the workspace is too small: run the call once before it is captured")
+            self._ws = torch.zeros((max(need, 256),), dtype=torch.uint8, device=self.device)
+            self._kept.append(self._ws)  # a graph captured before this goes on using the one it was captured with
+        return self._ws
+
+    def append(self, k, v, count=None, head_major: bool = False) -> None:
+        """Appends k, v bf16 [L, B, n, Hkv, d] ([L, B, Hkv, n, d] with
+        head_major); count int32 [L*B]: the rows of each layer and sequence."""
+        n = k.shape[3 if head_major else 2]
+        want = (self.L, self.B, self.Hkv, n, self.d) if head_major else (self.L, self.B, n, self.Hkv, self.d)
+        _expect(k, "k", want, _BF16, self.device)
+        _expect(v, "v", want, _BF16, self.device)
+        cnt = _expect_ints(count, "count", (self.L * self.B,), self.device)
+        if n == 0:
+            return
+        with _On(self.device) as stream:
+            viscache_q8_append(self.shape, self.c, _rows(k, head_major), _rows(v, head_major), n, cnt, 0, stream)
+
+    def load_pruned(self, pc: "PruneCall") -> None:
+        """Appends what pc.run() left in its outputs (bf16 values): every
+        layer's kept rows, a launch or two a layer.  Evicted layers get none."""
+        if (pc.L, pc.B, pc.Hkv, pc.d) != (self.L, self.B, self.Hkv, self.d) or pc.params.v_out_fp32:
+            raise ValueError("the pruned cache has another shape, or fp32 values")
+        per = self.B * self.Hkv
+        one = vc_decode_shape(self.B, 1, self.Hq, self.Hkv, self.d)
+        count = torch.tensor([[pc.k[b * pc.L + l] for b in range(pc.B)] for l in range(pc.L)], dtype=torch.int32)
+        off = torch.tensor([[pc.unit_rows(l, b, g)[0] * self.d for b in range(pc.B) for g in range(pc.Hkv)]
+                            for l in range(pc.L)], dtype=torch.int64)
+        most = count.amax(dim=1).tolist()
+        count, off = count.to(self.device), off.to(self.device)
+        with _On(self.device) as stream:
+            for l in range(pc.L):
+                if most[l] == 0:
+                    continue
+                c = vc_q8cache(self.c.format, self.c.k_codes, self.c.v_codes, self.c.k_scale, self.c.v_scale,
+                               self.k_tail[l * per:].data_ptr(), self.v_tail[l * per:].data_ptr(),
+                               self.row_off[l * per:].data_ptr(), self.cap[l * per:].data_ptr(),
+                               self.len[l * per:].data_ptr())
+                _expect(pc.k_out[l], "k_out", pc.k_out[l].shape, _BF16, self.device)
+                k = vc_rows(pc.k_out[l].data_ptr(), 0, 0, self.d, 0)
+                v = vc_rows(pc.v_out[l].data_ptr(), 0, 0, self.d, 0)
+                viscache_q8_append(one, c, k, v, most[l], count[l].data_ptr(), off[l].data_ptr(), stream)
+
+    def read(self, k, v, max_rows=None, head_major: bool = False) -> None:
+        """Reads rows [0, len) of every unit back into k, v (bf16 or fp32)
+        [L, B, rows, Hkv, d] ([L, B, Hkv, rows, d] with head_major); rows behind
+        them are left as they were.  max_rows: by default, as many as k holds."""
+        rows = k.shape[3 if head_major else 2]
+        want = (self.L, self.B, self.Hkv, rows, self.d) if head_major else (self.L, self.B, rows, self.Hkv, self.d)
+        _expect(k, "k", want, _OUT, self.device)
+        _expect(v, "v", want, (k.dtype,), self.device)
+        m = rows if max_rows is None else int(max_rows)
+        if m > rows:
+            raise ValueError(f"max_rows {m} exceeds the {rows} rows of k")
+        if rows == 0:
+            return
+        with _On(self.device) as stream:
+            viscache_q8_read(self.shape, self.c, m, _rows(k, head_major), _rows(v, head_major), 0,
+                             int(k.dtype == torch.float32), stream)
+
+    def attend(self, q, out, scale: float, count=None, causal: bool = True, max_rows=None) -> None:
+        """Attention of q bf16 [L, B, n, Hq, d] over the cache into out (bf16 or
+        fp32, the same shape); count int32 [B]: the queries of each sequence."""
+        n = q.shape[2]
+        want = (self.L, self.B, n, self.Hq, self.d)
+        _expect(q, "q", want, _BF16, self.device)
+        _expect(out, "out", want, _OUT, self.device)
+        cnt = _expect_ints(count, "count", (self.B,), self.device)
+        if n == 0:
+            return
+        rows = self.max_cap if max_rows is None else int(max_rows)
+        with _On(self.device) as stream:
+            ws = self._workspace(n, rows)
+            viscache_q8_attend(self.shape, self.c, _rows(q), _rows(out), n, cnt, int(causal),
+                               int(out.dtype == torch.float32), scale, rows, ws.data_ptr(), ws.numel(), stream)
+
+    def step(self, q, k, v, out, scale: float, rope: Rope | None = None, pos=None, q_out=None, k_out=None) -> None:
+        """A serving step: rotates q and k by pos (with `rope`; into q_out and
+        k_out, by default in place), appends k and v and attends q."""
+        if rope is not None:
+            q, k = rope.apply(pos, q, k, q_out=q_out, k_out=k_out)
+        self.append(k, v)
+        self.attend(q, out, scale)
+
+
+__all__ = ["PruneCall", "DecodeCache", "Q8Cache", "Rope", "make_params"]
