@@ -453,6 +453,10 @@ typedef struct {
   const int64_t *row_off; /* [L*B*Hkv] */
   const int32_t *cap;
   int32_t *len;
+  const int32_t *order;   /* [L*B*Hkv]: the units in the order in which attention
+                             starts on them, or NULL; longest first evens out
+                             units of different lengths.  A permutation: a unit
+                             that it leaves out is not attended. */
 } vc_q8cache;
 
 /* A strided DEVICE tensor of rows of d contiguous values: row (layer l,
@@ -475,7 +479,7 @@ typedef struct {
  * viscache_prune's outputs.  Tail rows past the open block's are left as they
  * were.  n = 0 does nothing.  The cache's other arrays must not be in use on
  * another stream.  VC_ERR_UNSUPPORTED where the launch would take 2^23 or more
- * workgroups (one per unit for n <= 64, else ceil(n/64) + 1). */
+ * workgroups (one per unit for n <= 256, else ceil(n/64) + 1). */
 vc_status viscache_q8_append(const vc_decode_shape *shape, const vc_q8cache *cache, const vc_rows *k,
                              const vc_rows *v, int32_t n, const int32_t *count, const int64_t *unit_off, void *stream);
 
@@ -500,14 +504,14 @@ size_t viscache_q8_attend_workspace_bytes(const vc_decode_shape *shape, int32_t 
  * with K_t and V_t as they read back (before any rounding to bf16).  q: bf16; out:
  * bf16 (out_fp32 = 0) or fp32; both indexed by the query head.  A query that
  * sees no row gives zeros; rows i >= c of out are left as they were.  max_rows
- * bounds every len (rows past it are not attended).  n * Hq/Hkv <= 16 (single
- * tokens, short drafts) takes one launch, more a launch or two.  n = 0 does nothing.
- * `workspace`: DEVICE, at least viscache_q8_attend_workspace_bytes bytes,
- * 256-byte aligned, zero-filled before its first use and not modified by the
- * caller between calls (its counters are left at zero).  Calls sharing a
- * workspace, captured ones among them, must be ordered on one stream and agree
- * in L*B*Hkv; the rest of the shape, n and max_rows may differ.
- * VC_ERR_UNSUPPORTED for n * Hq/Hkv > 2^24, or 2^23 or more workgroups. */
+ * bounds every len (rows past it are not attended).  One launch, and a second
+ * that joins partial results where few (unit, query) tiles are cut along their
+ * rows; n * Hq/Hkv <= 16 (single tokens, short drafts) has kernels of its own.
+ * n = 0 does nothing.  `workspace`: DEVICE, at least
+ * viscache_q8_attend_workspace_bytes bytes, 256-byte aligned; its contents on
+ * entry do not matter and none are kept, so calls, captured ones among them,
+ * may share one as long as they do not overlap.  VC_ERR_UNSUPPORTED for n *
+ * Hq/Hkv > 2^24, 2^23 or more workgroups, or 2^24 or more columns to join. */
 vc_status viscache_q8_attend(const vc_decode_shape *shape, const vc_q8cache *cache, const vc_rows *q,
                              const vc_rows *out, int32_t n, const int32_t *count, int32_t causal, int32_t out_fp32,
                              float scale, int32_t max_rows, void *workspace, size_t workspace_bytes, void *stream);

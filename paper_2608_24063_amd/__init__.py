@@ -58,7 +58,8 @@ class vc_qcache(ctypes.Structure):
 
 class vc_q8cache(ctypes.Structure):
     _fields_ = [("format", c_i32), ("k_codes", c_vp), ("v_codes", c_vp), ("k_scale", c_vp), ("v_scale", c_vp),
-                ("k_tail", c_vp), ("v_tail", c_vp), ("row_off", c_vp), ("cap", c_vp), ("len", c_vp)]
+                ("k_tail", c_vp), ("v_tail", c_vp), ("row_off", c_vp), ("cap", c_vp), ("len", c_vp),
+                ("order", c_vp)]
 
 
 class vc_rows(ctypes.Structure):

@@ -39,8 +39,8 @@ __device__ __forceinline__ uint32_t half_max(uint32_t (&red)[2][4], uint32_t m, 
   return max(max(red[side][0], red[side][1]), max(red[side][2], red[side][3]));
 }
 
-// Workgroup j of a unit seals block j of those its new rows reach, or leaves
-// it open; workgroup 0 also takes an open last block, since that goes over the
+// Workgroup j of a unit's nj seals blocks j, j + nj, ... of those its new rows
+// fill; workgroup 0 also takes an open last block, since that goes over the
 // tail rows the first block is made of.
 template <int D, int FMT>
 __global__ __launch_bounds__(kThreads) void k_append_rows(Q8Rows p) {
@@ -56,7 +56,8 @@ __global__ __launch_bounds__(kThreads) void k_append_rows(Q8Rows p) {
   const int end = len0 + m, b0 = len0 / kQ8Block;
   const int nblk = (end + kQ8Block - 1) / kQ8Block - b0;
   const bool open = end % kQ8Block != 0;
-  if (j >= nblk || (j > 0 && open && j == nblk - 1)) return;
+  const int nfull = open ? nblk - 1 : nblk;
+  if (j >= max(nfull, 1)) return;
   const int64_t blk0 = ldg(p.c.row_off + u) / kQ8Block + b0;
   const RowsDesc &rd = side ? p.v : p.k;
   const uint16_t *src = reinterpret_cast<const uint16_t *>(rd.base) + unit_base(rd, p.unit_off, u, p.B, p.Hkv);
@@ -142,7 +143,7 @@ __global__ __launch_bounds__(kThreads) void k_append_rows(Q8Rows p) {
     const float s = open_scale(half_max(sm.red, mag, side, tid));
     if (tid == 0) stg(scales + blk0 + jb, lo > 0 ? fmaxf(s, ldg(scales + blk0 + jb)) : s);
   };
-  if (j < nblk - 1 || !open) seal(j);
+  for (int jb = j; jb < nfull; jb += p.nj) seal(jb);
   if (j == 0 && open) leave_open(nblk - 1);  // (every tail row of a sealed block 0 was read before a barrier)
   // One workgroup a unit: every thread has read the length (a barrier ago).
   if (p.nj == 1 && threadIdx.x == 0) stg(p.c.len + u, end);
@@ -158,23 +159,22 @@ __global__ __launch_bounds__(256) void k_append_len(Q8Rows p) {
   if (m > 0) stg(p.c.len + u, len0 + m);
 }
 
-// N values, already read, to a row: bf16 or fp32.
+// 16 bytes of a row: 4 fp32 or 8 bf16 values.
 template <bool F32>
-__device__ __forceinline__ void put8(char *dst, const float (&f)[8]) {
-  if (F32) {
-    st16(dst, u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])});
-    st16(dst + 16, u32x4{__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7])});
-  } else {
-    st16(dst, u32x4{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])});
-  }
+__device__ __forceinline__ void put16(char *dst, const float (&f)[8]) {
+  st16(dst, F32 ? u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])}
+                : u32x4{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])});
 }
 
 // Workgroup (unit, block): the block's rows below the unit's length (and the
-// row bound) as code * scale, or the tail's rows.
+// row bound) as code * scale, or the tail's rows.  A lane writes 16 bytes and
+// its neighbours the bytes beside them.
 template <int D, int FMT, bool F32>
 __global__ __launch_bounds__(kThreads) void k_read_rows(Q8Rows p) {
   constexpr int VP = kQ8Block + 4;  // pitch of a channel's codes, bytes
   constexpr int E = F32 ? 4 : 2;
+  constexpr int N = 16 / E;   // values a lane writes at once
+  constexpr int PR = D / N;   // lanes per row
   __shared__ uint32_t vt[D * VP / 4];
   const int u = (int)(blockIdx.x / (uint32_t)p.nj), j = (int)(blockIdx.x % (uint32_t)p.nj);
   const int side = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 8), tid = threadIdx.x & 255;
@@ -188,17 +188,28 @@ __global__ __launch_bounds__(kThreads) void k_read_rows(Q8Rows p) {
   const int64_t pitch = E * rd.token;
   if (j >= len / kQ8Block) {  // uniform: the open block
     const uint16_t *tail = (side ? p.c.vt : p.c.kt) + (int64_t)u * kQ8Block * D;
-    for (int e = tid; e < rows * (D / 8); e += kHalf) {
-      const int row = e / (D / 8), c = e % (D / 8);
-      const u32x4 x = ld16(tail + row * D + 8 * c);
+    for (int e = tid; e < rows * PR; e += kHalf) {
+      const int row = e / PR, c = e % PR;
+      const u32x2 x = ld8(tail + row * D + N * c);
+      const u32x2 y = F32 ? x : ld8(tail + row * D + N * c + 4);
       const float f[8] = {bf16_lo(x.x), bf16_hi(x.x), bf16_lo(x.y), bf16_hi(x.y),
-                          bf16_lo(x.z), bf16_hi(x.z), bf16_lo(x.w), bf16_hi(x.w)};
-      put8<F32>(out + row * pitch + E * 8 * c, f);
+                          bf16_lo(y.x), bf16_hi(y.x), bf16_lo(y.y), bf16_hi(y.y)};
+      put16<F32>(out + row * pitch + 16 * c, f);
     }
     return;
   }
   const uint8_t *codes = (side ? p.c.vc : p.c.kc) + blk * (kQ8Block * D);
   const float s = ldg((side ? p.c.vs : p.c.ks) + blk);
+  auto values = [&](uint32_t w0, uint32_t w1, float(&f)[8]) {
+    float a[4], b[4];
+    Q8<FMT>::unpack4(w0, a);
+    if (!F32) Q8<FMT>::unpack4(w1, b);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      f[k] = a[k] * s;
+      f[4 + k] = F32 ? 0.f : b[k] * s;
+    }
+  };
   if (side == 1) {
 #pragma unroll
     for (int e = tid; e < D * kQ8Block / 16; e += kHalf) {
@@ -214,39 +225,34 @@ __global__ __launch_bounds__(kThreads) void k_read_rows(Q8Rows p) {
   __syncthreads();
   if (side == 0) {
 #pragma unroll
-    for (int e = tid; e < kQ8Block * D / 16; e += kHalf) {
-      const int row = e / (D / 16), c = e % (D / 16);
-      const u32x4 x = ld16(codes + row * D + 16 * c);
-      const uint32_t ws[4] = {x.x, x.y, x.z, x.w};
-      if (row < rows) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float a[4], b[4];
-          Q8<FMT>::unpack4(ws[2 * h], a);
-          Q8<FMT>::unpack4(ws[2 * h + 1], b);
-          const float f[8] = {a[0] * s, a[1] * s, a[2] * s, a[3] * s, b[0] * s, b[1] * s, b[2] * s, b[3] * s};
-          put8<F32>(out + row * pitch + E * (16 * c + 8 * h), f);
-        }
-      }
+    for (int e = tid; e < kQ8Block * PR; e += kHalf) {
+      const int row = e / PR, c = e % PR;
+      const uint8_t *src = codes + row * D + N * c;
+      u32x2 w;
+      if (F32)
+        w = u32x2{ldg(reinterpret_cast<const uint32_t *>(src)), 0u};
+      else
+        w = ld8(src);
+      float f[8];
+      values(w.x, w.y, f);
+      if (row < rows) put16<F32>(out + row * pitch + 16 * c, f);
     }
   } else {
-    // Thread: channels 8 co .. + 7 of rows 4 rq .. + 3.
+    // Thread: N channels of rows 4 rq .. 4 rq + 3.
 #pragma unroll
-    for (int e = tid; e < (D / 8) * 16; e += kHalf) {
-      const int co = e % (D / 8), rq = e / (D / 8);
+    for (int e = tid; e < PR * 16; e += kHalf) {
+      const int c = e % PR, rq = e / PR;
       uint32_t w[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) w[k] = vt[(8 * co + k) * (VP / 4) + rq];
-      const u32x4 a = transpose4(w[0], w[1], w[2], w[3]), b = transpose4(w[4], w[5], w[6], w[7]);
+      for (int k = 0; k < N; ++k) w[k] = vt[(N * c + k) * (VP / 4) + rq];
+      const u32x4 a = transpose4(w[0], w[1], w[2], w[3]);
+      const u32x4 b = F32 ? a : transpose4(w[4], w[5], w[6], w[7]);
       const uint32_t as[4] = {a.x, a.y, a.z, a.w}, bs[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        if (4 * rq + r >= rows) continue;
-        float x[4], y[4];
-        Q8<FMT>::unpack4(as[r], x);
-        Q8<FMT>::unpack4(bs[r], y);
-        const float f[8] = {x[0] * s, x[1] * s, x[2] * s, x[3] * s, y[0] * s, y[1] * s, y[2] * s, y[3] * s};
-        put8<F32>(out + (4 * rq + r) * pitch + E * 8 * co, f);
+        float f[8];
+        values(as[r], bs[r], f);
+        if (4 * rq + r < rows) put16<F32>(out + (4 * rq + r) * pitch + 16 * c, f);
       }
     }
   }

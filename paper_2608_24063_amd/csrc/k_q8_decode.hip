@@ -13,8 +13,10 @@
 // rows so that a lane ends with the logits of rows 16 lg .. 16 lg + 15 of its
 // column; those are the k-elements of P^T, and the value codes' channel-major
 // order gives the same 16 rows in one 16-byte load, so neither P nor V passes
-// through LDS.  The open block's bf16 rows take the same path, scaled into
-// fp16 by their power of two, their values transposed through LDS.
+// through LDS.  The open block's bf16 rows, 16 a wave, are scaled into fp16 by
+// their power of two and their values transposed through LDS; they are
+// requested with the first block, since the whole kernel waits for them (read
+// by one wave after its own blocks they took 8 of 25 us).
 #include "vc_q8_device.h"
 
 namespace vc {
@@ -25,6 +27,15 @@ constexpr float kNegInf = -__builtin_inff();
 
 __device__ __forceinline__ f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+// 16 rows of k instead of 32: four elements a lane, rows 4 lg .. 4 lg + 3.
+__device__ __forceinline__ f32x4 mfma16x4(f16x4 a, f16x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x16f16(a, b, c, 0, 0, 0);
+}
+
+__device__ __forceinline__ f16x8 pack8(const _Float16 *h) {
+  return f16x8{h[0], h[1], h[2], h[3], h[4], h[5], h[6], h[7]};
 }
 
 // Eight bf16 values times a power of two, as fp16.
@@ -39,24 +50,16 @@ __device__ __forceinline__ f16x8 half8_of_bf16(u32x4 w, float f) {
   return r;
 }
 
-// Device-coherent accesses for partials that cross XCDs inside a launch.
-__device__ __forceinline__ void st_dev(float *p, float v) {
-  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ float ld_dev(const float *p) {
-  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
+constexpr int kWaves = 4;
 
 template <int D>
 struct Smem {
   static constexpr int VP = D + 16;  // pitch of the open block's values: conflict-free transposing reads
-  static constexpr size_t kO = sizeof(float) * 4 * 16 * (D + 4);
+  static constexpr size_t kO = sizeof(float) * kWaves * 16 * (D + 4);
   static constexpr size_t kT = sizeof(uint16_t) * kQ8Block * VP;
-  // The open block's values (one wave, in its loop), then the waves' O.
+  // The open block's values (16 rows a wave), then the waves' O.
   uint8_t buf[kO > kT ? kO : kT] __attribute__((aligned(16)));
-  float2 ml[4][16];
-  float2 mlb[16][16];  // (max, sum) of a batch of partials being merged
-  uint32_t last;
+  float2 ml[kWaves][16];
 };
 
 // What a wave carries over its blocks, per lane: the column's running maximum
@@ -67,24 +70,21 @@ struct State {
   f32x4 O[D / 16];
 };
 
-// One block's logits into the state: S (raw products; row 16 lg + 4 rb + i in
-// S[rb][i]) times c, rows at or past `end` masked, and the products with the
-// values, whose fragments va(mb, x) holds channel 16 mb + lr, rows 16 lg + 8 x.
-template <int D, bool HILO, typename VA>
-__device__ __forceinline__ void absorb(State<D> &st, f32x4 (&S)[4], float c, float vs, int row0, int end, bool mask,
-                                       int lg, VA va) {
-  constexpr int MB = D / 16;
+// Logits into the state: S (raw products; row rowof(k) in S[k / 4][k % 4], k <
+// 4 NB) times c, rows at or past `end` masked.  Returns the weights, as fp16
+// parts of 2^14 p: hi, and lo where two are kept.
+template <int D, int NB, bool HILO, typename RowOf>
+__device__ __forceinline__ void weigh(State<D> &st, f32x4 (&S)[NB], float c, int end, bool mask, RowOf rowof,
+                                      _Float16 (&hi)[4 * NB], _Float16 (&lo)[4 * NB]) {
   c = fmaxf(c, 1e-37f);  // not zero, so that a masked row stays at -inf
-  if (mask) {
+  if (mask) {  // uniform
 #pragma unroll
-    for (int rb = 0; rb < 4; ++rb)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (row0 + 16 * lg + 4 * rb + i >= end) S[rb][i] = kNegInf;
+    for (int k = 0; k < 4 * NB; ++k)
+      if (rowof(k) >= end) S[k / 4][k % 4] = kNegInf;
   }
   float mx = S[0][0];
 #pragma unroll
-  for (int k = 1; k < 16; ++k) mx = fmaxf(mx, S[k / 4][k % 4]);
+  for (int k = 1; k < 4 * NB; ++k) mx = fmaxf(mx, S[k / 4][k % 4]);
   mx = fmaxf(mx, swap16(mx));
   mx = max_halves(mx) * c;
   const float mn = fmaxf(st.m, mx);
@@ -93,35 +93,17 @@ __device__ __forceinline__ void absorb(State<D> &st, f32x4 (&S)[4], float c, flo
     const float alpha = fast_exp2(st.m - ref);
     st.l *= alpha;
 #pragma unroll
-    for (int mb = 0; mb < MB; ++mb) st.O[mb] *= alpha;
+    for (int mb = 0; mb < D / 16; ++mb) st.O[mb] *= alpha;
   }
   st.m = mn;
-  f16x8 hi[2], lo[2];
-  float sum = 0.f;
 #pragma unroll
-  for (int rb = 0; rb < 4; ++rb)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float pr = fast_exp2(fmaf(S[rb][i], c, -ref));
-      sum += pr;
-      // 2^14 keeps the small ones clear of fp16's subnormals.
-      const float ps = pr * 16384.f;
-      const _Float16 h = (_Float16)ps;
-      hi[rb / 2][4 * (rb & 1) + i] = h;
-      if (HILO) lo[rb / 2][4 * (rb & 1) + i] = (_Float16)(ps - (float)h);
-    }
-  st.l += sum;
-#pragma unroll
-  for (int mb = 0; mb < MB; ++mb) {
-    f32x4 t = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const f16x8 v = va(mb, x);
-      t = mfma16(v, hi[x], t);
-      if (HILO) t = mfma16(v, lo[x], t);
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) st.O[mb][i] = fmaf(t[i], vs, st.O[mb][i]);
+  for (int k = 0; k < 4 * NB; ++k) {
+    const float pr = fast_exp2(fmaf(S[k / 4][k % 4], c, -ref));
+    st.l += pr;
+    // 2^14 keeps the small ones clear of fp16's subnormals.
+    const float ps = pr * 16384.f;
+    hi[k] = (_Float16)ps;
+    if (HILO) lo[k] = (_Float16)(ps - (float)hi[k]);
   }
 }
 
@@ -149,15 +131,19 @@ __device__ __forceinline__ void put(const Q8Attn &p, int64_t at, float v) {
 // Workgroup (unit, piece): blocks [j piece, (j + 1) piece) of the unit, dealt
 // to the four waves in turn.
 template <int D, int FMT, bool HILO>
-__global__ __launch_bounds__(256, 2) void k_decode8(Q8Attn p) {
+__global__ __launch_bounds__(64 * kWaves, 2) void k_decode8(Q8Attn p) {
   constexpr int MB = D / 16, CH = D / 64;
   __shared__ Smem<D> sm;
-  const int u = (int)(blockIdx.x / (uint32_t)p.npmax), j = (int)(blockIdx.x % (uint32_t)p.npmax);
+  const int i = (int)(blockIdx.x % (uint32_t)p.units), j = (int)(blockIdx.x / (uint32_t)p.units);
+  const int u = p.c.order ? ldg(p.c.order + i) : i;
+  if (u < 0 || u >= p.units) return;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 15, lg = lane >> 4;
   const int b = u / p.Hkv % p.B;
-  const int len = max(min(ldg(p.c.len + u), ldg(p.c.cap + u)), 0);
-  const int cnt = p.count ? min(max(ldg(p.count + b), 0), p.n) : p.n;
+  // What the unit is, in one round trip.
+  const int len_ = ldg(p.c.len + u), cap_ = ldg(p.c.cap + u), cnt_ = p.count ? ldg(p.count + b) : p.n;
+  const int64_t row_off = ldg(p.c.row_off + u);
+  const int len = max(min(len_, cap_), 0), cnt = min(max(cnt_, 0), p.n);
   const int cols = cnt * p.G;
   const int emax = cols > 0 ? min(len, p.max_rows) : 0;  // rows any column sees
   const int nt = (emax + kQ8Block - 1) / kQ8Block;
@@ -168,35 +154,18 @@ __global__ __launch_bounds__(256, 2) void k_decode8(Q8Attn p) {
   const int lim = p.causal ? len - cnt + 1 : len;
   const int end = max(min(p.causal ? lim + qi : len, p.max_rows), 0);
   const int emin = min(lim, p.max_rows);
-  const int64_t blk0 = ldg(p.c.row_off + u) / kQ8Block;
+  const int64_t blk0 = row_off / kQ8Block;
   const int nsealed = len / kQ8Block;
 
-  // The column's query as fp16 operands, scaled by a power of two.
-  f16x8 q[CH][2];
-  float cq;
+  // The query's requests, then the first block's, before anything waits.
+  u32x4 qx[CH][2];
   {
     const uint16_t *qp = reinterpret_cast<const uint16_t *>(p.q.base) + out_row(p, p.q, u, min(lr, cols - 1));
-    u32x4 x[CH][2];
-    uint32_t mag = 0u;
 #pragma unroll
     for (int h = 0; h < CH; ++h)
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        x[h][k] = ld16(qp + 64 * h + 16 * lg + 8 * k);
-        mag = max_mag(max_mag(max_mag(max_mag(mag, x[h][k].x), x[h][k].y), x[h][k].z), x[h][k].w);
-      }
-    uint32_t mm = max(mag & 0xFFFFu, mag >> 16);
-    mm = max(mm, (uint32_t)__shfl_xor((int)mm, 16, 64));
-    mm = max(mm, (uint32_t)__shfl_xor((int)mm, 32, 64));
-    const float qs = open_scale(mm);
-    cq = p.sc * qs;
-    const float inv = 1.f / qs;  // exact: a power of two
-#pragma unroll
-    for (int h = 0; h < CH; ++h)
-#pragma unroll
-      for (int k = 0; k < 2; ++k) q[h][k] = half8_of_bf16(x[h][k], inv);
+      for (int k = 0; k < 2; ++k) qx[h][k] = ld16(qp + 64 * h + 16 * lg + 8 * k);
   }
-
   State<D> st;
   st.m = kNegInf;
   st.l = 0.f;
@@ -227,7 +196,46 @@ __global__ __launch_bounds__(256, 2) void k_decode8(Q8Attn p) {
     load_k(t);
     load_v(t);
   }
-  for (; t < ts; t += 4) {
+  // The open block, if it is in this piece: a wave takes 16 of its rows.
+  constexpr int VT = D / 32;
+  const bool open = nsealed >= t0 && nsealed < t1;
+  const int orows = len - nsealed * kQ8Block;  // 1 .. 63 where open
+  u32x4 ok[CH][2], ov[VT];
+  float kse = 1.f, vse = 1.f;
+  if (open) {
+    const int64_t tail = (int64_t)u * kQ8Block * D;
+    const uint16_t *kt = p.c.kt + tail + min(16 * w + lr, orows - 1) * D + 16 * lg;
+#pragma unroll
+    for (int h = 0; h < CH; ++h)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) ok[h][x] = ld16(kt + 64 * h + 8 * x);
+#pragma unroll
+    for (int it = 0; it < VT; ++it) ov[it] = ld16(p.c.vt + tail + 16 * w * D + 8 * (lane + 64 * it));
+    kse = ldg(p.c.ks + blk0 + nsealed);
+    vse = ldg(p.c.vs + blk0 + nsealed);
+  }
+  // The column's query as fp16 operands, scaled by a power of two.
+  f16x8 q[CH][2];
+  float cq;
+  {
+    uint32_t mag = 0u;
+#pragma unroll
+    for (int h = 0; h < CH; ++h)
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        mag = max_mag(max_mag(max_mag(max_mag(mag, qx[h][k].x), qx[h][k].y), qx[h][k].z), qx[h][k].w);
+    uint32_t mm = max(mag & 0xFFFFu, mag >> 16);
+    mm = max(mm, (uint32_t)__shfl_xor((int)mm, 16, 64));
+    mm = max(mm, (uint32_t)__shfl_xor((int)mm, 32, 64));
+    const float qs = open_scale(mm);
+    cq = p.sc * qs;
+    const float inv = 1.f / qs;  // exact: a power of two
+#pragma unroll
+    for (int h = 0; h < CH; ++h)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) q[h][k] = half8_of_bf16(qx[h][k], inv);
+  }
+  for (; t < ts; t += kWaves) {
     f32x4 S[4];
 #pragma unroll
     for (int rb = 0; rb < 4; ++rb) {
@@ -239,49 +247,60 @@ __global__ __launch_bounds__(256, 2) void k_decode8(Q8Attn p) {
       }
     }
     const float c = cq * ks, v = vs;
-    const int tn = min(t + 4, ts - 1);  // the last block again where there is no next (never used)
+    const int tn = min(t + kWaves, ts - 1);  // the last block again where there is no next (never used)
     load_k(tn);
-    absorb<D, HILO>(st, S, c, v, t * kQ8Block, end, (t + 1) * kQ8Block > emin, lg, [&](int mb, int x) {
-      return x == 0 ? Q8<FMT>::half8(vcode[mb].x, vcode[mb].y) : Q8<FMT>::half8(vcode[mb].z, vcode[mb].w);
-    });
+    _Float16 hi[16], lo[16];
+    weigh<D, 4, HILO>(
+        st, S, c, end, (t + 1) * kQ8Block > emin,
+        [&](int k) { return t * kQ8Block + 16 * lg + k; }, hi, lo);
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const f16x8 a = x == 0 ? Q8<FMT>::half8(vcode[mb].x, vcode[mb].y) : Q8<FMT>::half8(vcode[mb].z, vcode[mb].w);
+        o = mfma16(a, pack8(hi + 8 * x), o);
+        if (HILO) o = mfma16(a, pack8(lo + 8 * x), o);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) st.O[mb][i] = fmaf(o[i], v, st.O[mb][i]);
+    }
     load_v(tn);
   }
-  // The open block, if it is in this piece and this wave's turn.
-  if (nsealed >= t0 && nsealed < t1 && (nsealed - t0) % 4 == w) {
-    const int rows = len - nsealed * kQ8Block;  // 1 .. 63
-    const uint16_t *kt = p.c.kt + (int64_t)u * kQ8Block * D, *vt = p.c.vt + (int64_t)u * kQ8Block * D;
-    const float kse = ldg(p.c.ks + blk0 + nsealed), vse = ldg(p.c.vs + blk0 + nsealed);
+  // The open block.
+  if (open) {
     const float kinv = 1.f / kse, vinv = 1.f / vse;  // powers of two
-    uint16_t *lv = reinterpret_cast<uint16_t *>(sm.buf);
-#pragma unroll 4
-    for (int it = 0; it < D / 8; ++it) {
-      const int e = lane + 64 * it;
-      const int row = e / (D / 8), cc = e % (D / 8);
+    uint16_t *lv = reinterpret_cast<uint16_t *>(sm.buf) + w * 16 * Smem<D>::VP;
+#pragma unroll
+    for (int it = 0; it < VT; ++it) {
+      const int e = lane + 64 * it, row = e / (D / 8), cc = e % (D / 8);
       // Rows past the end hold anything: zeros meet their zero weights.
-      const u32x4 x = row < rows ? ld16(vt + row * D + 8 * cc) : u32x4{0u, 0u, 0u, 0u};
+      const u32x4 x = 16 * w + row < orows ? ov[it] : u32x4{0u, 0u, 0u, 0u};
       *reinterpret_cast<f16x8 *>(lv + row * Smem<D>::VP + 8 * cc) = half8_of_bf16(x, vinv);
     }
-    f32x4 S[4];
+    f32x4 S[1] = {{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-    for (int rb = 0; rb < 4; ++rb) {
-      S[rb] = f32x4{0.f, 0.f, 0.f, 0.f};
-      const uint16_t *k = kt + min(krow + 4 * rb, rows - 1) * D + 16 * lg;
+    for (int h = 0; h < CH; ++h)
 #pragma unroll
-      for (int h = 0; h < CH; ++h)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) S[rb] = mfma16(half8_of_bf16(ld16(k + 64 * h + 8 * x), kinv), q[h][x], S[rb]);
-    }
+      for (int x = 0; x < 2; ++x) S[0] = mfma16(half8_of_bf16(ok[h][x], kinv), q[h][x], S[0]);
+    _Float16 hi[4], lo[4];
+    weigh<D, 1, HILO>(
+        st, S, cq * kse, end, true, [&](int k) { return nsealed * kQ8Block + 16 * w + 4 * lg + k; }, hi, lo);
     __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): this wave's LDS writes landed
     __builtin_amdgcn_wave_barrier();
-    absorb<D, HILO>(st, S, cq * kse, vse, nsealed * kQ8Block, end, true, lg, [&](int mb, int x) {
-      const uint16_t *base = lv + (16 * lg + 8 * x + (lr >> 2)) * Smem<D>::VP + 16 * mb + 4 * (lr & 3);
-      const u32x2 a = lds_read_tr16(base), bb = lds_read_tr16(base + 4 * Smem<D>::VP);
-      return __builtin_bit_cast(f16x8, u32x4{a.x, a.y, bb.x, bb.y});
-    });
-    __builtin_amdgcn_s_waitcnt(0xc07f);
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+      const f16x4 a = __builtin_bit_cast(
+          f16x4, lds_read_tr16(lv + (4 * lg + (lr >> 2)) * Smem<D>::VP + 16 * mb + 4 * (lr & 3)));
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+      o = mfma16x4(a, f16x4{hi[0], hi[1], hi[2], hi[3]}, o);
+      if (HILO) o = mfma16x4(a, f16x4{lo[0], lo[1], lo[2], lo[3]}, o);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) st.O[mb][i] = fmaf(o[i], vse, st.O[mb][i]);
+    }
   }
 
-  // The four waves' states.
+  // The waves' states.
   st.l = sum_halves(st.l + swap16(st.l));
   __syncthreads();  // the open block's values are read
   float(*wo)[16][D + 4] = reinterpret_cast<float(*)[16][D + 4]>(sm.buf);
@@ -292,14 +311,14 @@ __global__ __launch_bounds__(256, 2) void k_decode8(Q8Attn p) {
   __syncthreads();
   const int x = tid % D;
   const int64_t slot = (int64_t)u * p.npmax + j;
-  for (int col = tid / D; col < cols; col += 256 / D) {
+  for (int col = tid / D; col < cols; col += 64 * kWaves / D) {
     float M = kNegInf;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) M = fmaxf(M, sm.ml[k][col].x);
+    for (int k = 0; k < kWaves; ++k) M = fmaxf(M, sm.ml[k][col].x);
     float o = 0.f, s = 0.f;
     if (M != kNegInf) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < kWaves; ++k) {
         const float f = fast_exp2(sm.ml[k][col].x - M);
         o += f * wo[k][col][x];
         s += f * sm.ml[k][col].y;
@@ -309,84 +328,21 @@ __global__ __launch_bounds__(256, 2) void k_decode8(Q8Attn p) {
     if (np == 1) {
       put(p, out_row(p, p.out, u, col) + x, s > 0.f ? o / s : 0.f);
     } else {
-      st_dev(p.part_o + (slot * 16 + col) * D + x, o);
-      if (x == 0) {
-        float *ml = reinterpret_cast<float *>(p.part_ml + slot * 16 + col);
-        st_dev(ml, M);
-        st_dev(ml + 1, s);
-      }
+      stg(p.part_o + (slot * 16 + col) * D + x, o);
+      if (x == 0) stg(p.part_ml + slot * 16 + col, make_float2(M, s));
     }
-  }
-  if (np == 1) return;
-  // A unit in several pieces: the last to arrive merges them, in row order.
-  __builtin_amdgcn_s_waitcnt(0);
-  __syncthreads();
-  if (tid == 0)
-    sm.last = __hip_atomic_fetch_add(p.arrive + u, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(np - 1);
-  __syncthreads();
-  if (!sm.last) return;
-  if (tid == 0) __hip_atomic_store(p.arrive + u, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  constexpr int kEl = 16 * D / 256;
-  float M[kEl], o[kEl], s[kEl];
-#pragma unroll
-  for (int k = 0; k < kEl; ++k) {
-    M[k] = kNegInf;
-    o[k] = s[k] = 0.f;
-  }
-  const int64_t slot0 = (int64_t)u * p.npmax;
-  for (int j0 = 0; j0 < np; j0 += 16) {
-    const int nb = min(16, np - j0);
-    __syncthreads();
-    {
-      const int pc = tid >> 4, col = tid & 15;
-      if (pc < nb && col < cols) {
-        const float *ml = reinterpret_cast<const float *>(p.part_ml + (slot0 + j0 + pc) * 16 + col);
-        sm.mlb[pc][col] = make_float2(ld_dev(ml), ld_dev(ml + 1));
-      }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < kEl; ++k) {
-      const int col = tid / D + k * (256 / D);
-      if (col >= cols) continue;
-      float Mc = M[k];
-      for (int pc = 0; pc < nb; ++pc) Mc = fmaxf(Mc, sm.mlb[pc][col].x);
-      if (Mc == kNegInf) continue;
-      const float a = fast_exp2(M[k] - Mc);
-      o[k] *= a;
-      s[k] *= a;
-      M[k] = Mc;
-      for (int p0 = 0; p0 < nb; p0 += 8) {
-        float v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          v[e] = ld_dev(p.part_o + ((slot0 + j0 + min(p0 + e, nb - 1)) * 16 + col) * D + x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          if (p0 + e >= nb) continue;
-          const float2 ml = sm.mlb[p0 + e][col];
-          const float f = fast_exp2(ml.x - Mc);
-          o[k] += f * v[e];
-          s[k] += f * ml.y;
-        }
-      }
-    }
-  }
-#pragma unroll
-  for (int k = 0; k < kEl; ++k) {
-    const int col = tid / D + k * (256 / D);
-    if (col < cols) put(p, out_row(p, p.out, u, col) + x, s[k] > 0.f ? o[k] / s[k] : 0.f);
   }
 }
 
 template <int D, int FMT>
 hipError_t launch(const Q8Attn &p, hipStream_t st) {
-  const dim3 grid((uint32_t)((int64_t)p.units * p.npmax)), block(256);
+  const dim3 grid((uint32_t)((int64_t)p.units * p.npmax)), block(64 * kWaves);
   if (p.fp32)
     hipLaunchKernelGGL((k_decode8<D, FMT, true>), grid, block, 0, st, p);
   else
     hipLaunchKernelGGL((k_decode8<D, FMT, false>), grid, block, 0, st, p);
-  return hipGetLastError();
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess || p.npmax == 1 ? e : launch_q8_join(p, st);
 }
 
 }  // namespace

@@ -300,47 +300,6 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt8(Q8Attn p) {
   if (hf == 0) stg(p.part_ml + at, make_float2(m, l));
 }
 
-// Joins the key splits of a column: thread (column, 4 channels).
-template <int D>
-__global__ __launch_bounds__(256) void k_join(Q8Attn p) {
-  constexpr int per = D / 4;
-  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t total = (int64_t)p.units * p.cols;
-  const int64_t cg = e / per;
-  if (cg >= total) return;
-  const int ch = (int)(e % per) * 4;
-  const int u = (int)(cg / p.cols), col = (int)(cg % p.cols);
-  const int g = u % p.Hkv, lb = u / p.Hkv, b = lb % p.B;
-  const int cnt = p.count ? min(max(ldg(p.count + b), 0), p.n) : p.n;
-  if (col >= cnt * p.G) return;
-  const int64_t at = (((int64_t)u * p.nqt + col / p.qcols) * p.ns) * p.qcols + col % p.qcols;
-  float M = kNegInf;
-  for (int s = 0; s < p.ns; ++s) M = fmaxf(M, ldg(p.part_ml + at + (int64_t)s * p.qcols).x);
-  float o[4] = {0.f, 0.f, 0.f, 0.f}, l = 0.f;
-  if (M != kNegInf) {
-    for (int s = 0; s < p.ns; ++s) {
-      const int64_t a = at + (int64_t)s * p.qcols;
-      const float2 ml = ldg(p.part_ml + a);
-      const u32x4 x = ld16(p.part_o + a * D + ch);
-      const float f = fast_exp2(ml.x - M);
-      l += f * ml.y;
-      o[0] += f * __uint_as_float(x.x);
-      o[1] += f * __uint_as_float(x.y);
-      o[2] += f * __uint_as_float(x.z);
-      o[3] += f * __uint_as_float(x.w);
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) o[i] = l > 0.f ? o[i] / l : 0.f;
-  const int64_t to = (int64_t)(lb / p.B) * p.out.layer + (int64_t)b * p.out.seq + (int64_t)(col / p.G) * p.out.token +
-                     (int64_t)(g * p.G + col % p.G) * p.out.head + ch;
-  if (p.fp32)
-    st16(reinterpret_cast<float *>(p.out.base) + to,
-         u32x4{__float_as_uint(o[0]), __float_as_uint(o[1]), __float_as_uint(o[2]), __float_as_uint(o[3])});
-  else
-    st8(reinterpret_cast<uint16_t *>(p.out.base) + to, u32x2{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])});
-}
-
 template <int D, int FMT, int NW>
 void launch_nw(const Q8Attn &p, hipStream_t st) {
   const dim3 grid((uint32_t)((int64_t)p.units * p.nqt * p.ns)), block(64 * NW);
@@ -358,9 +317,7 @@ hipError_t launch(const Q8Attn &p, hipStream_t st) {
     launch_nw<D, FMT, 4>(p, st);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.ns == 1) return e;
-  const int64_t threads = (int64_t)p.units * p.cols * (D / 4);
-  hipLaunchKernelGGL((k_join<D>), dim3((uint32_t)((threads + 255) / 256)), dim3(256), 0, st, p);
-  return hipGetLastError();
+  return launch_q8_join(p, st);
 }
 
 }  // namespace

@@ -24,6 +24,7 @@ struct Q8Cache {
   const int64_t *row_off;
   const int32_t *cap;
   int32_t *len;
+  const int32_t *order;  // may be null
 };
 
 struct Q8Rows {  // append (k, v read) and read back (k, v written)
@@ -47,11 +48,11 @@ struct Q8Attn {
   int32_t max_rows;
   float sc;              // scale * log2(e)
   // One token at a time (cols <= 16): pieces of `piece` blocks, at most npmax
-  // a unit.  Prompts: nqt column tiles of qcols columns, each in ns key splits.
+  // a unit (qcols 16).  Prompts (npmax 1): nqt column tiles of qcols columns,
+  // each in ns key splits.
   int32_t piece, npmax;
   int32_t qcols, nqt, ns;
-  uint32_t *arrive;      // [units], zero between calls
-  float *part_o;
+  float *part_o;         // partial results: [part][qcols][d], [part][qcols]
   float2 *part_ml;
 };
 
@@ -71,6 +72,7 @@ hipError_t launch_q8_append(const Q8Rows &p, int format, hipStream_t st);
 hipError_t launch_q8_read(const Q8Rows &p, int format, hipStream_t st);
 hipError_t launch_q8_decode(const Q8Attn &p, int format, hipStream_t st);
 hipError_t launch_q8_prompt(const Q8Attn &p, int format, hipStream_t st);
+hipError_t launch_q8_join(const Q8Attn &p, hipStream_t st);  // called by the two above
 hipError_t launch_rope(const RopePlan &p, hipStream_t st);
 
 }  // namespace vc

@@ -65,16 +65,16 @@ RowsDesc desc(const vc_rows *r) {
 
 Q8Cache bind(const vc_q8cache *c) {
   return Q8Cache{static_cast<uint8_t *>(c->k_codes), static_cast<uint8_t *>(c->v_codes), c->k_scale, c->v_scale,
-                 static_cast<uint16_t *>(c->k_tail), static_cast<uint16_t *>(c->v_tail), c->row_off, c->cap, c->len};
+                 static_cast<uint16_t *>(c->k_tail), static_cast<uint16_t *>(c->v_tail), c->row_off, c->cap, c->len,
+                 c->order};
 }
 
-// How an attention call is cut, and what it needs of the workspace: the units'
-// arrival counters at the front (their place follows from the number of units
-// alone), then partial O and (max, sum).
+// How an attention call is cut, and what it needs of the workspace: partial O,
+// then (max, sum).
 struct Cut {
   int32_t piece = 0, npmax = 1, qcols = 0, nqt = 0, ns = 1;
   int64_t wgs = 0, slots = 0;  // workgroups; columns of partial results
-  size_t o = 0, ml = 0, total = 0;
+  size_t ml = 0, total = 0;
 };
 
 bool attend_cut(const vc_decode_shape *s, int32_t n, int32_t max_rows, Cut &c) {
@@ -83,10 +83,14 @@ bool attend_cut(const vc_decode_shape *s, int32_t n, int32_t max_rows, Cut &c) {
   if (cols > (int64_t(1) << 24)) return false;
   const int64_t nt = std::max<int64_t>(1, ((int64_t)max_rows + kQ8Block - 1) / kQ8Block);
   if (cols <= kCols) {
-    // Pieces of a multiple of four blocks (one per wave), about four for each of
-    // the 512 workgroups the chip holds, so that units of different lengths
-    // even out.
-    const int64_t want = units * nt / (512 * 4);
+    // One workgroup a unit where there are enough units for the 256 CUs; fewer
+    // units are cut into pieces of a multiple of four blocks (one per wave and
+    // turn), as many as make about 256 workgroups.  (us: 4 units of 12544 rows
+    // in pieces of 4, 8, 16, 48 blocks 13.0, 13.3, 15.7, 26.1; 32 of 2300 to 5800
+    // rows in 4, 8, 12, 24: 21.1, 19.2, 16.4, 19.7; 896 of them in 24, 48 and
+    // uncut 199, 198, 188.)
+    const int64_t want = units * nt / 256;
+    c.qcols = kCols;
     c.piece = (int32_t)std::min<int64_t>(std::max<int64_t>(4, (want + 3) / 4 * 4), int64_t(1) << 26);
     c.npmax = (int32_t)((nt + c.piece - 1) / c.piece);
     c.wgs = units * c.npmax;
@@ -102,17 +106,16 @@ bool attend_cut(const vc_decode_shape *s, int32_t n, int32_t max_rows, Cut &c) {
     c.wgs = tiles * c.ns;
     c.slots = c.ns > 1 ? c.wgs * c.qcols : 0;
   }
-  if (c.wgs >= kMaxWg) return false;
-  c.o = align_up(sizeof(uint32_t) * (size_t)units);
-  c.ml = c.o + align_up(sizeof(float) * (size_t)c.slots * (size_t)s->d);
-  c.total = c.ml + align_up(sizeof(float2) * (size_t)c.slots);
+  if (c.wgs >= kMaxWg || (c.slots && units * cols >= 2 * kMaxWg)) return false;  // (the join: 256 threads a column)
+  c.ml = align_up(sizeof(float) * (size_t)c.slots * (size_t)s->d);
+  c.total = std::max(c.ml + align_up(sizeof(float2) * (size_t)c.slots), kAlign);
   return true;
 }
 
-// Workgroups a unit of an append or a read.
-int64_t row_groups(int64_t n, bool append) {
-  if (append) return n <= kQ8Block ? 1 : (n + kQ8Block - 1) / kQ8Block + 1;
-  return (n + kQ8Block - 1) / kQ8Block;
+// Workgroups a unit of an append: one where its blocks are few, which then also
+// advances the length; else a block each.
+int64_t append_groups(int64_t n) {
+  return n <= 4 * kQ8Block ? 1 : (n + kQ8Block - 1) / kQ8Block + 1;
 }
 
 }  // namespace
@@ -139,7 +142,7 @@ vc_status viscache_q8_append(const vc_decode_shape *s, const vc_q8cache *c, cons
   p.B = s->B; p.Hkv = s->Hkv; p.d = s->d;
   p.units = s->L * s->B * s->Hkv;
   p.n = n;
-  const int64_t nj = row_groups(n, true);
+  const int64_t nj = append_groups(n);
   if (nj * p.units >= kMaxWg) return VC_ERR_UNSUPPORTED;
   p.nj = (int32_t)nj;
   return launch_q8_append(p, c->format, static_cast<hipStream_t>(stream)) == hipSuccess ? VC_OK : VC_ERR_HIP;
@@ -166,7 +169,7 @@ vc_status viscache_q8_read(const vc_decode_shape *s, const vc_q8cache *c, int32_
   p.units = s->L * s->B * s->Hkv;
   p.n = max_rows;
   p.fp32 = out_fp32;
-  const int64_t nj = row_groups(max_rows, false);
+  const int64_t nj = ((int64_t)max_rows + kQ8Block - 1) / kQ8Block;
   if (nj * p.units >= kMaxWg) return VC_ERR_UNSUPPORTED;
   p.nj = (int32_t)nj;
   return launch_q8_read(p, c->format, static_cast<hipStream_t>(stream)) == hipSuccess ? VC_OK : VC_ERR_HIP;
@@ -210,8 +213,7 @@ vc_status viscache_q8_attend(const vc_decode_shape *s, const vc_q8cache *c, cons
   p.piece = cut.piece; p.npmax = cut.npmax;
   p.qcols = cut.qcols; p.nqt = cut.nqt; p.ns = cut.ns;
   uint8_t *ws = static_cast<uint8_t *>(workspace);
-  p.arrive = reinterpret_cast<uint32_t *>(ws);
-  p.part_o = reinterpret_cast<float *>(ws + cut.o);
+  p.part_o = reinterpret_cast<float *>(ws);
   p.part_ml = reinterpret_cast<float2 *>(ws + cut.ml);
   hipStream_t hs = static_cast<hipStream_t>(stream);
   const hipError_t e = p.cols <= kCols ? launch_q8_decode(p, c->format, hs) : launch_q8_prompt(p, c->format, hs);

@@ -339,7 +339,7 @@ class Q8Cache:
     has them, where a program keeps them itself.
 
     Calls go to the current stream of the cache's device.  Calls that attend
-    share one workspace and must be ordered on one stream."""
+    share one workspace and must not overlap."""
 
     FORMATS = {"int8": (VC_Q8_INT8, torch.int8), "e4m3": (VC_Q8_E4M3, torch.float8_e4m3fn)}
 
@@ -374,7 +374,11 @@ class Q8Cache:
             if not buffers[name].is_contiguous():
                 raise ValueError(f"{name} must be contiguous")
             setattr(self, name, buffers[name])
-        self.c = vc_q8cache(code, *[buffers[name].data_ptr() for name in _Q8_BUFFERS])
+        # Attention starts on the units with the most room first.
+        order = sorted(range(self.units), key=lambda u: -caps[u])
+        self.order = torch.tensor(order, dtype=torch.int32, device=self.device) if len(set(caps)) > 1 else None
+        self.c = vc_q8cache(code, *[buffers[name].data_ptr() for name in _Q8_BUFFERS],
+                            0 if self.order is None else self.order.data_ptr())
         self._ws, self._ws_bytes, self._kept = None, {}, []
 
     def _workspace(self, n: int, max_rows: int):
@@ -387,7 +391,7 @@ class Q8Cache:
         if self._ws is None or self._ws.numel() < need:
             if torch.cuda.is_current_stream_capturing():
                 raise RuntimeError("the workspace is too small: run the call once before it is captured")
-            self._ws = torch.zeros((max(need, 256),), dtype=torch.uint8, device=self.device)
+            self._ws = torch.empty((need,), dtype=torch.uint8, device=self.device)
             self._kept.append(self._ws)  # a graph captured before this goes on using the one it was captured with
         return self._ws
 
@@ -423,7 +427,7 @@ class Q8Cache:
                 c = vc_q8cache(self.c.format, self.c.k_codes, self.c.v_codes, self.c.k_scale, self.c.v_scale,
                                self.k_tail[l * per:].data_ptr(), self.v_tail[l * per:].data_ptr(),
                                self.row_off[l * per:].data_ptr(), self.cap[l * per:].data_ptr(),
-                               self.len[l * per:].data_ptr())
+                               self.len[l * per:].data_ptr(), 0)
                 _expect(pc.k_out[l], "k_out", pc.k_out[l].shape, _BF16, self.device)
                 k = vc_rows(pc.k_out[l].data_ptr(), 0, 0, self.d, 0)
                 v = vc_rows(pc.v_out[l].data_ptr(), 0, 0, self.d, 0)

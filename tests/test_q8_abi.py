@@ -27,7 +27,7 @@ def _shape(vc, B=2, L=3, Hq=8, Hkv=2, d=128):
 
 
 def _cache(vc, **kw):
-    c = vc.vc_q8cache(kw.pop("format", vc.VC_Q8_INT8), *[P16] * 9)
+    c = vc.vc_q8cache(kw.pop("format", vc.VC_Q8_INT8), *[P16] * 9, None)
     for k, v in kw.items():
         setattr(c, k, v)
     return c
@@ -135,11 +135,10 @@ def test_workspace(vc):
         assert need > 0
         assert _attend(vc, n=n, rows=5000, ws=0) == _attend(vc, n=n, rows=5000, ws=P16 + 16) == W
         assert _attend(vc, n=n, rows=5000, bytes_=need - 1) == W
-    # the counters come first, and the rest follows them: never less than a word a unit
     for d in (64, 128):
-        for n in (1, 2, 4, 33, 1000):
+        for n in (0, 1, 2, 4, 33, 1000):
             for rows in (0, 1, 64, 4096, 2 ** 31 - 1):
-                assert vc.viscache_q8_attend_workspace_bytes(_shape(vc, d=d), n, rows) >= 4 * 12
+                assert 256 <= vc.viscache_q8_attend_workspace_bytes(_shape(vc, d=d), n, rows) < 1 << 30
 
 
 def test_too_large(vc):
