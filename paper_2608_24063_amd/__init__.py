@@ -119,16 +119,14 @@ def lib() -> ctypes.CDLL:
                                                    ctypes.c_size_t, c_vp, c_vp, c_vp, c_vp, c_f32, c_i64, c_vp,
                                                    ctypes.c_size_t, c_vp]
         L.viscache_quantize_rows.argtypes = [c_i32, c_i64, c_vp, c_vp, c_vp, c_vp]
-        L.viscache_q8_append.argtypes = [P(vc_decode_shape), P(vc_q8cache), P(vc_rows), P(vc_rows), c_i32, c_vp,
-                                         c_vp, c_vp]
-        L.viscache_q8_read.argtypes = [P(vc_decode_shape), P(vc_q8cache), c_i32, P(vc_rows), P(vc_rows), c_vp,
-                                       c_i32, c_vp]
+        # Structures as plain addresses: tensors.py passes packed ones.
+        L.viscache_q8_append.argtypes = [c_vp, c_vp, c_vp, c_vp, c_i32, c_vp, c_vp, c_vp]
+        L.viscache_q8_read.argtypes = [c_vp, c_vp, c_i32, c_vp, c_vp, c_vp, c_i32, c_vp]
         L.viscache_q8_attend_workspace_bytes.argtypes = [P(vc_decode_shape), c_i32, c_i32]
         L.viscache_q8_attend_workspace_bytes.restype = ctypes.c_size_t
-        L.viscache_q8_attend.argtypes = [P(vc_decode_shape), P(vc_q8cache), P(vc_rows), P(vc_rows), c_i32, c_vp,
-                                         c_i32, c_i32, c_f32, c_i32, c_vp, ctypes.c_size_t, c_vp]
-        L.viscache_rope.argtypes = [P(vc_decode_shape), P(vc_rope), c_i32, c_vp, c_vp, P(vc_rows), P(vc_rows),
-                                    P(vc_rows), P(vc_rows), c_vp]
+        L.viscache_q8_attend.argtypes = [c_vp, c_vp, c_vp, c_vp, c_i32, c_vp, c_i32, c_i32, c_f32, c_i32, c_vp,
+                                         ctypes.c_size_t, c_vp]
+        L.viscache_rope.argtypes = [c_vp, c_vp, c_i32, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp]
         L.viscache_strerror.argtypes = [c_i32]
         L.viscache_strerror.restype = ctypes.c_char_p
         for name in ("viscache_budget", "viscache_out_rows", "viscache_prune", "viscache_prune_score_offsets",
@@ -342,15 +340,13 @@ def viscache_q8_append(shape: vc_decode_shape, cache: vc_q8cache, k: vc_rows, v:
                        unit_off: int, stream: int) -> None:
     """count, unit_off: device addresses, 0 for none."""
     st = lib().viscache_q8_append(_ref(shape), _ref(cache), _ref(k), _ref(v), n, count, unit_off, stream)
-    if st:
-        _check(st, "viscache_q8_append")
+    _check(st, "viscache_q8_append")
 
 
 def viscache_q8_read(shape: vc_decode_shape, cache: vc_q8cache, max_rows: int, k: vc_rows, v: vc_rows, unit_off: int,
                      out_fp32: int, stream: int) -> None:
     st = lib().viscache_q8_read(_ref(shape), _ref(cache), max_rows, _ref(k), _ref(v), unit_off, out_fp32, stream)
-    if st:
-        _check(st, "viscache_q8_read")
+    _check(st, "viscache_q8_read")
 
 
 def viscache_q8_attend_workspace_bytes(shape: vc_decode_shape, n: int, max_rows: int) -> int:
@@ -362,8 +358,7 @@ def viscache_q8_attend(shape: vc_decode_shape, cache: vc_q8cache, q: vc_rows, ou
                        stream: int) -> None:
     st = lib().viscache_q8_attend(_ref(shape), _ref(cache), _ref(q), _ref(out), n, count, causal, out_fp32, scale,
                                   max_rows, workspace, workspace_bytes, stream)
-    if st:
-        _check(st, "viscache_q8_attend")
+    _check(st, "viscache_q8_attend")
 
 
 def viscache_rope(shape: vc_decode_shape, rope: vc_rope, n: int, pos: int, count: int, q_in, q_out, k_in, k_out,
@@ -371,8 +366,7 @@ def viscache_rope(shape: vc_decode_shape, rope: vc_rope, n: int, pos: int, count
     """q_in ... k_out: vc_rows or None."""
     st = lib().viscache_rope(_ref(shape), _ref(rope), n, pos, count, _ref(q_in), _ref(q_out), _ref(k_in), _ref(k_out),
                              stream)
-    if st:
-        _check(st, "viscache_rope")
+    _check(st, "viscache_rope")
 
 
 def viscache_strerror(status: int) -> str:

@@ -7,14 +7,13 @@ import ctypes
 
 import torch
 
-from . import (VC_PRUNE_EVENTS, VC_Q8_BLOCK, VC_Q8_E4M3, VC_Q8_INT8, VC_RANK_GLOBAL, make_params, make_prune_io, make_shape, prune_with_io, vc_cache,
+from . import (VC_PRUNE_EVENTS, VC_Q8_BLOCK, VisCacheError, lib, VC_Q8_E4M3, VC_Q8_INT8, VC_RANK_GLOBAL, make_params, make_prune_io, make_shape, prune_with_io, vc_cache,
                vc_decode_shape, vc_q8cache, vc_qcache, vc_rope, vc_rows, viscache_append_kv, viscache_budget, viscache_decode_attn,
                viscache_decode_plan, viscache_decode_step, viscache_decode_step_noalloc,
                viscache_decode_step_planned, viscache_decode_step_q4,
                viscache_decode_step_workspace_bytes,
                viscache_decode_workspace_bytes, viscache_out_rows, viscache_prune_workspace_bytes,
-               viscache_q8_append, viscache_q8_attend, viscache_q8_attend_workspace_bytes, viscache_q8_read,
-               viscache_quantize_rows, viscache_rope)
+               viscache_q8_append, viscache_q8_attend_workspace_bytes, viscache_quantize_rows)
 
 
 def _stream() -> int:
@@ -226,54 +225,52 @@ class DecodeCache:
                                 _stream())
 
 
-def _rows(t: torch.Tensor, head_major: bool = False) -> vc_rows:
-    """The vc_rows of a tensor [L, B, n, H, d] ([L, B, H, n, d] with head_major)."""
-    sl, sb, s2, s3, sd = t.stride()
-    if sd != 1 and t.shape[-1] != 1:
-        raise ValueError("rows must be contiguous")
-    return vc_rows(t.data_ptr(), sl, sb, s3, s2) if head_major else vc_rows(t.data_ptr(), sl, sb, s2, s3)
+# ---- the 8-bit cache and the rotary positions ---------------------------------
+# A call of a few microseconds on the GPU is soon bound by what is done for it
+# here, so descriptors are packed as plain integers (a vc_rows is five of them)
+# and a tensor is looked at once.
+
+_Rows2, _Rows4 = ctypes.c_int64 * 10, ctypes.c_int64 * 20
+_ROWS_BYTES = 40
+assert ctypes.sizeof(vc_rows) == _ROWS_BYTES
+_current_device = getattr(torch._C, "_cuda_getDevice", None)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_BF16, _FP32 = torch.bfloat16, torch.float32
 
 
-def _expect(t: torch.Tensor, name: str, shape, dtypes, device) -> None:
-    if t.shape != shape or t.dtype not in dtypes or t.device != device:
-        raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype} on {t.device}, need {tuple(shape)} "
-                         f"{' or '.join(str(x) for x in dtypes)} on {device}")
+def _refuse(t, name, shape, typ, index):
+    raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype} on {t.device}, need {tuple(shape)} {typ} on GPU {index}")
 
 
-def _expect_ints(t, name: str, shape, device) -> int:
+def _take(t: torch.Tensor, name: str, shape, typ, index: int):
+    """(address, strides of the first four dimensions) of a tensor of this shape,
+    type and GPU whose rows are contiguous."""
+    if t.shape != shape or t.dtype is not typ or t.get_device() != index or index < 0:
+        _refuse(t, name, shape, typ, index)
+    s = t.stride()
+    if s[4] != 1:
+        raise ValueError(f"{name}: rows must be contiguous")
+    return t.data_ptr(), s[0], s[1], s[2], s[3]
+
+
+def _ints(t, name: str, shape, index: int) -> int:
     """Address of a contiguous int32 tensor (0 for None)."""
     if t is None:
         return 0
-    _expect(t, name, shape, (torch.int32,), device)
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
+    if t.shape != shape or t.dtype is not torch.int32 or t.get_device() != index or not t.is_contiguous():
+        _refuse(t, name, shape, "contiguous int32", index)
     return t.data_ptr()
 
 
-def _device(device) -> torch.device:
-    d = torch.device(device)
-    return torch.device(d.type, torch.cuda.current_device()) if d.type == "cuda" and d.index is None else d
-
-
-class _On:
-    """The device as the current one, for as long as a call is enqueued."""
-
-    def __init__(self, device: torch.device):
-        self.device = device
-
-    def __enter__(self):
-        self.prev = torch.cuda.current_device()
-        if self.prev != self.device.index:
-            torch.cuda.set_device(self.device)
-        return torch.cuda.current_stream().cuda_stream
-
-    def __exit__(self, *exc):
-        if self.prev != self.device.index:
-            torch.cuda.set_device(self.prev)
-
-
-_BF16 = (torch.bfloat16,)
-_OUT = (torch.bfloat16, torch.float32)
+def _enqueue(name: str, f, index: int, *args) -> None:
+    """f(*args, stream): the current stream of GPU `index`, as the current device."""
+    if _current_device() == index:
+        st = f(*args, _raw_stream(index))
+    else:
+        with torch.cuda.device(index):
+            st = f(*args, _raw_stream(index))
+    if st:
+        raise VisCacheError(st, name)
 
 
 class Rope:
@@ -290,41 +287,54 @@ class Rope:
             if len(inv_freq) != rot // 2:
                 raise ValueError(f"inv_freq: {len(inv_freq)} frequencies, need {rot // 2}")
             self._freq = (ctypes.c_double * (rot // 2))(*[float(x) for x in inv_freq])
-        self._params = {}
-        for fp32 in (0, 1):
-            for inverse in (0, 1):
-                self._params[fp32, inverse] = vc_rope(rot, (ctypes.c_int32 * 3)(*sections), layout, pairing, fp32,
-                                                      inverse, scale, theta, self._freq)
+        elif theta > 0:  # once, not in every call
+            self._freq = (ctypes.c_double * (rot // 2))(*[float(theta) ** (-2.0 * i / rot) for i in range(rot // 2)])
+        # By (fp32, inverse).
+        self._params = [[vc_rope(rot, (ctypes.c_int32 * 3)(*sections), layout, pairing, fp32, inverse, scale, theta,
+                                 self._freq) for inverse in (0, 1)] for fp32 in (0, 1)]
+        self._address = [[ctypes.addressof(p) for p in row] for row in self._params]
+        self._shapes = {}
+        self._f = lib().viscache_rope
 
     def apply(self, pos, q=None, k=None, q_out=None, k_out=None, inverse: bool = False, count=None):
         """Rotates q [L, B, n, Hq, d] and k [L, B, n, Hkv, d] (either may be
         None; both bf16 or fp32) by pos int32 [3, B, n] into q_out and k_out, by
-        default in place, on the current stream of their device.  `inverse`
-        turns back, which is the gradient.  Returns (q_out, k_out)."""
+        default in place, on the current stream of their GPU.  count int32 [B]:
+        the tokens of each sequence.  `inverse` turns back, which is the
+        gradient.  Returns (q_out, k_out)."""
         ref = q if q is not None else k
         if ref is None:
             raise ValueError("nothing to rotate")
+        typ, index = ref.dtype, ref.get_device()
         L, B, n, _, d = ref.shape
-        Hq = q.shape[3] if q is not None else k.shape[3]
-        Hkv = k.shape[3] if k is not None else Hq
-        if q is not None and q_out is None:
-            q_out = q
-        if k is not None and k_out is None:
-            k_out = k
-        dev, typ = ref.device, ref.dtype
-        if typ not in _OUT or d != self.d or dev.type != "cuda":
-            raise ValueError(f"rows of {d} {typ} on {dev}, need {self.d} bf16 or fp32 on a GPU")
-        for t, name, H in ((q, "q", Hq), (q_out, "q_out", Hq), (k, "k", Hkv), (k_out, "k_out", Hkv)):
-            if t is not None:
-                _expect(t, name, (L, B, n, H, d), (typ,), dev)
-        cnt = _expect_ints(count, "count", (B,), dev)
-        at = _expect_ints(pos, "pos", (3, B, n), dev)
+        if (typ is not _BF16 and typ is not _FP32) or d != self.d:
+            _refuse(ref, "q" if q is not None else "k", ref.shape[:-1] + (self.d,), "bf16 or fp32", max(index, 0))
+        none = (0, 0, 0, 0, 0)
+        qi = qo = ki = ko = none
+        Hq = Hkv = 0
+        if q is not None:
+            qi = _take(q, "q", ref.shape, typ, index)
+            qo = qi if q_out is None else _take(q_out, "q_out", q.shape, typ, index)
+            Hq = q.shape[3]
+        if k is not None:
+            Hkv = k.shape[3]
+            ki = _take(k, "k", (L, B, n, Hkv, d), typ, index)
+            ko = ki if k_out is None else _take(k_out, "k_out", k.shape, typ, index)
+        cnt = _ints(count, "count", (B,), index)
+        at = _ints(pos, "pos", (3, B, n), index)
+        q_out, k_out = q if q_out is None else q_out, k if k_out is None else k_out
         if ref.numel() == 0:
             return q_out, k_out
-        r = [None if t is None else _rows(t) for t in (q, q_out, k, k_out)]
-        with _On(dev) as stream:
-            viscache_rope(vc_decode_shape(B, L, Hq, Hkv, d), self._params[int(typ == torch.float32), int(inverse)], n,
-                          at, cnt, r[0], r[1], r[2], r[3], stream)
+        key = (L, B, Hq or Hkv, Hkv or Hq)
+        shape = self._shapes.get(key)
+        if shape is None:
+            shape = self._shapes[key] = vc_decode_shape(B, L, Hq or Hkv, Hkv or Hq, d)
+        rows = _Rows4(*qi, *qo, *ki, *ko)
+        r = ctypes.addressof(rows)
+        rq, rk = (r if Hq else 0), (r + 2 * _ROWS_BYTES if Hkv else 0)
+        _enqueue("viscache_rope", self._f, index, ctypes.addressof(shape),
+                 self._address[typ is _FP32][bool(inverse)], n, at, cnt, rq, rq and rq + _ROWS_BYTES, rk,
+                 rk and rk + _ROWS_BYTES)
         return q_out, k_out
 
 
@@ -346,7 +356,10 @@ class Q8Cache:
     def __init__(self, L, B, Hq, Hkv, d, caps, device, format: str = "e4m3", buffers=None):
         self.L, self.B, self.Hq, self.Hkv, self.d = L, B, Hq, Hkv, d
         self.shape = vc_decode_shape(B, L, Hq, Hkv, d)
-        self.device = _device(device)
+        self.device = torch.device(device)
+        if self.device.type == "cuda" and self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self._index = self.device.index if self.device.type == "cuda" else -1
         self.units = L * B * Hkv
         caps = [int(c) for c in caps]
         if len(caps) != self.units or min(caps, default=0) < 0:
@@ -370,43 +383,57 @@ class Q8Cache:
             buffers["row_off"] = torch.tensor(offs, dtype=torch.int64, device=self.device) * VC_Q8_BLOCK
             buffers["cap"] = torch.tensor(caps, dtype=torch.int32, device=self.device)
         for name, (shape, t) in need.items():
-            _expect(buffers[name], name, shape, (t,), self.device)
-            if not buffers[name].is_contiguous():
-                raise ValueError(f"{name} must be contiguous")
-            setattr(self, name, buffers[name])
+            b = buffers[name]
+            if b.shape != shape or b.dtype is not t or b.device != self.device or not b.is_contiguous():
+                _refuse(b, name, shape, f"contiguous {t}", self._index)
+            setattr(self, name, b)
         # Attention starts on the units with the most room first.
         order = sorted(range(self.units), key=lambda u: -caps[u])
         self.order = torch.tensor(order, dtype=torch.int32, device=self.device) if len(set(caps)) > 1 else None
         self.c = vc_q8cache(code, *[buffers[name].data_ptr() for name in _Q8_BUFFERS],
                             0 if self.order is None else self.order.data_ptr())
-        self._ws, self._ws_bytes, self._kept = None, {}, []
+        self._ws, self._ws_of, self._kept = None, {}, []
+        self._shape_at, self._cache_at = ctypes.addressof(self.shape), ctypes.addressof(self.c)
+        self._lib = lib()
 
     def _workspace(self, n: int, max_rows: int):
-        """The workspace, grown when a call needs more than any before it (a
-        call that is captured into a graph must have run once before)."""
-        key = (n, max_rows)
-        need = self._ws_bytes.get(key)
-        if need is None:
-            need = self._ws_bytes[key] = viscache_q8_attend_workspace_bytes(self.shape, n, max_rows)
-        if self._ws is None or self._ws.numel() < need:
-            if torch.cuda.is_current_stream_capturing():
-                raise RuntimeError("the workspace is too small: run the call once before it is captured")
-            self._ws = torch.empty((need,), dtype=torch.uint8, device=self.device)
-            self._kept.append(self._ws)  # a graph captured before this goes on using the one it was captured with
-        return self._ws
+        """(address, bytes) of the workspace, grown when a call needs more than any
+        before it (a call that is captured into a graph must have run once)."""
+        ws = self._ws_of.get((n, max_rows))
+        if ws is None:
+            need = viscache_q8_attend_workspace_bytes(self.shape, n, max_rows)
+            if self._ws is None or self._ws.numel() < need:
+                if torch.cuda.is_current_stream_capturing():
+                    raise RuntimeError("the workspace is too small: run the call once before it is captured")
+                self._ws = torch.empty((need,), dtype=torch.uint8, device=self.device)
+                self._kept.append(self._ws)  # a graph captured before this goes on using the one it knows
+                self._ws_of.clear()
+            ws = self._ws_of[n, max_rows] = self._ws.data_ptr(), self._ws.numel()
+        return ws
 
     def append(self, k, v, count=None, head_major: bool = False) -> None:
         """Appends k, v bf16 [L, B, n, Hkv, d] ([L, B, Hkv, n, d] with
         head_major); count int32 [L*B]: the rows of each layer and sequence."""
-        n = k.shape[3 if head_major else 2]
-        want = (self.L, self.B, self.Hkv, n, self.d) if head_major else (self.L, self.B, n, self.Hkv, self.d)
-        _expect(k, "k", want, _BF16, self.device)
-        _expect(v, "v", want, _BF16, self.device)
-        cnt = _expect_ints(count, "count", (self.L * self.B,), self.device)
+        kr, vr, n = self._pair(k, v, head_major, _BF16)
+        cnt = _ints(count, "count", (self.L * self.B,), self._index)
         if n == 0:
             return
-        with _On(self.device) as stream:
-            viscache_q8_append(self.shape, self.c, _rows(k, head_major), _rows(v, head_major), n, cnt, 0, stream)
+        rows = _Rows2(*kr, *vr)
+        r = ctypes.addressof(rows)
+        _enqueue("viscache_q8_append", self._lib.viscache_q8_append, self._index, self._shape_at, self._cache_at, r,
+                 r + _ROWS_BYTES, n, cnt, 0)
+
+    def _pair(self, k, v, head_major, typ):
+        """The descriptors of keys and values [L, B, n, Hkv, d] (or [L, B, Hkv, n, d]), and n."""
+        if head_major:
+            n = k.shape[3]
+            want = (self.L, self.B, self.Hkv, n, self.d)
+            (p, s0, s1, s2, s3), (pv, v0, v1, v2, v3) = (_take(k, "k", want, typ, self._index),
+                                                         _take(v, "v", want, typ, self._index))
+            return (p, s0, s1, s3, s2), (pv, v0, v1, v3, v2), n
+        n = k.shape[2]
+        want = (self.L, self.B, n, self.Hkv, self.d)
+        return _take(k, "k", want, typ, self._index), _take(v, "v", want, typ, self._index), n
 
     def load_pruned(self, pc: "PruneCall") -> None:
         """Appends what pc.run() left in its outputs (bf16 values): every
@@ -420,7 +447,8 @@ class Q8Cache:
                             for l in range(pc.L)], dtype=torch.int64)
         most = count.amax(dim=1).tolist()
         count, off = count.to(self.device), off.to(self.device)
-        with _On(self.device) as stream:
+        with torch.cuda.device(self._index):
+            stream = _raw_stream(self._index)
             for l in range(pc.L):
                 if most[l] == 0:
                     continue
@@ -428,7 +456,8 @@ class Q8Cache:
                                self.k_tail[l * per:].data_ptr(), self.v_tail[l * per:].data_ptr(),
                                self.row_off[l * per:].data_ptr(), self.cap[l * per:].data_ptr(),
                                self.len[l * per:].data_ptr(), 0)
-                _expect(pc.k_out[l], "k_out", pc.k_out[l].shape, _BF16, self.device)
+                if pc.k_out[l].get_device() != self._index:
+                    raise ValueError("the pruned cache is on another device")
                 k = vc_rows(pc.k_out[l].data_ptr(), 0, 0, self.d, 0)
                 v = vc_rows(pc.v_out[l].data_ptr(), 0, 0, self.d, 0)
                 viscache_q8_append(one, c, k, v, most[l], count[l].data_ptr(), off[l].data_ptr(), stream)
@@ -437,34 +466,36 @@ class Q8Cache:
         """Reads rows [0, len) of every unit back into k, v (bf16 or fp32)
         [L, B, rows, Hkv, d] ([L, B, Hkv, rows, d] with head_major); rows behind
         them are left as they were.  max_rows: by default, as many as k holds."""
-        rows = k.shape[3 if head_major else 2]
-        want = (self.L, self.B, self.Hkv, rows, self.d) if head_major else (self.L, self.B, rows, self.Hkv, self.d)
-        _expect(k, "k", want, _OUT, self.device)
-        _expect(v, "v", want, (k.dtype,), self.device)
+        typ = k.dtype
+        if typ is not _BF16 and typ is not _FP32:
+            _refuse(k, "k", k.shape, "bf16 or fp32", self._index)
+        kr, vr, rows = self._pair(k, v, head_major, typ)
         m = rows if max_rows is None else int(max_rows)
         if m > rows:
             raise ValueError(f"max_rows {m} exceeds the {rows} rows of k")
         if rows == 0:
             return
-        with _On(self.device) as stream:
-            viscache_q8_read(self.shape, self.c, m, _rows(k, head_major), _rows(v, head_major), 0,
-                             int(k.dtype == torch.float32), stream)
+        rows = _Rows2(*kr, *vr)
+        r = ctypes.addressof(rows)
+        _enqueue("viscache_q8_read", self._lib.viscache_q8_read, self._index, self._shape_at, self._cache_at, m, r,
+                 r + _ROWS_BYTES, 0, int(typ is _FP32))
 
     def attend(self, q, out, scale: float, count=None, causal: bool = True, max_rows=None) -> None:
         """Attention of q bf16 [L, B, n, Hq, d] over the cache into out (bf16 or
         fp32, the same shape); count int32 [B]: the queries of each sequence."""
         n = q.shape[2]
         want = (self.L, self.B, n, self.Hq, self.d)
-        _expect(q, "q", want, _BF16, self.device)
-        _expect(out, "out", want, _OUT, self.device)
-        cnt = _expect_ints(count, "count", (self.B,), self.device)
+        fp32 = out.dtype is _FP32
+        packed = _Rows2(*_take(q, "q", want, _BF16, self._index),
+                        *_take(out, "out", want, _FP32 if fp32 else _BF16, self._index))
+        cnt = _ints(count, "count", (self.B,), self._index)
         if n == 0:
             return
         rows = self.max_cap if max_rows is None else int(max_rows)
-        with _On(self.device) as stream:
-            ws = self._workspace(n, rows)
-            viscache_q8_attend(self.shape, self.c, _rows(q), _rows(out), n, cnt, int(causal),
-                               int(out.dtype == torch.float32), scale, rows, ws.data_ptr(), ws.numel(), stream)
+        ws = self._workspace(n, rows)
+        r = ctypes.addressof(packed)
+        _enqueue("viscache_q8_attend", self._lib.viscache_q8_attend, self._index, self._shape_at, self._cache_at, r,
+                 r + _ROWS_BYTES, n, cnt, int(causal), int(fp32), scale, rows, ws[0], ws[1])
 
     def step(self, q, k, v, out, scale: float, rope: Rope | None = None, pos=None, q_out=None, k_out=None) -> None:
         """A serving step: rotates q and k by pos (with `rope`; into q_out and

@@ -172,17 +172,13 @@ def test_rope_frequencies_are_checked(vc):
 def test_python_checks():
     """Shapes, types and devices are checked before any pointer is taken."""
     import torch
-    from paper_2608_24063_amd.tensors import Q8Cache, Rope, _expect, _rows
+    from paper_2608_24063_amd.tensors import Q8Cache, Rope
     with pytest.raises(ValueError):
         Rope(64).apply(None)
     with pytest.raises(ValueError):
         Rope(64).apply(torch.zeros(3, 1, 2, dtype=torch.int32), torch.zeros(1, 1, 2, 4, 64))  # not on a GPU
     with pytest.raises(ValueError):
         Rope(64, inv_freq=[1.0] * 31)
-    with pytest.raises(ValueError):
-        _rows(torch.zeros(1, 1, 2, 64, 4).transpose(3, 4))
-    with pytest.raises(ValueError):
-        _expect(torch.zeros(3), "x", (4,), (torch.float32,), torch.device("cpu"))
     with pytest.raises(ValueError):
         Q8Cache(1, 1, 2, 2, 64, [5], "cpu")
     c = Q8Cache(1, 1, 4, 2, 64, [5, 70], "cpu")
@@ -197,8 +193,13 @@ def test_python_checks():
         c.append(x, x, count=torch.zeros(2, dtype=torch.int32))
     with pytest.raises(ValueError):
         c.attend(x, x, 1.0)
+    with pytest.raises(ValueError):  # the right shapes, but nothing of it on a GPU
+        c.append(x, x)
     with pytest.raises(ValueError):
-        c.read(x, x, max_rows=3)
+        c.read(x, x)
+    q = torch.zeros(1, 1, 2, 4, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError):
+        c.attend(q, q, 1.0)
     buf = {n: getattr(c, n) for n in ("k_codes", "v_codes", "k_scale", "v_scale", "k_tail", "v_tail", "row_off", "cap", "len")}
     Q8Cache(1, 1, 4, 2, 64, [5, 70], "cpu", buffers=buf)
     with pytest.raises(ValueError):
