@@ -44,12 +44,14 @@ __device__ __forceinline__ f16x8 half8_of_bf16(u32x4 w, float f) {
   return r;
 }
 
+// Pitches in halves: 16-byte reads of 32 rows without conflicts.
 template <int D>
-struct Tile {
-  static constexpr int KP = D + 8;           // pitches in halves: 16-byte reads of 32 rows without conflicts
-  static constexpr int VP = kQ8Block + 8;
-  _Float16 k[kQ8Block][KP];
-  _Float16 v[D][VP];
+struct Keys {
+  _Float16 k[kQ8Block][D + 8];
+};
+template <int D>
+struct Values {
+  _Float16 v[D][kQ8Block + 8];
 };
 
 // Where row r of a 32-row half sits in LDS: matrix row 8 j + 4 h + i holds row
@@ -65,7 +67,14 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt8(Q8Attn p) {
   constexpr int kItems = kQ8Block * D / 16;           // 16-code chunks of a block's keys (or values)
   constexpr int IT = (kItems + NT - 1) / NT;
   constexpr bool kPart = kItems < NT;                 // only the first kItems threads have one
-  __shared__ Tile<D> tile[2] __attribute__((aligned(16)));
+  // Phases (see the loop) pay where there are two waves a SIMD and the matrix
+  // part is long: d = 128 with bf16 outputs.  (us, with and without: 2048 queries
+  // over 23040 rows in 64 heads 1362, 1427; 64 over 1300 in 28 layers 52, 58; d =
+  // 64, 1024 over 8192 in four sequences 132, 126; fp32 outputs, which then spill
+  // registers, 2222, 2186.)
+  constexpr bool kPair = NW == 8 && D == 128 && !F32;
+  __shared__ Keys<D> tk[2] __attribute__((aligned(16)));
+  __shared__ Values<D> tv[2] __attribute__((aligned(16)));
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int ln = lane & 31, hf = lane >> 5;
   // Workgroups of a unit follow each other on one XCD and share its L2.
@@ -84,7 +93,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt8(Q8Attn p) {
   auto rows_seen = [&](int col) { return max(min(p.causal ? lim + col / p.G : len, p.max_rows), 0); };
   const int emax = rows_seen(cl);
   const int nt = (emax + kQ8Block - 1) / kQ8Block;
-  const int t0 = (int)((int64_t)sp * nt / p.ns), t1 = (int)((int64_t)(sp + 1) * nt / p.ns);
+  const int t0 = (int)((int64_t)sp * nt / p.ns), T = (int)((int64_t)(sp + 1) * nt / p.ns) - t0;
   const int col = c0 + 32 * w + ln;
   const int end = rows_seen(min(col, cl));
   const int wmin = rows_seen(min(c0 + 32 * w, cl));  // fewest rows a column of the wave sees
@@ -118,78 +127,136 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt8(Q8Attn p) {
   }
 
   u32x4 rk[IT], rv[IT];
-  auto fetch = [&](int t) {
-    const uint8_t *k = p.c.kc + (blk0 + t) * (kQ8Block * D), *v = p.c.vc + (blk0 + t) * (kQ8Block * D);
+  auto fetch_k = [&](int t) {
+    const uint8_t *k = p.c.kc + (blk0 + t) * (kQ8Block * D);
 #pragma unroll
-    for (int it = 0; it < IT; ++it) {
-      const int e = kPart ? min(tid, kItems - 1) : tid + NT * it;
-      rk[it] = ld16(k + 16 * e);
-      rv[it] = ld16(v + 16 * e);
-    }
+    for (int it = 0; it < IT; ++it) rk[it] = ld16(k + 16 * (kPart ? min(tid, kItems - 1) : tid + NT * it));
   };
-  auto stage = [&](int buf) {
+  auto fetch_v = [&](int t) {
+    const uint8_t *v = p.c.vc + (blk0 + t) * (kQ8Block * D);
+#pragma unroll
+    for (int it = 0; it < IT; ++it) rv[it] = ld16(v + 16 * (kPart ? min(tid, kItems - 1) : tid + NT * it));
+  };
+  auto stage_k = [&](int buf) {
     if (kPart && tid >= kItems) return;
 #pragma unroll
     for (int it = 0; it < IT; ++it) {
       const int e = tid + NT * it;
-      const int row = place(e / (D / 16)), c = e % (D / 16);
-      _Float16 *kd = &tile[buf].k[row][16 * c];
-      *reinterpret_cast<f16x8 *>(kd) = Q8<FMT>::half8(rk[it].x, rk[it].y);
-      *reinterpret_cast<f16x8 *>(kd + 8) = Q8<FMT>::half8(rk[it].z, rk[it].w);
-      _Float16 *vd = &tile[buf].v[e / 4][16 * (e % 4)];
-      *reinterpret_cast<f16x8 *>(vd) = Q8<FMT>::half8(rv[it].x, rv[it].y);
-      *reinterpret_cast<f16x8 *>(vd + 8) = Q8<FMT>::half8(rv[it].z, rv[it].w);
+      _Float16 *to = &tk[buf].k[place(e / (D / 16))][16 * (e % (D / 16))];
+      *reinterpret_cast<f16x8 *>(to) = Q8<FMT>::half8(rk[it].x, rk[it].y);
+      *reinterpret_cast<f16x8 *>(to + 8) = Q8<FMT>::half8(rk[it].z, rk[it].w);
+    }
+  };
+  auto stage_v = [&](int buf) {
+    if (kPart && tid >= kItems) return;
+#pragma unroll
+    for (int it = 0; it < IT; ++it) {
+      const int e = tid + NT * it;
+      _Float16 *to = &tv[buf].v[e / 4][16 * (e % 4)];
+      *reinterpret_cast<f16x8 *>(to) = Q8<FMT>::half8(rv[it].x, rv[it].y);
+      *reinterpret_cast<f16x8 *>(to + 8) = Q8<FMT>::half8(rv[it].z, rv[it].w);
     }
   };
   // The open block: bf16 rows scaled by their powers of two, zeros past its end.
-  auto stage_open = [&](int buf) {
-    const int rows = len - nsealed * kQ8Block;
-    const uint16_t *kt = p.c.kt + (int64_t)u * kQ8Block * D, *vt = p.c.vt + (int64_t)u * kQ8Block * D;
-    const float kinv = 1.f / ldg(p.c.ks + blk0 + nsealed), vinv = 1.f / ldg(p.c.vs + blk0 + nsealed);
+  const int orows = len - nsealed * kQ8Block;
+  const int Tc = max(min(t0 + T, nsealed) - t0, 0);  // sealed blocks
+  auto open_rows = [&](const uint16_t *tail, const float *scale, auto put) {
+    const float inv = 1.f / ldg(scale + blk0 + nsealed);
     for (int e = tid; e < kQ8Block * D / 8; e += NT) {
       const int row = e / (D / 8), c = e % (D / 8);
-      const bool in = row < rows;
-      const u32x4 zero = {0u, 0u, 0u, 0u};
-      *reinterpret_cast<f16x8 *>(&tile[buf].k[place(row)][8 * c]) =
-          half8_of_bf16(in ? ld16(kt + row * D + 8 * c) : zero, kinv);
-      const f16x8 v = half8_of_bf16(in ? ld16(vt + row * D + 8 * c) : zero, vinv);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) tile[buf].v[8 * c + k][row] = v[k];
+      const u32x4 x = row < orows ? ld16(tail + (int64_t)u * kQ8Block * D + row * D + 8 * c) : u32x4{0u, 0u, 0u, 0u};
+      put(row, 8 * c, half8_of_bf16(x, inv));
     }
   };
+  auto open_k = [&](int buf) {
+    open_rows(p.c.kt, p.c.ks, [&](int row, int c, f16x8 x) { *reinterpret_cast<f16x8 *>(&tk[buf].k[place(row)][c]) = x; });
+  };
+  auto open_v = [&](int buf) {
+    open_rows(p.c.vt, p.c.vs, [&](int row, int c, f16x8 x) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) tv[buf].v[c + k][row] = x[k];
+    });
+  };
 
-  f32x16 O[CB];
+  f32x16 O[CB], S[2];
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
     for (int i = 0; i < 16; ++i) O[cb][i] = 0.f;
   float m = kNegInf, l = 0.f;
+  f16x8 hi[4], lo[4];
+  float vprev = 1.f;  // the value scale that belongs to hi and lo
 
-  // Block t, staged in T, into the wave's state.
-  auto absorb = [&](int t, const Tile<D> &T) {
-    const float ks = ldg(p.c.ks + blk0 + t), vs = ldg(p.c.vs + blk0 + t);
-    f32x16 S[2];
+  auto logits = [&](const Keys<D> &K) {
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
+    for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) S[kb][i] = 0.f;
+      for (int k = 0; k < 16; ++k) S[kb][k] = 0.f;
 #pragma unroll
-      for (int s = 0; s < KS; ++s)
-        S[kb] = mfma32(*reinterpret_cast<const f16x8 *>(&T.k[32 * kb + ln][16 * s + 8 * hf]), q[s], S[kb]);
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+        S[kb] = mfma32(*reinterpret_cast<const f16x8 *>(&K.k[32 * kb + ln][16 * s + 8 * hf]), q[s], S[kb]);
+  };
+  auto outputs = [&](const Values<D> &V) {
+    if (F32) {
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) {
+        f32x16 acc;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) acc[k] = 0.f;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+          const f16x8 a = *reinterpret_cast<const f16x8 *>(&V.v[32 * cb + ln][16 * s + 8 * hf]);
+          acc = mfma32(a, lo[s], mfma32(a, hi[s], acc));
+        }
+#pragma unroll
+        for (int k = 0; k < 16; ++k) O[cb][k] = fmaf(acc[k], vprev, O[cb][k]);
+      }
+    } else {
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb)
+          O[cb] = mfma32(*reinterpret_cast<const f16x8 *>(&V.v[32 * cb + ln][16 * s + 8 * hf]), hi[s], O[cb]);
     }
+  };
+  // The matrix part of block i: its logits, and the block before it into O; the
+  // operands' reads run kAhead products ahead.
+  auto products = [&](int i) {
+    outputs(tv[(i & 1) ^ 1]);
+    logits(tk[i & 1]);
+    if (!F32) {
+      constexpr int kAll = 2 * KS + 4 * CB, kAhead = 4;
+      __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+      for (int k = 0; k < kAll - kAhead; ++k) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x8, kAhead, 0);
+    }
+  };
+  // The weights of block t0 + i from its logits.
+  auto weights = [&](int i, float ks, float vs) {
+    const int t = t0 + i;
     const float c = fmaxf(cq * ks, 1e-37f);
     if ((t + 1) * kQ8Block > wmin) {  // wave-uniform
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int row = t * kQ8Block + 32 * kb + 16 * (i >> 3) + 8 * hf + 4 * ((i >> 2) & 1) + (i & 3);
-          if (row >= end) S[kb][i] = kNegInf;
+        for (int k = 0; k < 16; ++k) {
+          const int row = t * kQ8Block + 32 * kb + 16 * (k >> 3) + 8 * hf + 4 * ((k >> 2) & 1) + (k & 3);
+          if (row >= end) S[kb][k] = kNegInf;
         }
     }
-    float mx = fmaxf(S[0][0], S[1][0]);
+    // (med3 with infinity is a maximum that needs no quieted inputs.)
+    float x[16];
 #pragma unroll
-    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, fmaxf(S[0][i], S[1][i]));
+    for (int k = 0; k < 16; ++k) x[k] = __builtin_amdgcn_fmed3f(S[0][k], S[1][k], __builtin_inff());
+    float mx = fmaxf(x[0], x[1]);
+#pragma unroll
+    for (int k = 2; k < 16; ++k) mx = fmaxf(mx, x[k]);
     const float lvs = F32 ? 0.f : __builtin_amdgcn_logf(vs);
     mx = fmaf(max_halves(mx), c, lvs);
     if (__builtin_amdgcn_ballot_w64(mx > (F32 ? m : m + kLag))) {
@@ -203,69 +270,93 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt8(Q8Attn p) {
     // lvs less the maximum, plus the lift; anything finite while the column
     // has seen no row.
     const float off = (m == kNegInf ? 0.f : lvs - m) + (F32 ? 0.f : kLift);
-    f16x8 hi[4], lo[4];
     float sum = 0.f;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float pr = fast_exp2(fmaf(S[kb][i], c, off));
+      for (int k = 0; k < 16; ++k) {
+        const float pr = fast_exp2(fmaf(S[kb][k], c, off));
         sum += pr;
         if (F32) {
           const float ps = pr * 16384.f;
           const _Float16 h = (_Float16)ps;
-          hi[2 * kb + i / 8][i % 8] = h;
-          lo[2 * kb + i / 8][i % 8] = (_Float16)(ps - (float)h);
+          hi[2 * kb + k / 8][k % 8] = h;
+          lo[2 * kb + k / 8][k % 8] = (_Float16)(ps - (float)h);
         } else {
-          hi[2 * kb + i / 8][i % 8] = (_Float16)pr;
+          hi[2 * kb + k / 8][k % 8] = (_Float16)pr;
         }
       }
     l = F32 ? l + sum : fmaf(sum, __builtin_amdgcn_rcpf(vs), l);
-#pragma unroll
-    for (int cb = 0; cb < CB; ++cb) {
-      f32x16 acc;
-      if (F32) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) acc[i] = 0.f;
-      } else {
-        acc = O[cb];
-      }
-#pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const f16x8 v = *reinterpret_cast<const f16x8 *>(&T.v[32 * cb + ln][16 * s + 8 * hf]);
-        acc = mfma32(v, hi[s], acc);
-        if (F32) acc = mfma32(v, lo[s], acc);
-      }
-      if (F32) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) O[cb][i] = fmaf(acc[i], vs, O[cb][i]);
-      } else {
-        O[cb] = acc;
-      }
-    }
+    vprev = vs;
   };
+  // Keys of sealed block i + 1 and values of block i into LDS, and the requests
+  // of the ones after them.  Past the last block the last one again: under a
+  // condition the requests would wait for each other.
+  auto supply = [&](int i) {
+    stage_k((i + 1) & 1);
+    stage_v(i & 1);
+    fetch_k(t0 + min(i + 2, Tc - 1));
+    fetch_v(t0 + min(i + 1, Tc - 1));
+  };
+  auto scale_at = [&](const float *scale, int i) { return ldg(scale + blk0 + t0 + min(i, Tc - 1)); };
 
-  if (t0 < t1) {
-    if (t0 < nsealed) {
-      fetch(t0);
-      stage(0);
+  if (Tc > 0) {
+    fetch_k(t0);
+    fetch_v(t0);
+    stage_k(0);
+    fetch_k(t0 + min(1, Tc - 1));
+    __syncthreads();
+    if (kPair) {
+      // Two waves share a SIMD: while one multiplies and stages, the other
+      // weighs.  The second half of the waves runs one phase behind.
+      const bool first = w < NW / 2;
+      float ks = scale_at(p.c.ks, 0), vs = scale_at(p.c.vs, 0);
+      if (!first) __syncthreads();
+      if (live) logits(tk[0]);
+      supply(0);
+      __syncthreads();
+      for (int i = 1; i < Tc; ++i) {
+        if (live) weights(i - 1, ks, vs);
+        ks = scale_at(p.c.ks, i), vs = scale_at(p.c.vs, i);
+        __syncthreads();
+        if (live) products(i);
+        supply(i);
+        __syncthreads();
+      }
+      if (live) weights(Tc - 1, ks, vs);
+      if (first) __syncthreads();
+      if (live) outputs(tv[(Tc - 1) & 1]);
     } else {
-      stage_open(0);
+      float ks = scale_at(p.c.ks, 0), vs = scale_at(p.c.vs, 0);
+      if (live) {
+        logits(tk[0]);
+        weights(0, ks, vs);
+      }
+      supply(0);
+      __syncthreads();
+      for (int i = 1; i < Tc; ++i) {
+        ks = scale_at(p.c.ks, i), vs = scale_at(p.c.vs, i);
+        if (live) {
+          products(i);
+          weights(i, ks, vs);
+        }
+        supply(i);
+        __syncthreads();
+      }
+      if (live) outputs(tv[(Tc - 1) & 1]);
     }
   }
-  __syncthreads();
-  for (int t = t0; t < t1; ++t) {
-    const int buf = (t - t0) & 1;
-    const bool more = t + 1 < t1, code = t + 1 < nsealed;
-    if (more && code) fetch(t + 1);
-    if (live) absorb(t, tile[buf]);
-    if (more) {
-      if (code)
-        stage(buf ^ 1);
-      else
-        stage_open(buf ^ 1);
-    }
+  if (T > Tc) {  // the open block, by itself
+    __syncthreads();  // the last values are read
+    open_k(Tc & 1);
+    open_v(Tc & 1);
     __syncthreads();
+    if (live) {
+      const float ks = ldg(p.c.ks + blk0 + nsealed), vs = ldg(p.c.vs + blk0 + nsealed);
+      logits(tk[Tc & 1]);
+      weights(Tc, ks, vs);
+      outputs(tv[Tc & 1]);
+    }
   }
   l = sum_halves(l);
   if (F32) l *= 16384.f;  // the factor that P's two parts carry
