@@ -336,7 +336,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_decode8(Q8Attn p) {
 
 template <int D, int FMT>
 hipError_t launch(const Q8Attn &p, hipStream_t st) {
-  const dim3 grid((uint32_t)((int64_t)p.units * p.npmax)), block(64 * kWaves);
+  const dim3 grid((uint32_t)p.wgs), block(64 * kWaves);
   if (p.fp32)
     hipLaunchKernelGGL((k_decode8<D, FMT, true>), grid, block, 0, st, p);
   else

@@ -25,6 +25,8 @@ __global__ __launch_bounds__(256) void k_join(Q8Attn p) {
   const int tid = threadIdx.x, grp = tid / TPG, ch = tid % TPG * 4;
   const int g = u % p.Hkv, lb = u / p.Hkv, b = lb % p.B;
   const int len_ = ldg(p.c.len + u), cap_ = ldg(p.c.cap + u), cnt_ = p.count ? ldg(p.count + b) : p.n;
+  int2 tiles = make_int2(0, 0);
+  if (p.npmax == 1 && p.count) tiles = count_tiles(p, b, tid & 63);
   if (col >= min(max(cnt_, 0), p.n) * p.G) return;
   int64_t at;  // part 0 of the column
   int ns;
@@ -34,8 +36,14 @@ __global__ __launch_bounds__(256) void k_join(Q8Attn p) {
     if (ns <= 1) return;
     at = (int64_t)u * p.npmax * p.qcols + col;
   } else {
+    int64_t tile = (int64_t)u * p.nqt;
     ns = p.ns;
-    at = ((int64_t)u * p.nqt + col / p.qcols) * p.ns * p.qcols + col % p.qcols;
+    if (p.count) {  // as share_of has them
+      ns = splits_of(p, tiles.x, (uint32_t)p.wgs);
+      tile = ((int64_t)(lb / p.B) * tiles.x + tiles.y) * p.Hkv + (int64_t)g * tiles_of(p, b);
+    }
+    if (ns == 1) return;  // written already
+    at = (tile + col / p.qcols) * ns * p.qcols + col % p.qcols;
   }
   float M = kNegInf, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
   for (int s0 = grp; s0 < ns; s0 += NG * U) {

@@ -79,9 +79,9 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt8(Q8Attn p) {
   const int ln = lane & 31, hf = lane >> 5;
   // Workgroups of a unit follow each other on one XCD and share its L2.
   const uint32_t id = xcd_block(blockIdx.x, gridDim.x);
-  const int per = p.nqt * p.ns;
-  const int u = (int)(id / (uint32_t)per), rest = (int)(id % (uint32_t)per);
-  const int qt = rest / p.ns, sp = rest % p.ns;
+  const Share sh = share_of(p, id, (uint32_t)p.wgs, lane);
+  const int u = sh.u, qt = sh.qt, sp = sh.sp, ns = sh.ns;
+  if (u < 0) return;
   const int b = u / p.Hkv % p.B;
   const int len = max(min(ldg(p.c.len + u), ldg(p.c.cap + u)), 0);
   const int cnt = p.count ? min(max(ldg(p.count + b), 0), p.n) : p.n;
@@ -93,7 +93,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt8(Q8Attn p) {
   auto rows_seen = [&](int col) { return max(min(p.causal ? lim + col / p.G : len, p.max_rows), 0); };
   const int emax = rows_seen(cl);
   const int nt = (emax + kQ8Block - 1) / kQ8Block;
-  const int t0 = (int)((int64_t)sp * nt / p.ns), T = (int)((int64_t)(sp + 1) * nt / p.ns) - t0;
+  const int t0 = (int)((int64_t)sp * nt / ns), T = (int)((int64_t)(sp + 1) * nt / ns) - t0;
   const int col = c0 + 32 * w + ln;
   const int end = rows_seen(min(col, cl));
   const int wmin = rows_seen(min(c0 + 32 * w, cl));  // fewest rows a column of the wave sees
@@ -361,7 +361,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt8(Q8Attn p) {
   l = sum_halves(l);
   if (F32) l *= 16384.f;  // the factor that P's two parts carry
   if (col > cl) return;
-  if (p.ns == 1) {
+  if (ns == 1) {
     const float inv = l > 0.f ? 1.f / l : 0.f;
     const int64_t at = row_of(p.out, col);
 #pragma unroll
@@ -379,8 +379,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt8(Q8Attn p) {
       }
     return;
   }
-  const int64_t slot = ((int64_t)u * p.nqt + qt) * p.ns + sp;
-  const int64_t at = slot * p.qcols + 32 * w + ln;
+  const int64_t at = (int64_t)id * p.qcols + 32 * w + ln;
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
@@ -393,7 +392,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt8(Q8Attn p) {
 
 template <int D, int FMT, int NW>
 void launch_nw(const Q8Attn &p, hipStream_t st) {
-  const dim3 grid((uint32_t)((int64_t)p.units * p.nqt * p.ns)), block(64 * NW);
+  const dim3 grid((uint32_t)p.wgs), block(64 * NW);
   if (p.fp32)
     hipLaunchKernelGGL((k_prompt8<D, FMT, NW, true>), grid, block, 0, st, p);
   else

@@ -42,16 +42,18 @@ struct Q8Attn {
   Q8Cache c;
   RowsDesc q, out;
   const int32_t *count;  // queries per sequence; null: n
-  int32_t B, Hq, Hkv, G, d, units;
+  int32_t L, B, Hq, Hkv, G, d, units;
+  int32_t wgs;           // workgroups of the attention launch
   int32_t n, cols;       // queries per sequence; cols = n * G
   int32_t causal, fp32;
   int32_t max_rows;
   float sc;              // scale * log2(e)
   // One token at a time (cols <= 16): pieces of `piece` blocks, at most npmax
   // a unit (qcols 16).  Prompts (npmax 1): nqt column tiles of qcols columns,
-  // each in ns key splits.
+  // each in ns key splits, or, where counts leave tiles empty, as many (up to
+  // nsmax) as the launch's workgroups allow.
   int32_t piece, npmax;
-  int32_t qcols, nqt, ns;
+  int32_t qcols, nqt, ns, nsmax;
   float *part_o;         // partial results: [part][qcols][d], [part][qcols]
   float2 *part_ml;
 };

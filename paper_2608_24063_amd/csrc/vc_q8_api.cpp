@@ -72,7 +72,7 @@ Q8Cache bind(const vc_q8cache *c) {
 // How an attention call is cut, and what it needs of the workspace: partial O,
 // then (max, sum).
 struct Cut {
-  int32_t piece = 0, npmax = 1, qcols = 0, nqt = 0, ns = 1;
+  int32_t piece = 0, npmax = 1, qcols = 0, nqt = 0, ns = 1, nsmax = 1;
   int64_t wgs = 0, slots = 0;  // workgroups; columns of partial results
   size_t ml = 0, total = 0;
 };
@@ -102,7 +102,8 @@ bool attend_cut(const vc_decode_shape *s, int32_t n, int32_t max_rows, Cut &c) {
     if (tiles >= kMaxWg) return false;
     const int64_t resident = c.qcols == 256 ? 256 : 512;
     c.nqt = (int32_t)nqt;
-    c.ns = (int32_t)std::max<int64_t>(1, std::min<int64_t>(resident / tiles, nt / 4));
+    c.nsmax = (int32_t)std::max<int64_t>(1, nt / 4);
+    c.ns = (int32_t)std::max<int64_t>(1, std::min<int64_t>(resident / tiles, c.nsmax));
     c.wgs = tiles * c.ns;
     c.slots = c.ns > 1 ? c.wgs * c.qcols : 0;
   }
@@ -202,7 +203,7 @@ vc_status viscache_q8_attend(const vc_decode_shape *s, const vc_q8cache *c, cons
   p.q = desc(q);
   p.out = desc(out);
   p.count = count;
-  p.B = s->B; p.Hq = s->Hq; p.Hkv = s->Hkv; p.G = s->Hq / s->Hkv; p.d = s->d;
+  p.L = s->L; p.B = s->B; p.Hq = s->Hq; p.Hkv = s->Hkv; p.G = s->Hq / s->Hkv; p.d = s->d;
   p.units = s->L * s->B * s->Hkv;
   p.n = n;
   p.cols = n * p.G;
@@ -210,8 +211,9 @@ vc_status viscache_q8_attend(const vc_decode_shape *s, const vc_q8cache *c, cons
   p.fp32 = out_fp32;
   p.max_rows = max_rows;
   p.sc = scale * 1.4426950408889634f;
+  p.wgs = (int32_t)cut.wgs;
   p.piece = cut.piece; p.npmax = cut.npmax;
-  p.qcols = cut.qcols; p.nqt = cut.nqt; p.ns = cut.ns;
+  p.qcols = cut.qcols; p.nqt = cut.nqt; p.ns = cut.ns; p.nsmax = cut.nsmax;
   uint8_t *ws = static_cast<uint8_t *>(workspace);
   p.part_o = reinterpret_cast<float *>(ws);
   p.part_ml = reinterpret_cast<float2 *>(ws + cut.ml);

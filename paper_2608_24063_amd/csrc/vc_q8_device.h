@@ -110,4 +110,62 @@ __device__ __forceinline__ int64_t unit_base(const RowsDesc &r, const int64_t *u
   return (int64_t)(lb / B) * r.layer + (int64_t)(lb % B) * r.seq + (int64_t)g * r.head;
 }
 
+// Which column tile and key split a prompt's workgroup takes, and where the
+// partial results of a tile's splits begin.
+struct Share {
+  int u, qt, sp, ns;  // unit (-1: nothing to do), tile, split of ns
+};
+
+// Column tiles of sequence b.
+__device__ __forceinline__ int tiles_of(const Q8Attn &p, int b) {
+  const int cnt = p.count ? min(max(ldg(p.count + b), 0), p.n) : p.n;
+  return (cnt * p.G + p.qcols - 1) / p.qcols;
+}
+
+// Tiles of all sequences of a layer and head, and of those before sequence
+// `b`; every lane of the wave takes part.
+__device__ __forceinline__ int2 count_tiles(const Q8Attn &p, int b, int lane) {
+  int all = 0, before = 0;
+  for (int b0 = 0; b0 < p.B; b0 += 64) {
+    const int q = b0 + lane < p.B ? tiles_of(p, b0 + lane) : 0;
+    all += __builtin_amdgcn_readlane((int)wave_incl_scan((uint32_t)q), 63);
+    before += __builtin_amdgcn_readlane((int)wave_incl_scan((uint32_t)(b0 + lane < b ? q : 0)), 63);
+  }
+  return make_int2(all, before);
+}
+// Key splits where `all` tiles a layer and head are not empty.
+__device__ __forceinline__ int splits_of(const Q8Attn &p, int all, uint32_t wgs) {
+  const int64_t live = (int64_t)all * p.L * p.Hkv;
+  return (int)min(max((int64_t)wgs / max(live, (int64_t)1), (int64_t)1), (int64_t)p.nsmax);
+}
+
+// Workgroup `id` of `wgs`: tiles in the order of their units, splits innermost.
+// With counts, the empty tiles' workgroups go to the others as further splits.
+__device__ __forceinline__ Share share_of(const Q8Attn &p, uint32_t id, uint32_t wgs, int lane) {
+  if (!p.count || p.ns == 1) {
+    const uint32_t per = (uint32_t)(p.nqt * p.ns), rest = id % per;
+    return Share{(int)(id / per), (int)(rest / (uint32_t)p.ns), (int)(rest % (uint32_t)p.ns), p.ns};
+  }
+  const int all = count_tiles(p, 0, lane).x;
+  const int ns = splits_of(p, all, wgs);
+  const int tile = (int)(id / (uint32_t)ns), per = all * p.Hkv;
+  Share s{-1, 0, (int)(id % (uint32_t)ns), ns};
+  if (per == 0 || tile >= per * p.L) return s;
+  const int l = tile / per, r = tile % per, x = r / p.Hkv;  // x: which of the sequences' tiles
+  int base = 0;
+  for (int b0 = 0; b0 < p.B; b0 += 64) {
+    const int q = b0 + lane < p.B ? tiles_of(p, b0 + lane) : 0;
+    const int inc = (int)wave_incl_scan((uint32_t)q), a = base + inc - q;
+    const uint64_t hit = __builtin_amdgcn_ballot_w64(a <= x && x < a + q);
+    if (hit) {
+      const int src = __builtin_ctzll(hit);
+      const int qb = __builtin_amdgcn_readlane(q, src), rr = r - p.Hkv * __builtin_amdgcn_readlane(a, src);
+      s.u = (l * p.B + b0 + src) * p.Hkv + rr / qb;
+      s.qt = rr % qb;
+    }
+    base += __builtin_amdgcn_readlane(inc, 63);
+  }
+  return s;
+}
+
 }  // namespace vc
