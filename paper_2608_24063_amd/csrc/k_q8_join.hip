@@ -2,12 +2,12 @@
 // over the 8-bit cache leaves for a column whose rows went to several
 // workgroups.
 //
-// Bound by latency: a workgroup takes one column and deals its parts to groups
-// of D / 4 threads, four parts in flight each, so that a unit cut into many
-// parts costs few round trips.  A launch of its own costs less than the last
-// workgroup's joining them in the attention's launch did: there the partials
-// need device-coherent stores, a wait for them and an atomic, and one workgroup
-// joins a whole unit (4 units of 12544 rows: 18.5 us in one launch).
+// Bound by latency: a column's parts are dealt to groups of D / 4 lanes, four
+// parts in flight each, so that a unit cut into many parts costs few round
+// trips.  A launch of its own costs less than the last workgroup's joining them
+// in the attention's launch did: there the partials need device-coherent
+// stores, a wait for them and an atomic, and one workgroup joins a whole unit
+// (4 units of 12544 rows: 18.5 us in one launch, 13.0 in two).
 #include "vc_q8_device.h"
 
 namespace vc {
@@ -16,24 +16,41 @@ namespace {
 
 constexpr float kNegInf = -__builtin_inff();
 
-template <int D>
+struct Part {
+  float M, l, o[4];
+};
+
+// b into a.
+__device__ __forceinline__ void add(Part &a, const Part &b) {
+  const float M = fmaxf(a.M, b.M);
+  if (M == kNegInf) return;
+  const float fa = fast_exp2(a.M - M), fb = fast_exp2(b.M - M);
+  a.M = M;
+  a.l = fa * a.l + fb * b.l;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) a.o[i] = fa * a.o[i] + fb * b.o[i];
+}
+
+// WPC waves take a column: four where columns are few and parts many, one
+// where the columns fill the chip.
+template <int D, bool HALF, int WPC>
 __global__ __launch_bounds__(256) void k_join(Q8Attn p) {
-  constexpr int TPG = D / 4, NG = 256 / TPG, U = 4;
-  __shared__ float so[NG][D + 4];
-  __shared__ float2 sml[NG];
-  const int u = (int)(blockIdx.x / (uint32_t)p.cols), col = (int)(blockIdx.x % (uint32_t)p.cols);
-  const int tid = threadIdx.x, grp = tid / TPG, ch = tid % TPG * 4;
+  constexpr int TPG = D / 4, GPW = 64 / TPG, NG = GPW * WPC, U = 4;
+  __shared__ Part sp[WPC][TPG];
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t cg = (int64_t)blockIdx.x * (4 / WPC) + w / WPC;
+  const int u = (int)min(cg / p.cols, (int64_t)p.units - 1), col = (int)(cg % p.cols);
+  const int grp = w % WPC * GPW + lane / TPG, ch = lane % TPG * 4;
   const int g = u % p.Hkv, lb = u / p.Hkv, b = lb % p.B;
-  const int len_ = ldg(p.c.len + u), cap_ = ldg(p.c.cap + u), cnt_ = p.count ? ldg(p.count + b) : p.n;
+  const int cnt_ = p.count ? ldg(p.count + b) : p.n;
   int2 tiles = make_int2(0, 0);
-  if (p.npmax == 1 && p.count) tiles = count_tiles(p, b, tid & 63);
-  if (col >= min(max(cnt_, 0), p.n) * p.G) return;
+  if (p.npmax == 1 && p.count) tiles = count_tiles(p, b, lane);
+  if (cg >= (int64_t)p.units * p.cols || col >= min(max(cnt_, 0), p.n) * p.G) return;
   int64_t at;  // part 0 of the column
   int ns;
   if (p.npmax > 1) {  // pieces: as many as the unit's rows make; a single one wrote its output
-    const int rows = min(max(min(len_, cap_), 0), p.max_rows);
+    const int rows = min(max(min(ldg(p.c.len + u), ldg(p.c.cap + u)), 0), p.max_rows);
     ns = ((rows + kQ8Block - 1) / kQ8Block + p.piece - 1) / p.piece;
-    if (ns <= 1) return;
     at = (int64_t)u * p.npmax * p.qcols + col;
   } else {
     int64_t tile = (int64_t)u * p.nqt;
@@ -42,74 +59,95 @@ __global__ __launch_bounds__(256) void k_join(Q8Attn p) {
       ns = splits_of(p, tiles.x, (uint32_t)p.wgs);
       tile = ((int64_t)(lb / p.B) * tiles.x + tiles.y) * p.Hkv + (int64_t)g * tiles_of(p, b);
     }
-    if (ns == 1) return;  // written already
     at = (tile + col / p.qcols) * ns * p.qcols + col % p.qcols;
   }
-  float M = kNegInf, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+  if (ns <= 1) return;  // written already
+  Part t{kNegInf, 0.f, {0.f, 0.f, 0.f, 0.f}};
   for (int s0 = grp; s0 < ns; s0 += NG * U) {
     float2 ml[U];
-    u32x4 x[U];
+    float x[U][4];
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       const int64_t a = at + (int64_t)min(s0 + k * NG, ns - 1) * p.qcols;
       ml[k] = ldg(p.part_ml + a);
-      x[k] = ld16(p.part_o + a * D + ch);
+      if (HALF) {
+        const f16x4 h = __builtin_bit_cast(f16x4, ld8(reinterpret_cast<const _Float16 *>(p.part_o) + a * D + ch));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[k][i] = (float)h[i];
+      } else {
+        const u32x4 v = ld16(p.part_o + a * D + ch);
+        x[k][0] = __uint_as_float(v.x);
+        x[k][1] = __uint_as_float(v.y);
+        x[k][2] = __uint_as_float(v.z);
+        x[k][3] = __uint_as_float(v.w);
+      }
     }
-    float Mc = M;
+    float M = t.M;
 #pragma unroll
     for (int k = 0; k < U; ++k)
-      if (s0 + k * NG < ns) Mc = fmaxf(Mc, ml[k].x);
-    if (Mc == kNegInf) continue;
-    const float f0 = fast_exp2(M - Mc);
-    l *= f0;
+      if (s0 + k * NG < ns) M = fmaxf(M, ml[k].x);
+    if (M == kNegInf) continue;
+    const float f0 = fast_exp2(t.M - M);
+    t.M = M;
+    t.l *= f0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] *= f0;
-    M = Mc;
+    for (int i = 0; i < 4; ++i) t.o[i] *= f0;
 #pragma unroll
     for (int k = 0; k < U; ++k) {
-      if (s0 + k * NG >= ns) continue;
-      const float f = fast_exp2(ml[k].x - Mc);
-      l += f * ml[k].y;
-      o[0] += f * __uint_as_float(x[k].x);
-      o[1] += f * __uint_as_float(x[k].y);
-      o[2] += f * __uint_as_float(x[k].z);
-      o[3] += f * __uint_as_float(x[k].w);
+      const float f = s0 + k * NG < ns ? fast_exp2(ml[k].x - M) : 0.f;
+      t.l += f * ml[k].y;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) t.o[i] += f * x[k][i];
     }
   }
+  // The groups of a wave, then the waves.
 #pragma unroll
-  for (int i = 0; i < 4; ++i) so[grp][ch + i] = o[i];
-  if (ch == 0) sml[grp] = make_float2(M, l);
-  __syncthreads();
-  if (tid >= D) return;
-  float Mt = kNegInf;
+  for (int d = TPG; d < 64; d *= 2) {
+    Part y;
+    y.M = shfl_xor(t.M, d);
+    y.l = shfl_xor(t.l, d);
 #pragma unroll
-  for (int k = 0; k < NG; ++k) Mt = fmaxf(Mt, sml[k].x);
-  float ot = 0.f, lt = 0.f;
-  if (Mt != kNegInf) {
-#pragma unroll
-    for (int k = 0; k < NG; ++k) {
-      const float f = fast_exp2(sml[k].x - Mt);
-      ot += f * so[k][tid];
-      lt += f * sml[k].y;
-    }
+    for (int i = 0; i < 4; ++i) y.o[i] = shfl_xor(t.o[i], d);
+    add(t, y);
   }
-  const float v = lt > 0.f ? ot / lt : 0.f;
+  if (WPC > 1) {
+    if (lane < TPG) sp[w][lane] = t;
+    __syncthreads();
+    if (w > 0) return;
+#pragma unroll
+    for (int k = 1; k < WPC; ++k) add(t, sp[k][lane % TPG]);
+  }
+  if (lane >= TPG) return;
+  const float inv = t.l > 0.f ? 1.f / t.l : 0.f;
   const int64_t to = (int64_t)(lb / p.B) * p.out.layer + (int64_t)b * p.out.seq + (int64_t)(col / p.G) * p.out.token +
-                     (int64_t)(g * p.G + col % p.G) * p.out.head + tid;
+                     (int64_t)(g * p.G + col % p.G) * p.out.head + ch;
+  const float v[4] = {t.o[0] * inv, t.o[1] * inv, t.o[2] * inv, t.o[3] * inv};
   if (p.fp32)
-    stg(reinterpret_cast<float *>(p.out.base) + to, v);
+    st16(reinterpret_cast<float *>(p.out.base) + to,
+         u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
   else
-    stg(reinterpret_cast<uint16_t *>(p.out.base) + to, (uint16_t)pack_bf16(v, 0.f));
+    st8(reinterpret_cast<uint16_t *>(p.out.base) + to, u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])});
+}
+
+template <int D, bool HALF>
+void launch(const Q8Attn &p, hipStream_t st) {
+  const int64_t cols = (int64_t)p.units * p.cols;
+  // 1024 columns and more are a wave each: 5460 columns of 12 parts 13.2 us in
+  // four waves, see below in one; 28 columns of 49 to 125 parts need the four.
+  if (cols >= 1024)
+    hipLaunchKernelGGL((k_join<D, HALF, 1>), dim3((uint32_t)((cols + 3) / 4)), dim3(256), 0, st, p);
+  else
+    hipLaunchKernelGGL((k_join<D, HALF, 4>), dim3((uint32_t)cols), dim3(256), 0, st, p);
 }
 
 }  // namespace
 
 hipError_t launch_q8_join(const Q8Attn &p, hipStream_t st) {
-  const dim3 grid((uint32_t)((int64_t)p.units * p.cols)), block(256);
+  const bool half = p.npmax == 1 && !p.fp32;  // a prompt's parts of bf16 outputs
   if (p.d == 128)
-    hipLaunchKernelGGL((k_join<128>), grid, block, 0, st, p);
+    half ? launch<128, true>(p, st) : launch<128, false>(p, st);
   else
-    hipLaunchKernelGGL((k_join<64>), grid, block, 0, st, p);
+    half ? launch<64, true>(p, st) : launch<64, false>(p, st);
   return hipGetLastError();
 }
 

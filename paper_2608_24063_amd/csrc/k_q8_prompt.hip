@@ -380,13 +380,38 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt8(Q8Attn p) {
     return;
   }
   const int64_t at = (int64_t)id * p.qcols + 32 * w + ln;
+  if (F32) {
 #pragma unroll
-  for (int cb = 0; cb < CB; ++cb)
+    for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      st16(p.part_o + at * D + 32 * cb + 8 * i + 4 * hf,
-           u32x4{__float_as_uint(O[cb][4 * i]), __float_as_uint(O[cb][4 * i + 1]), __float_as_uint(O[cb][4 * i + 2]),
-                 __float_as_uint(O[cb][4 * i + 3])});
+      for (int i = 0; i < 4; ++i)
+        st16(p.part_o + at * D + 32 * cb + 8 * i + 4 * hf,
+             u32x4{__float_as_uint(O[cb][4 * i]), __float_as_uint(O[cb][4 * i + 1]), __float_as_uint(O[cb][4 * i + 2]),
+                   __float_as_uint(O[cb][4 * i + 3])});
+  } else {
+    // Half the traffic: fp16 (2^-12 of the value), the column's largest brought
+    // to [2^14, 2^15) by a power of two 2^-k; (m, l) become (m + k, l 2^-k), so
+    // that the parts still join by 2^m.
+    float big = 0.f;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) big = fmaxf(big, fabsf(O[cb][i]));
+    big = max_halves(big);
+    const int k = big > 0.f ? (int)(__float_as_uint(big) >> 23) - 127 - 14 : 0;
+    const float down = ldexpf(1.f, -k);
+    m += (float)k;
+    l *= down;
+    _Float16 *to = reinterpret_cast<_Float16 *>(p.part_o) + at * D;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f16x4 h = {(_Float16)(O[cb][4 * i] * down), (_Float16)(O[cb][4 * i + 1] * down),
+                         (_Float16)(O[cb][4 * i + 2] * down), (_Float16)(O[cb][4 * i + 3] * down)};
+        st8(to + 32 * cb + 8 * i + 4 * hf, __builtin_bit_cast(u32x2, h));
+      }
+  }
   if (hf == 0) stg(p.part_ml + at, make_float2(m, l));
 }
 

@@ -83,15 +83,17 @@ bool attend_cut(const vc_decode_shape *s, int32_t n, int32_t max_rows, Cut &c) {
   if (cols > (int64_t(1) << 24)) return false;
   const int64_t nt = std::max<int64_t>(1, ((int64_t)max_rows + kQ8Block - 1) / kQ8Block);
   if (cols <= kCols) {
-    // One workgroup a unit where there are enough units for the 256 CUs; fewer
-    // units are cut into pieces of a multiple of four blocks (one per wave and
-    // turn), as many as make about 256 workgroups.  (us: 4 units of 12544 rows
-    // in pieces of 4, 8, 16, 48 blocks 13.0, 13.3, 15.7, 26.1; 32 of 2300 to 5800
-    // rows in 4, 8, 12, 24: 21.1, 19.2, 16.4, 19.7; 896 of them in 24, 48 and
-    // uncut 199, 198, 188.)
+    // Units are cut into pieces of a multiple of four blocks (one per wave and
+    // turn), as many as make about 256 workgroups, one a CU, and not where that
+    // were two a unit.  (us: 4 units of 12544 rows in pieces of 4, 8, 16, 48 blocks
+    // 12.4, 13.3, 15.7, 26.1; 32 of 2300 to 5800 rows in 4, 8, 12, 24: 21.1, 19.2,
+    // 16.4, 19.7; 112 of 620 to 1490 in 12 and uncut 17.1, 16.2; 160 of 800 to
+    // 1900 in 20 and uncut 19.7, 18.5; 896 of 2300 to 5800 in 24, 48 and uncut
+    // 199, 198, 188.)
     const int64_t want = units * nt / 256;
     c.qcols = kCols;
     c.piece = (int32_t)std::min<int64_t>(std::max<int64_t>(4, (want + 3) / 4 * 4), int64_t(1) << 26);
+    if (nt <= 2 * (int64_t)c.piece) c.piece = (int32_t)nt;
     c.npmax = (int32_t)((nt + c.piece - 1) / c.piece);
     c.wgs = units * c.npmax;
     c.slots = c.npmax > 1 ? c.wgs * kCols : 0;
