@@ -553,6 +553,20 @@ vc_status viscache_rope(const vc_decode_shape *shape, const vc_rope *rope, int32
                         const int32_t *count, const vc_rows *q_in, const vc_rows *q_out, const vc_rows *k_in,
                         const vc_rows *k_out, void *stream);
 
+/* Device, asynchronous.  One token's step of every sequence and layer, with the
+ * result of viscache_rope on q and k (rope not NULL: bf16, pos DEVICE int32
+ * [3][B]), viscache_q8_append of k and v and viscache_q8_attend of q (n = 1),
+ * bit for bit, in one launch, or two where few units are cut along their rows.
+ * q, k and v (their token strides are not read) are left as they are.  Where a
+ * unit is full its row is not appended and not attended.  max_rows bounds every len after the
+ * append, workspace and errors as for viscache_q8_attend with n = 1;
+ * VC_ERR_ARG also for bad k or v, rope->fp32, a rope that viscache_rope
+ * refuses, and a rope without pos. */
+vc_status viscache_q8_step(const vc_decode_shape *shape, const vc_q8cache *cache, const vc_rope *rope,
+                           const int32_t *pos, const vc_rows *q, const vc_rows *k, const vc_rows *v,
+                           const vc_rows *out, int32_t out_fp32, float scale, int32_t max_rows, void *workspace,
+                           size_t workspace_bytes, void *stream);
+
 /* Static text for a status code. */
 const char *viscache_strerror(vc_status s);
 

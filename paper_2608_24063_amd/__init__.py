@@ -126,6 +126,8 @@ def lib() -> ctypes.CDLL:
         L.viscache_q8_attend_workspace_bytes.restype = ctypes.c_size_t
         L.viscache_q8_attend.argtypes = [c_vp, c_vp, c_vp, c_vp, c_i32, c_vp, c_i32, c_i32, c_f32, c_i32, c_vp,
                                          ctypes.c_size_t, c_vp]
+        L.viscache_q8_step.argtypes = [c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_i32, c_f32, c_i32, c_vp,
+                                       ctypes.c_size_t, c_vp]
         L.viscache_rope.argtypes = [c_vp, c_vp, c_i32, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp]
         L.viscache_strerror.argtypes = [c_i32]
         L.viscache_strerror.restype = ctypes.c_char_p
@@ -134,7 +136,7 @@ def lib() -> ctypes.CDLL:
                      "viscache_append_kv", "viscache_decode_attn", "viscache_decode_step",
                      "viscache_decode_step_q4", "viscache_decode_step_noalloc", "viscache_decode_plan",
                      "viscache_decode_step_planned", "viscache_quantize_rows", "viscache_q8_append",
-                     "viscache_q8_read", "viscache_q8_attend", "viscache_rope"):
+                     "viscache_q8_read", "viscache_q8_attend", "viscache_q8_step", "viscache_rope"):
             getattr(L, name).restype = c_i32
         _lib = L
     return _lib
@@ -369,6 +371,15 @@ def viscache_rope(shape: vc_decode_shape, rope: vc_rope, n: int, pos: int, count
     _check(st, "viscache_rope")
 
 
+def viscache_q8_step(shape: vc_decode_shape, cache: vc_q8cache, rope, pos: int, q: vc_rows, k: vc_rows, v: vc_rows,
+                     out: vc_rows, out_fp32: int, scale: float, max_rows: int, workspace: int, workspace_bytes: int,
+                     stream: int) -> None:
+    """rope: vc_rope or None."""
+    st = lib().viscache_q8_step(_ref(shape), _ref(cache), _ref(rope), pos, _ref(q), _ref(k), _ref(v), _ref(out),
+                                out_fp32, scale, max_rows, workspace, workspace_bytes, stream)
+    _check(st, "viscache_q8_step")
+
+
 def viscache_strerror(status: int) -> str:
     return strerror(status)
 
@@ -380,4 +391,4 @@ EXPORTED = ("viscache_default_params", "viscache_budget", "viscache_out_rows",
             "viscache_decode_step", "viscache_decode_step_q4", "viscache_decode_step_noalloc",
             "viscache_decode_plan_bytes", "viscache_decode_plan", "viscache_decode_step_planned",
             "viscache_quantize_rows", "viscache_q8_append", "viscache_q8_read",
-            "viscache_q8_attend_workspace_bytes", "viscache_q8_attend", "viscache_rope", "viscache_strerror")
+            "viscache_q8_attend_workspace_bytes", "viscache_q8_attend", "viscache_rope", "viscache_q8_step", "viscache_strerror")

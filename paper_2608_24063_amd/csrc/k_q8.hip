@@ -9,9 +9,7 @@
 // transposition is paid once, here.
 //
 // Bound by memory: 2 bytes a value in, 1 out.  A workgroup takes a block's
-// keys with one half of its waves and its values with the other; each half
-// holds its 64 rows in registers between the search for the maximum and the
-// rounding, so the rows are read once.
+// keys with one half of its waves and its values with the other.
 #include "vc_q8_device.h"
 
 namespace vc {
@@ -21,32 +19,14 @@ namespace {
 constexpr int kThreads = 512;  // 256 for keys, 256 for values
 constexpr int kHalf = 256;
 
-template <int D>
-struct WriteSmem {
-  static constexpr int VP = D + 8;  // pitch of the value codes' rows, bytes
-  uint8_t v[kQ8Block * VP] __attribute__((aligned(16)));
-  uint32_t red[2][4];
-};
-
-// Largest over a half's four waves of per-thread packed magnitudes; one
-// barrier (the next use of `red` must come after another one).
-__device__ __forceinline__ uint32_t half_max(uint32_t (&red)[2][4], uint32_t m, int side, int tid) {
-  uint32_t x = max(m & 0xFFFFu, m >> 16);
-#pragma unroll
-  for (int k = 32; k >= 1; k >>= 1) x = max(x, (uint32_t)__shfl_xor((int)x, k, 64));
-  if ((tid & 63) == 0) red[side][(tid >> 6) & 3] = x;
-  __syncthreads();
-  return max(max(red[side][0], red[side][1]), max(red[side][2], red[side][3]));
-}
-
 // Workgroup j of a unit's nj seals blocks j, j + nj, ... of those its new rows
 // fill; workgroup 0 also takes an open last block, since that goes over the
 // tail rows the first block is made of.
 template <int D, int FMT>
 __global__ __launch_bounds__(kThreads) void k_append_rows(Q8Rows p) {
-  __shared__ WriteSmem<D> sm;
+  __shared__ uint8_t lds[kQ8Block * (D + 8)] __attribute__((aligned(16)));
+  __shared__ uint32_t red[2][4];
   constexpr int CPR = D / 16;                     // 16-channel chunks per row
-  constexpr int IT = kQ8Block * CPR / kHalf;      // chunks per thread (2 or 1)
   const int u = (int)(blockIdx.x / (uint32_t)p.nj), j = (int)(blockIdx.x % (uint32_t)p.nj);
   const int side = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 8), tid = threadIdx.x & 255;
   const int len0 = max(ldg(p.c.len + u), 0), cap = ldg(p.c.cap + u);
@@ -67,64 +47,10 @@ __global__ __launch_bounds__(kThreads) void k_append_rows(Q8Rows p) {
   auto seal = [&](int jb) {
     const int lo = jb == 0 ? len0 % kQ8Block : 0;
     const int64_t r0 = (int64_t)(b0 + jb) * kQ8Block - len0;  // new row of the block's row 0
-    u32x4 x[IT][2];
-    uint32_t mag = 0u;
-#pragma unroll
-    for (int it = 0; it < IT; ++it) {
-      const int e = tid + kHalf * it, row = e / CPR, c = e % CPR;
-      const uint16_t *s = row < lo ? tail + row * D : src + (r0 + row) * rd.token;
-      x[it][0] = ld16(s + 16 * c);
-      x[it][1] = ld16(s + 16 * c + 8);
-    }
-#pragma unroll
-    for (int it = 0; it < IT; ++it)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        mag = max_mag(max_mag(mag, x[it][h].x), x[it][h].y);
-        mag = max_mag(max_mag(mag, x[it][h].z), x[it][h].w);
-      }
-    const float top = __uint_as_float(half_max(sm.red, mag, side, tid) << 16);
-    const float eff = fminf(fmaxf(top, Q8<FMT>::kEffMin), Q8<FMT>::kEffMax);
-    const float inv = __fdiv_rn(Q8<FMT>::kTop, eff);
-    if (tid == 0) stg(scales + blk0 + jb, __fdiv_rn(eff, Q8<FMT>::kTop));
-    uint8_t *dst = (side ? p.c.vc : p.c.kc) + (blk0 + jb) * (kQ8Block * D);
-#pragma unroll
-    for (int it = 0; it < IT; ++it) {
-      const int e = tid + kHalf * it, row = e / CPR, c = e % CPR;
-      uint32_t o[4];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint32_t ws[4] = {x[it][h].x, x[it][h].y, x[it][h].z, x[it][h].w};
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-          o[2 * h + k] = Q8<FMT>::pack4(
-              Q8<FMT>::code_value(bf16_lo(ws[2 * k]), inv), Q8<FMT>::code_value(bf16_hi(ws[2 * k]), inv),
-              Q8<FMT>::code_value(bf16_lo(ws[2 * k + 1]), inv), Q8<FMT>::code_value(bf16_hi(ws[2 * k + 1]), inv));
-      }
-      if (side == 0) {
-        st16(dst + row * D + 16 * c, u32x4{o[0], o[1], o[2], o[3]});
-      } else {
-        u32x2 *t = reinterpret_cast<u32x2 *>(sm.v + row * WriteSmem<D>::VP + 16 * c);
-        t[0] = u32x2{o[0], o[1]};
-        t[1] = u32x2{o[2], o[3]};
-      }
-    }
-    __syncthreads();
-    if (side == 1) {
-      // Thread: channels 4 cq .. 4 cq + 3, rows 8 rg .. 8 rg + 7.
-      const int rg = tid % 8;
-#pragma unroll
-      for (int cq = tid / 8; cq < D / 4; cq += kHalf / 8) {
-        uint32_t w[8];
-#pragma unroll
-        for (int r = 0; r < 8; ++r)
-          w[r] = *reinterpret_cast<const uint32_t *>(sm.v + (8 * rg + r) * WriteSmem<D>::VP + 4 * cq);
-        const u32x4 a = transpose4(w[0], w[1], w[2], w[3]), b = transpose4(w[4], w[5], w[6], w[7]);
-        const uint32_t as[4] = {a.x, a.y, a.z, a.w}, bs[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) st8(dst + (4 * cq + k) * kQ8Block + 8 * rg, u32x2{as[k], bs[k]});
-      }
-    }
+    seal_block<D, FMT>(
+        red[side], lds, tid, side == 1,
+        [&](int row, int c) { return ld16((row < lo ? tail + row * D : src + (r0 + row) * rd.token) + 8 * c); },
+        (side ? p.c.vc : p.c.kc) + (blk0 + jb) * (kQ8Block * D), scales + blk0 + jb);
   };
   // Rows lo .. hi - 1 of open block jb into the tail.
   auto leave_open = [&](int jb) {
@@ -140,7 +66,7 @@ __global__ __launch_bounds__(kThreads) void k_append_rows(Q8Rows p) {
       mag = max_mag(max_mag(max_mag(max_mag(mag, a.x), a.y), a.z), a.w);
       mag = max_mag(max_mag(max_mag(max_mag(mag, b.x), b.y), b.z), b.w);
     }
-    const float s = open_scale(half_max(sm.red, mag, side, tid));
+    const float s = open_scale(max_of_256(red[side], mag, tid));
     if (tid == 0) stg(scales + blk0 + jb, lo > 0 ? fmaxf(s, ldg(scales + blk0 + jb)) : s);
   };
   for (int jb = j; jb < nfull; jb += p.nj) seal(jb);
@@ -159,10 +85,13 @@ __global__ __launch_bounds__(256) void k_append_len(Q8Rows p) {
   if (m > 0) stg(p.c.len + u, len0 + m);
 }
 
-// 16 bytes of a row: 4 fp32 or 8 bf16 values.
+// 16 bytes of a row: 4 fp32 or 8 bf16 values.  (Streamed: reading back 3.6 M
+// rows in fp32 and writing them before 1432 -> 1390 us, 118000 in bf16 50 -> 43; the
+// codes that an append writes are read soon, and streaming them cost the
+// smaller case 5 us.)
 template <bool F32>
 __device__ __forceinline__ void put16(char *dst, const float (&f)[8]) {
-  st16(dst, F32 ? u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])}
+  st16_stream(dst, F32 ? u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])}
                 : u32x4{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])});
 }
 

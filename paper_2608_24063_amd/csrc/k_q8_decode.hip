@@ -17,6 +17,10 @@
 // their power of two and their values transposed through LDS; they are
 // requested with the first block, since the whole kernel waits for them (read
 // by one wave after its own blocks they took 8 of 25 us).
+//
+// A step is one launch: every workgroup turns its unit's queries itself while
+// its first blocks are on their way, and the one with the unit's last rows
+// appends the new one, sealing the block that it completes first.
 #include "vc_q8_device.h"
 
 namespace vc {
@@ -60,6 +64,10 @@ struct Smem {
   // The open block's values (16 rows a wave), then the waves' O.
   uint8_t buf[kO > kT ? kO : kT] __attribute__((aligned(16)));
   float2 ml[kWaves][16];
+  // A step's rows: the query heads, the new key (16) and value (17).
+  uint16_t rows[18][D + 8] __attribute__((aligned(16)));
+  float2 cs[kRopeMaxHalf];
+  uint32_t red[4];
 };
 
 // What a wave carries over its blocks, per lane: the column's running maximum
@@ -128,9 +136,48 @@ __device__ __forceinline__ void put(const Q8Attn &p, int64_t at, float v) {
     stg(reinterpret_cast<uint16_t *>(p.out.base) + at, (uint16_t)pack_bf16(v, 0.f));
 }
 
+// The query heads of the unit (rows 0 .. G - 1), the new key (16) and the new
+// value (17) into LDS, queries and key turned to their position; two barriers.
+template <int D>
+__device__ __forceinline__ void step_rows(const Q8Attn &p, Smem<D> &sm, int u, int tid) {
+  const int g = u % p.Hkv, lb = u / p.Hkv, b = lb % p.B, l = lb / p.B;
+  for (int e = tid; e < (p.G + 2) * (D / 8); e += 256) {
+    const int r = e / (D / 8), c = e % (D / 8);
+    const RowsDesc &d = r < p.G ? p.q : r == p.G ? p.k : p.v;
+    const int64_t at = (int64_t)l * d.layer + (int64_t)b * d.seq + (int64_t)(r < p.G ? g * p.G + r : g) * d.head;
+    *reinterpret_cast<u32x4 *>(&sm.rows[r < p.G ? r : 16 + r - p.G][8 * c]) =
+        ld16(reinterpret_cast<const uint16_t *>(d.base) + at + 8 * c);
+  }
+  const int half = p.rope.rot / 2;
+  if (tid < half) sm.cs[tid] = turn_of(p.rope, tid, ldg(p.pos + (int64_t)axis_of(p.rope, tid) * p.B + b));
+  __syncthreads();
+  for (int e = tid; e < (p.G + 1) * half; e += 256) {
+    const int r = e / half, i = e % half;
+    uint16_t *row = sm.rows[r < p.G ? r : 16];
+    uint16_t *x1 = row + (p.rope.adjacent ? 2 * i : i), *x2 = row + (p.rope.adjacent ? 2 * i + 1 : i + half);
+    float a = __uint_as_float((uint32_t)*x1 << 16), c = __uint_as_float((uint32_t)*x2 << 16);
+    turn(a, c, sm.cs[i]);
+    *x1 = (uint16_t)pack_bf16(a, 0.f);
+    *x2 = (uint16_t)pack_bf16(c, 0.f);
+  }
+  if (half > 0) __syncthreads();
+}
+
+// The open block's scale once `row` is its row `slot`.
+template <int D>
+__device__ __forceinline__ float grown_scale(const uint16_t *row, int slot, float before, int lane) {
+  uint32_t m = 0u;
+  if (lane < D / 2) m = max_mag(0u, reinterpret_cast<const uint32_t *>(row)[lane]);
+  uint32_t x = max(m & 0xFFFFu, m >> 16);
+#pragma unroll
+  for (int k = 32; k >= 1; k >>= 1) x = max(x, (uint32_t)__shfl_xor((int)x, k, 64));
+  const float s = open_scale(x);
+  return slot > 0 ? fmaxf(s, before) : s;
+}
+
 // Workgroup (unit, piece): blocks [j piece, (j + 1) piece) of the unit, dealt
 // to the four waves in turn.
-template <int D, int FMT, bool HILO>
+template <int D, int FMT, bool HILO, bool STEP>
 __global__ __launch_bounds__(64 * kWaves, 2) void k_decode8(Q8Attn p) {
   constexpr int MB = D / 16, CH = D / 64;
   __shared__ Smem<D> sm;
@@ -143,7 +190,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_decode8(Q8Attn p) {
   // What the unit is, in one round trip.
   const int len_ = ldg(p.c.len + u), cap_ = ldg(p.c.cap + u), cnt_ = p.count ? ldg(p.count + b) : p.n;
   const int64_t row_off = ldg(p.c.row_off + u);
-  const int len = max(min(len_, cap_), 0), cnt = min(max(cnt_, 0), p.n);
+  const int len0 = max(min(len_, cap_), 0), cnt = min(max(cnt_, 0), p.n);
+  const bool room = STEP && len_ >= 0 && len_ < cap_;  // a step appends a row
+  const int len = len0 + room;
   const int cols = cnt * p.G;
   const int emax = cols > 0 ? min(len, p.max_rows) : 0;  // rows any column sees
   const int nt = (emax + kQ8Block - 1) / kQ8Block;
@@ -156,10 +205,33 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_decode8(Q8Attn p) {
   const int emin = min(lim, p.max_rows);
   const int64_t blk0 = row_off / kQ8Block;
   const int nsealed = len / kQ8Block;
+  // The unit's last piece appends, at `slot` of the open block.
+  const bool mine = room && j == np - 1;
+  const int slot = len0 % kQ8Block;
+  const int64_t tail = (int64_t)u * kQ8Block * D;
+  const bool seals = STEP && mine && slot == kQ8Block - 1;
+  if (seals) {  // the new row completes its block, which is read as codes below
+    step_rows<D>(p, sm, u, tid);
+#pragma unroll 1
+    for (int side = 0; side < 2; ++side) {
+      const uint16_t *from = (side ? p.c.vt : p.c.kt) + tail;
+      const int64_t blk = blk0 + len0 / kQ8Block;
+      seal_block<D, FMT>(
+          sm.red, sm.buf, tid, side == 1,
+          [&](int row, int c) {
+            return row < slot ? ld16(from + row * D + 8 * c)
+                              : *reinterpret_cast<const u32x4 *>(&sm.rows[16 + side][8 * c]);
+          },
+          (side ? p.c.vc : p.c.kc) + blk * (kQ8Block * D), (side ? p.c.vs : p.c.ks) + blk);
+      __threadfence_block();
+      __builtin_amdgcn_s_waitcnt(0);
+      __syncthreads();  // the codes are written, sm.buf and sm.red are free
+    }
+  }
 
   // The query's requests, then the first block's, before anything waits.
   u32x4 qx[CH][2];
-  {
+  if (!STEP) {
     const uint16_t *qp = reinterpret_cast<const uint16_t *>(p.q.base) + out_row(p, p.q, u, min(lr, cols - 1));
 #pragma unroll
     for (int h = 0; h < CH; ++h)
@@ -203,7 +275,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_decode8(Q8Attn p) {
   u32x4 ok[CH][2], ov[VT];
   float kse = 1.f, vse = 1.f;
   if (open) {
-    const int64_t tail = (int64_t)u * kQ8Block * D;
     const uint16_t *kt = p.c.kt + tail + min(16 * w + lr, orows - 1) * D + 16 * lg;
 #pragma unroll
     for (int h = 0; h < CH; ++h)
@@ -213,6 +284,43 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_decode8(Q8Attn p) {
     for (int it = 0; it < VT; ++it) ov[it] = ld16(p.c.vt + tail + 16 * w * D + 8 * (lane + 64 * it));
     kse = ldg(p.c.ks + blk0 + nsealed);
     vse = ldg(p.c.vs + blk0 + nsealed);
+  }
+  if (STEP) {
+    if (!seals) step_rows<D>(p, sm, u, tid);
+    if (mine && !seals) {
+      if (tid < 2 * (D / 8)) {
+        const int side = tid / (D / 8), c = tid % (D / 8);
+        st16((side ? p.c.vt : p.c.kt) + tail + slot * D + 8 * c,
+             *reinterpret_cast<const u32x4 *>(&sm.rows[16 + side][8 * c]));
+      }
+      // The block's scales grow with the row (the same in every wave, whether it
+      // has read them before or after wave 0 wrote them) ...
+      const int64_t blk = blk0 + len0 / kQ8Block;
+      kse = grown_scale<D>(sm.rows[16], slot, ldg(p.c.ks + blk), lane);
+      vse = grown_scale<D>(sm.rows[17], slot, ldg(p.c.vs + blk), lane);
+      if (tid == 0) {
+        stg(p.c.ks + blk, kse);
+        stg(p.c.vs + blk, vse);
+      }
+      // ... and the row itself comes from LDS.
+      if (min(16 * w + lr, orows - 1) == slot) {
+#pragma unroll
+        for (int h = 0; h < CH; ++h)
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+            ok[h][x] = *reinterpret_cast<const u32x4 *>(&sm.rows[16][64 * h + 16 * lg + 8 * x]);
+      }
+#pragma unroll
+      for (int it = 0; it < VT; ++it) {
+        const int e = lane + 64 * it;
+        if (16 * w + e / (D / 8) == slot) ov[it] = *reinterpret_cast<const u32x4 *>(&sm.rows[17][8 * (e % (D / 8))]);
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < CH; ++h)
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        qx[h][k] = *reinterpret_cast<const u32x4 *>(&sm.rows[min(lr, cols - 1)][64 * h + 16 * lg + 8 * k]);
   }
   // The column's query as fp16 operands, scaled by a power of two.
   f16x8 q[CH][2];
@@ -303,6 +411,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_decode8(Q8Attn p) {
   // The waves' states.
   st.l = sum_halves(st.l + swap16(st.l));
   __syncthreads();  // the open block's values are read
+  if (STEP && tid == 0) {
+    // The length: by the join where there is one, since the other pieces read it.
+    if (p.npmax > 1) {
+      if (j == np - 1) stg(p.np + u, np | (int)room << 30);
+    } else if (room) {
+      stg(p.c.len + u, len_ + 1);
+    }
+  }
   float(*wo)[16][D + 4] = reinterpret_cast<float(*)[16][D + 4]>(sm.buf);
 #pragma unroll
   for (int mb = 0; mb < MB; ++mb)
@@ -310,7 +426,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_decode8(Q8Attn p) {
   if (lg == 0) sm.ml[w][lr] = make_float2(st.m, st.l);
   __syncthreads();
   const int x = tid % D;
-  const int64_t slot = (int64_t)u * p.npmax + j;
+  const int64_t part = (int64_t)u * p.npmax + j;
   for (int col = tid / D; col < cols; col += 64 * kWaves / D) {
     float M = kNegInf;
 #pragma unroll
@@ -328,8 +444,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_decode8(Q8Attn p) {
     if (np == 1) {
       put(p, out_row(p, p.out, u, col) + x, s > 0.f ? o / s : 0.f);
     } else {
-      stg(p.part_o + (slot * 16 + col) * D + x, o);
-      if (x == 0) stg(p.part_ml + slot * 16 + col, make_float2(M, s));
+      stg(p.part_o + (part * 16 + col) * D + x, o);
+      if (x == 0) stg(p.part_ml + part * 16 + col, make_float2(M, s));
     }
   }
 }
@@ -337,10 +453,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_decode8(Q8Attn p) {
 template <int D, int FMT>
 hipError_t launch(const Q8Attn &p, hipStream_t st) {
   const dim3 grid((uint32_t)p.wgs), block(64 * kWaves);
-  if (p.fp32)
-    hipLaunchKernelGGL((k_decode8<D, FMT, true>), grid, block, 0, st, p);
-  else
-    hipLaunchKernelGGL((k_decode8<D, FMT, false>), grid, block, 0, st, p);
+  if (p.step) {
+    if (p.fp32)
+      hipLaunchKernelGGL((k_decode8<D, FMT, true, true>), grid, block, 0, st, p);
+    else
+      hipLaunchKernelGGL((k_decode8<D, FMT, false, true>), grid, block, 0, st, p);
+  } else {
+    if (p.fp32)
+      hipLaunchKernelGGL((k_decode8<D, FMT, true, false>), grid, block, 0, st, p);
+    else
+      hipLaunchKernelGGL((k_decode8<D, FMT, false, false>), grid, block, 0, st, p);
+  }
   const hipError_t e = hipGetLastError();
   return e != hipSuccess || p.npmax == 1 ? e : launch_q8_join(p, st);
 }

@@ -7,7 +7,8 @@
 // trips.  A launch of its own costs less than the last workgroup's joining them
 // in the attention's launch did: there the partials need device-coherent
 // stores, a wait for them and an atomic, and one workgroup joins a whole unit
-// (4 units of 12544 rows: 18.5 us in one launch, 13.0 in two).
+// (4 units of 12544 rows: 18.5 us in one launch, 13.0 in two).  After a step it
+// also advances the lengths, which every piece of a unit reads.
 #include "vc_q8_device.h"
 
 namespace vc {
@@ -49,8 +50,14 @@ __global__ __launch_bounds__(256) void k_join(Q8Attn p) {
   int64_t at;  // part 0 of the column
   int ns;
   if (p.npmax > 1) {  // pieces: as many as the unit's rows make; a single one wrote its output
-    const int rows = min(max(min(ldg(p.c.len + u), ldg(p.c.cap + u)), 0), p.max_rows);
-    ns = ((rows + kQ8Block - 1) / kQ8Block + p.piece - 1) / p.piece;
+    if (p.step) {
+      const int v = ldg(p.np + u);
+      ns = v & 0x3FFFFFFF;
+      if (col == 0 && (v >> 30) && lane == 0 && w % WPC == 0) stg(p.c.len + u, ldg(p.c.len + u) + 1);
+    } else {
+      const int rows = min(max(min(ldg(p.c.len + u), ldg(p.c.cap + u)), 0), p.max_rows);
+      ns = ((rows + kQ8Block - 1) / kQ8Block + p.piece - 1) / p.piece;
+    }
     at = (int64_t)u * p.npmax * p.qcols + col;
   } else {
     int64_t tile = (int64_t)u * p.nqt;

@@ -38,6 +38,14 @@ struct Q8Rows {  // append (k, v read) and read back (k, v written)
   int32_t fp32; // read: element type
 };
 
+constexpr int kRopeMaxHalf = 64;
+struct RopeTable {
+  int32_t rot, adjacent;   // rotated channels (0: no rotation); pairs (2i, 2i+1) or (i, i + rot/2)
+  uint64_t axis1, axis2;   // bit i: frequency i turns with the height / the width
+  float scale, sgn;
+  double turns[kRopeMaxHalf];  // frequency i over 2 pi
+};
+
 struct Q8Attn {
   Q8Cache c;
   RowsDesc q, out;
@@ -56,18 +64,23 @@ struct Q8Attn {
   int32_t qcols, nqt, ns, nsmax;
   float *part_o;         // partial results: [part][qcols][d], [part][qcols]
   float2 *part_ml;
+  // A step (step = 1; else attention alone): the new rows, the rotation of queries and
+  // new keys, and, where units are cut, the units' pieces for the join, which
+  // then advances the lengths (bit 30: by a row).
+  int32_t step;
+  RowsDesc k, v;
+  RopeTable rope;
+  const int32_t *pos;    // [3][B]
+  int32_t *np;
 };
 
-constexpr int kRopeMaxHalf = 64;
 struct RopePlan {
   RowsDesc qi, qo, ki, ko;
   const int32_t *pos;    // [3][B][n]
   const int32_t *count;  // tokens per sequence; null: n
   int32_t B, L, Hq, Hkv, d, n;  // Hq (Hkv) is 0 where there are no queries (keys)
-  int32_t rot, adjacent, fp32;
-  uint64_t axis1, axis2;  // bit i: frequency i turns with the height / the width
-  float scale, sgn;
-  double turns[kRopeMaxHalf];  // frequency i over 2 pi
+  int32_t fp32;
+  RopeTable t;
 };
 
 hipError_t launch_q8_append(const Q8Rows &p, int format, hipStream_t st);

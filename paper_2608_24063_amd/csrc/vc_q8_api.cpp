@@ -70,11 +70,11 @@ Q8Cache bind(const vc_q8cache *c) {
 }
 
 // How an attention call is cut, and what it needs of the workspace: partial O,
-// then (max, sum).
+// (max, sum), and the units' pieces of a step.
 struct Cut {
   int32_t piece = 0, npmax = 1, qcols = 0, nqt = 0, ns = 1, nsmax = 1;
   int64_t wgs = 0, slots = 0;  // workgroups; columns of partial results
-  size_t ml = 0, total = 0;
+  size_t ml = 0, np = 0, total = 0;
 };
 
 bool attend_cut(const vc_decode_shape *s, int32_t n, int32_t max_rows, Cut &c) {
@@ -111,14 +111,86 @@ bool attend_cut(const vc_decode_shape *s, int32_t n, int32_t max_rows, Cut &c) {
   }
   if (c.wgs >= kMaxWg || (c.slots && units * cols >= 2 * kMaxWg)) return false;  // (the join: 256 threads a column)
   c.ml = align_up(sizeof(float) * (size_t)c.slots * (size_t)s->d);
-  c.total = std::max(c.ml + align_up(sizeof(float2) * (size_t)c.slots), kAlign);
+  c.np = c.ml + align_up(sizeof(float2) * (size_t)c.slots);
+  c.total = std::max(c.np + (cols <= kCols ? align_up(sizeof(int32_t) * (size_t)units) : 0), kAlign);
   return true;
+}
+
+// The rotation as the kernels take it.
+vc_status rope_table(const vc_rope *r, int32_t d, RopeTable &t) {
+  if (r->rot < 16 || r->rot % 16 != 0 || r->rot > d) return VC_ERR_ARG;
+  for (int i = 0; i < 3; ++i)
+    if (r->sections[i] < 0 || r->sections[i] > r->rot / 2) return VC_ERR_ARG;
+  if (r->sections[0] + r->sections[1] + r->sections[2] != r->rot / 2) return VC_ERR_ARG;
+  if ((r->layout != VC_ROPE_SECTIONED && r->layout != VC_ROPE_INTERLEAVED) ||
+      (r->pairing != VC_ROPE_HALVES && r->pairing != VC_ROPE_ADJACENT) || (r->fp32 != 0 && r->fp32 != 1) ||
+      (r->inverse != 0 && r->inverse != 1) || !std::isfinite(r->scale))
+    return VC_ERR_ARG;
+  if (!r->inv_freq && !(r->theta > 0.0 && std::isfinite(r->theta))) return VC_ERR_ARG;
+  t = RopeTable{};
+  for (int i = 0; i < r->rot / 2; ++i) {
+    const double f = r->inv_freq ? r->inv_freq[i] : std::pow(r->theta, -2.0 * i / r->rot);
+    if (!std::isfinite(f)) return VC_ERR_ARG;
+    t.turns[i] = f / 6.283185307179586476925286766559;
+    int axis;
+    if (r->layout == VC_ROPE_SECTIONED)
+      axis = (i >= r->sections[0]) + (i >= r->sections[0] + r->sections[1]);
+    else
+      axis = i % 3 == 1 && i < 3 * r->sections[1] ? 1 : i % 3 == 2 && i < 3 * r->sections[2] ? 2 : 0;
+    t.axis1 |= (uint64_t)(axis == 1) << i;
+    t.axis2 |= (uint64_t)(axis == 2) << i;
+  }
+  t.rot = r->rot;
+  t.adjacent = r->pairing == VC_ROPE_ADJACENT;
+  t.scale = r->scale;
+  t.sgn = r->inverse ? -1.f : 1.f;
+  return VC_OK;
 }
 
 // Workgroups a unit of an append: one where its blocks are few, which then also
 // advances the length; else a block each.
 int64_t append_groups(int64_t n) {
   return n <= 4 * kQ8Block ? 1 : (n + kQ8Block - 1) / kQ8Block + 1;
+}
+
+// The checks and the plan of an attention call (n = 0: the checks that apply).
+vc_status attend_plan(const vc_decode_shape *s, const vc_q8cache *c, const vc_rows *q, const vc_rows *out, int32_t n,
+                      const int32_t *count, int32_t causal, int32_t out_fp32, float scale, int32_t max_rows,
+                      void *workspace, size_t workspace_bytes, Q8Attn &p) {
+  vc_status st = check_shape(s);
+  if (st != VC_OK) return st;
+  if ((st = check_cache(c)) != VC_OK) return st;
+  if (n < 0 || max_rows < 0 || (causal != 0 && causal != 1) || (out_fp32 != 0 && out_fp32 != 1)) return VC_ERR_ARG;
+  if (!(scale > 0.f) || !std::isfinite(scale)) return VC_ERR_ARG;
+  if (n == 0) return VC_OK;
+  if (!rows_ok(q, 2, s->L, s->B, n, s->Hq, s->d, false, false) ||
+      !rows_ok(out, out_fp32 ? 4 : 2, s->L, s->B, n, s->Hq, s->d, true, false))
+    return VC_ERR_ARG;
+  Cut cut;
+  if (!attend_cut(s, n, max_rows, cut)) return VC_ERR_UNSUPPORTED;
+  if (!workspace || workspace_bytes < cut.total || reinterpret_cast<uintptr_t>(workspace) % kAlign != 0)
+    return VC_ERR_WORKSPACE;
+  p = Q8Attn{};
+  p.c = bind(c);
+  p.q = desc(q);
+  p.out = desc(out);
+  p.count = count;
+  p.L = s->L; p.B = s->B; p.Hq = s->Hq; p.Hkv = s->Hkv; p.G = s->Hq / s->Hkv; p.d = s->d;
+  p.units = s->L * s->B * s->Hkv;
+  p.n = n;
+  p.cols = n * p.G;
+  p.causal = causal;
+  p.fp32 = out_fp32;
+  p.max_rows = max_rows;
+  p.sc = scale * 1.4426950408889634f;
+  p.wgs = (int32_t)cut.wgs;
+  p.piece = cut.piece; p.npmax = cut.npmax;
+  p.qcols = cut.qcols; p.nqt = cut.nqt; p.ns = cut.ns; p.nsmax = cut.nsmax;
+  uint8_t *ws = static_cast<uint8_t *>(workspace);
+  p.part_o = reinterpret_cast<float *>(ws);
+  p.part_ml = reinterpret_cast<float2 *>(ws + cut.ml);
+  p.np = reinterpret_cast<int32_t *>(ws + cut.np);
+  return VC_OK;
 }
 
 }  // namespace
@@ -187,72 +259,43 @@ size_t viscache_q8_attend_workspace_bytes(const vc_decode_shape *s, int32_t n, i
 vc_status viscache_q8_attend(const vc_decode_shape *s, const vc_q8cache *c, const vc_rows *q, const vc_rows *out,
                              int32_t n, const int32_t *count, int32_t causal, int32_t out_fp32, float scale,
                              int32_t max_rows, void *workspace, size_t workspace_bytes, void *stream) {
-  vc_status st = check_shape(s);
-  if (st != VC_OK) return st;
-  if ((st = check_cache(c)) != VC_OK) return st;
-  if (n < 0 || max_rows < 0 || (causal != 0 && causal != 1) || (out_fp32 != 0 && out_fp32 != 1)) return VC_ERR_ARG;
-  if (!(scale > 0.f) || !std::isfinite(scale)) return VC_ERR_ARG;
-  if (n == 0) return VC_OK;
-  if (!rows_ok(q, 2, s->L, s->B, n, s->Hq, s->d, false, false) ||
-      !rows_ok(out, out_fp32 ? 4 : 2, s->L, s->B, n, s->Hq, s->d, true, false))
-    return VC_ERR_ARG;
-  Cut cut;
-  if (!attend_cut(s, n, max_rows, cut)) return VC_ERR_UNSUPPORTED;
-  if (!workspace || workspace_bytes < cut.total || reinterpret_cast<uintptr_t>(workspace) % kAlign != 0)
-    return VC_ERR_WORKSPACE;
-  Q8Attn p{};
-  p.c = bind(c);
-  p.q = desc(q);
-  p.out = desc(out);
-  p.count = count;
-  p.L = s->L; p.B = s->B; p.Hq = s->Hq; p.Hkv = s->Hkv; p.G = s->Hq / s->Hkv; p.d = s->d;
-  p.units = s->L * s->B * s->Hkv;
-  p.n = n;
-  p.cols = n * p.G;
-  p.causal = causal;
-  p.fp32 = out_fp32;
-  p.max_rows = max_rows;
-  p.sc = scale * 1.4426950408889634f;
-  p.wgs = (int32_t)cut.wgs;
-  p.piece = cut.piece; p.npmax = cut.npmax;
-  p.qcols = cut.qcols; p.nqt = cut.nqt; p.ns = cut.ns; p.nsmax = cut.nsmax;
-  uint8_t *ws = static_cast<uint8_t *>(workspace);
-  p.part_o = reinterpret_cast<float *>(ws);
-  p.part_ml = reinterpret_cast<float2 *>(ws + cut.ml);
+  Q8Attn p;
+  const vc_status st =
+      attend_plan(s, c, q, out, n, count, causal, out_fp32, scale, max_rows, workspace, workspace_bytes, p);
+  if (st != VC_OK || n == 0) return st;
   hipStream_t hs = static_cast<hipStream_t>(stream);
   const hipError_t e = p.cols <= kCols ? launch_q8_decode(p, c->format, hs) : launch_q8_prompt(p, c->format, hs);
   return e == hipSuccess ? VC_OK : VC_ERR_HIP;
 }
 
+vc_status viscache_q8_step(const vc_decode_shape *s, const vc_q8cache *c, const vc_rope *rope, const int32_t *pos,
+                           const vc_rows *q, const vc_rows *k, const vc_rows *v, const vc_rows *out, int32_t out_fp32,
+                           float scale, int32_t max_rows, void *workspace, size_t workspace_bytes, void *stream) {
+  Q8Attn p;
+  vc_status st = attend_plan(s, c, q, out, 1, nullptr, 1, out_fp32, scale, max_rows, workspace, workspace_bytes, p);
+  if (st != VC_OK) return st;
+  if (!rows_ok(k, 2, s->L, s->B, 1, s->Hkv, s->d, false, false) ||
+      !rows_ok(v, 2, s->L, s->B, 1, s->Hkv, s->d, false, false))
+    return VC_ERR_ARG;
+  if (rope) {
+    if (rope->fp32 || !pos) return VC_ERR_ARG;
+    if ((st = rope_table(rope, s->d, p.rope)) != VC_OK) return st;
+  }
+  p.step = 1;
+  p.k = desc(k);
+  p.v = desc(v);
+  p.pos = pos;
+  return launch_q8_decode(p, c->format, static_cast<hipStream_t>(stream)) == hipSuccess ? VC_OK : VC_ERR_HIP;
+}
+
 vc_status viscache_rope(const vc_decode_shape *s, const vc_rope *r, int32_t n, const int32_t *pos,
                         const int32_t *count, const vc_rows *q_in, const vc_rows *q_out, const vc_rows *k_in,
                         const vc_rows *k_out, void *stream) {
-  const vc_status st = check_shape(s);
+  vc_status st = check_shape(s);
   if (st != VC_OK) return st;
   if (!r || n < 0) return VC_ERR_ARG;
-  if (r->rot < 16 || r->rot % 16 != 0 || r->rot > s->d) return VC_ERR_ARG;
-  for (int i = 0; i < 3; ++i)
-    if (r->sections[i] < 0 || r->sections[i] > r->rot / 2) return VC_ERR_ARG;
-  if (r->sections[0] + r->sections[1] + r->sections[2] != r->rot / 2) return VC_ERR_ARG;
-  if ((r->layout != VC_ROPE_SECTIONED && r->layout != VC_ROPE_INTERLEAVED) ||
-      (r->pairing != VC_ROPE_HALVES && r->pairing != VC_ROPE_ADJACENT) || (r->fp32 != 0 && r->fp32 != 1) ||
-      (r->inverse != 0 && r->inverse != 1) || !std::isfinite(r->scale))
-    return VC_ERR_ARG;
-  if (!r->inv_freq && !(r->theta > 0.0 && std::isfinite(r->theta))) return VC_ERR_ARG;
   RopePlan p{};
-  const int half = r->rot / 2;
-  for (int i = 0; i < half; ++i) {
-    const double f = r->inv_freq ? r->inv_freq[i] : std::pow(r->theta, -2.0 * i / r->rot);
-    if (!std::isfinite(f)) return VC_ERR_ARG;
-    p.turns[i] = f / 6.283185307179586476925286766559;
-    int axis;
-    if (r->layout == VC_ROPE_SECTIONED)
-      axis = (i >= r->sections[0]) + (i >= r->sections[0] + r->sections[1]);
-    else
-      axis = i % 3 == 1 && i < 3 * r->sections[1] ? 1 : i % 3 == 2 && i < 3 * r->sections[2] ? 2 : 0;
-    p.axis1 |= (uint64_t)(axis == 1) << i;
-    p.axis2 |= (uint64_t)(axis == 2) << i;
-  }
+  if ((st = rope_table(r, s->d, p.t)) != VC_OK) return st;
   if (!q_in != !q_out || !k_in != !k_out || (!q_in && !k_in)) return VC_ERR_ARG;
   if (n == 0) return VC_OK;
   if (!pos) return VC_ERR_ARG;
@@ -277,11 +320,7 @@ vc_status viscache_rope(const vc_decode_shape *s, const vc_rope *r, int32_t n, c
   p.pos = pos;
   p.count = count;
   p.B = s->B; p.L = s->L; p.d = s->d; p.n = n;
-  p.rot = r->rot;
-  p.adjacent = r->pairing == VC_ROPE_ADJACENT;
   p.fp32 = r->fp32;
-  p.scale = r->scale;
-  p.sgn = r->inverse ? -1.f : 1.f;
   return launch_rope(p, static_cast<hipStream_t>(stream)) == hipSuccess ? VC_OK : VC_ERR_HIP;
 }
 

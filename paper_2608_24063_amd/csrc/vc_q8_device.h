@@ -80,6 +80,16 @@ struct Q8 {
   }
 };
 
+// Accesses that ask the caches not to keep what passes through once and in bulk.
+template <typename T>
+__device__ __forceinline__ void st16_stream(T *p, u32x4 v) {
+  __builtin_nontemporal_store(v, reinterpret_cast<VC_GLOBAL u32x4 *>(gp(p)));
+}
+template <typename T>
+__device__ __forceinline__ u32x4 ld16_stream(const T *p) {
+  return __builtin_nontemporal_load(reinterpret_cast<const VC_GLOBAL u32x4 *>(gp(p)));
+}
+
 // Largest magnitude of packed bf16 pairs, as bf16 bits (unsigned compare of
 // the bits without the sign).
 __device__ __forceinline__ uint32_t max_mag(uint32_t m, uint32_t w) {
@@ -101,6 +111,105 @@ __device__ __forceinline__ u32x4 transpose4(uint32_t w0, uint32_t w1, uint32_t w
   const uint32_t t2 = __builtin_amdgcn_perm(w1, w0, 0x07030602u), t3 = __builtin_amdgcn_perm(w3, w2, 0x07030602u);
   return u32x4{__builtin_amdgcn_perm(t1, t0, 0x05040100u), __builtin_amdgcn_perm(t1, t0, 0x07060302u),
                __builtin_amdgcn_perm(t3, t2, 0x05040100u), __builtin_amdgcn_perm(t3, t2, 0x07060302u)};
+}
+
+// The pair (x1, x2) turned: cs = scale (cos a, sin a).
+__device__ __forceinline__ void turn(float &x1, float &x2, float2 cs) {
+  const float a = x1, b = x2;
+  x1 = fmaf(a, cs.x, -(b * cs.y));
+  x2 = fmaf(b, cs.x, a * cs.y);
+}
+// scale (cos, sin) of the angle of a position: reduced in 64 bits as a number
+// of turns, then 32.
+__device__ __forceinline__ float2 turn_of(const RopeTable &t, int i, int pos) {
+  const double a = (double)pos * t.turns[i];
+  float s, c;
+  sincospif(2.f * (float)(a - rint(a)), &s, &c);
+  return make_float2(c * t.scale, s * t.scale * t.sgn);
+}
+// The axis of frequency i.
+__device__ __forceinline__ int axis_of(const RopeTable &t, int i) {
+  return (int)(t.axis1 >> i & 1) + 2 * (int)(t.axis2 >> i & 1);
+}
+
+// Largest over 256 threads (waves of one half of `red`) of per-thread packed
+// magnitudes; one barrier of the whole workgroup (the next use of `red` must
+// come after another one).
+__device__ __forceinline__ uint32_t max_of_256(uint32_t (&red)[4], uint32_t m, int tid) {
+  uint32_t x = max(m & 0xFFFFu, m >> 16);
+#pragma unroll
+  for (int k = 32; k >= 1; k >>= 1) x = max(x, (uint32_t)__shfl_xor((int)x, k, 64));
+  if ((tid & 63) == 0) red[tid >> 6] = x;
+  __syncthreads();
+  return max(max(red[0], red[1]), max(red[2], red[3]));
+}
+
+// Quantises a block of 64 rows with 256 threads: get(row, c) is 16-byte chunk c
+// of a row, codes go to dst (row-major, or channel-major for values, through
+// `lds`, 64 rows of D + 8 bytes) and the scale to *scale.  The rows are in
+// registers between the search for the largest and the rounding, so they are
+// read once.  Two barriers of the whole workgroup.
+template <int D, int FMT, typename Get>
+__device__ __forceinline__ void seal_block(uint32_t (&red)[4], uint8_t *lds, int tid, bool values, Get get, uint8_t *dst,
+                                           float *scale) {
+  constexpr int CPR = D / 16;                // 16-channel chunks per row
+  constexpr int IT = kQ8Block * CPR / 256;   // chunks per thread (2 or 1)
+  constexpr int VP = D + 8;                  // pitch of the value codes' rows, bytes
+  u32x4 x[IT][2];
+  uint32_t mag = 0u;
+#pragma unroll
+  for (int it = 0; it < IT; ++it) {
+    const int e = tid + 256 * it, row = e / CPR, c = e % CPR;
+    x[it][0] = get(row, 2 * c);
+    x[it][1] = get(row, 2 * c + 1);
+  }
+#pragma unroll
+  for (int it = 0; it < IT; ++it)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      mag = max_mag(max_mag(mag, x[it][h].x), x[it][h].y);
+      mag = max_mag(max_mag(mag, x[it][h].z), x[it][h].w);
+    }
+  const float top = __uint_as_float(max_of_256(red, mag, tid) << 16);
+  const float eff = fminf(fmaxf(top, Q8<FMT>::kEffMin), Q8<FMT>::kEffMax);
+  const float inv = __fdiv_rn(Q8<FMT>::kTop, eff);
+  if (tid == 0) stg(scale, __fdiv_rn(eff, Q8<FMT>::kTop));
+#pragma unroll
+  for (int it = 0; it < IT; ++it) {
+    const int e = tid + 256 * it, row = e / CPR, c = e % CPR;
+    uint32_t o[4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t ws[4] = {x[it][h].x, x[it][h].y, x[it][h].z, x[it][h].w};
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        o[2 * h + k] = Q8<FMT>::pack4(
+            Q8<FMT>::code_value(bf16_lo(ws[2 * k]), inv), Q8<FMT>::code_value(bf16_hi(ws[2 * k]), inv),
+            Q8<FMT>::code_value(bf16_lo(ws[2 * k + 1]), inv), Q8<FMT>::code_value(bf16_hi(ws[2 * k + 1]), inv));
+    }
+    if (!values) {
+      st16(dst + row * D + 16 * c, u32x4{o[0], o[1], o[2], o[3]});
+    } else {
+      u32x2 *t = reinterpret_cast<u32x2 *>(lds + row * VP + 16 * c);
+      t[0] = u32x2{o[0], o[1]};
+      t[1] = u32x2{o[2], o[3]};
+    }
+  }
+  __syncthreads();
+  if (values) {
+    // Thread: channels 4 cq .. 4 cq + 3, rows 8 rg .. 8 rg + 7.
+    const int rg = tid % 8;
+#pragma unroll
+    for (int cq = tid / 8; cq < D / 4; cq += 32) {
+      uint32_t w[8];
+#pragma unroll
+      for (int r = 0; r < 8; ++r) w[r] = *reinterpret_cast<const uint32_t *>(lds + (8 * rg + r) * VP + 4 * cq);
+      const u32x4 a = transpose4(w[0], w[1], w[2], w[3]), b = transpose4(w[4], w[5], w[6], w[7]);
+      const uint32_t as[4] = {a.x, a.y, a.z, a.w}, bs[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) st8(dst + (4 * cq + k) * kQ8Block + 8 * rg, u32x2{as[k], bs[k]});
+    }
+  }
 }
 
 // First element of row i of unit u = (l*B + b)*Hkv + g in a strided tensor.

@@ -498,12 +498,32 @@ class Q8Cache:
                  r + _ROWS_BYTES, n, cnt, int(causal), int(fp32), scale, rows, ws[0], ws[1])
 
     def step(self, q, k, v, out, scale: float, rope: Rope | None = None, pos=None, q_out=None, k_out=None) -> None:
-        """A serving step: rotates q and k by pos (with `rope`; into q_out and
-        k_out, by default in place), appends k and v and attends q."""
+        """A serving step: rotates q and k by pos int32 [3, B, n] (with `rope`),
+        appends k and v and attends q.  One token (n = 1) is a single call
+        (viscache_q8_step).  With more, the rotated rows go to q_out and k_out,
+        by default new tensors.  q, k and v are left as they are."""
+        n, index = q.shape[2], self._index
+        if n != 1:
+            if rope is not None:
+                q, k = rope.apply(pos, q, k, q_out=torch.empty_like(q) if q_out is None else q_out,
+                                  k_out=torch.empty_like(k) if k_out is None else k_out)
+            self.append(k, v)
+            self.attend(q, out, scale)
+            return
+        want, kv = (self.L, self.B, 1, self.Hq, self.d), (self.L, self.B, 1, self.Hkv, self.d)
+        fp32 = out.dtype is _FP32
+        packed = _Rows4(*_take(q, "q", want, _BF16, index), *_take(k, "k", kv, _BF16, index),
+                        *_take(v, "v", kv, _BF16, index), *_take(out, "out", want, _FP32 if fp32 else _BF16, index))
+        r = ctypes.addressof(packed)
+        turn, at = 0, 0
         if rope is not None:
-            q, k = rope.apply(pos, q, k, q_out=q_out, k_out=k_out)
-        self.append(k, v)
-        self.attend(q, out, scale)
+            if rope.d != self.d or pos is None:
+                raise ValueError("the rotation is of another head dim, or has no positions")
+            turn, at = rope._address[0][0], _ints(pos, "pos", (3, self.B, 1), index)
+        ws = self._workspace(1, self.max_cap)
+        _enqueue("viscache_q8_step", self._lib.viscache_q8_step, index, self._shape_at, self._cache_at, turn, at, r,
+                 r + _ROWS_BYTES, r + 2 * _ROWS_BYTES, r + 3 * _ROWS_BYTES, int(fp32), scale, self.max_cap, ws[0],
+                 ws[1])
 
 
 __all__ = ["PruneCall", "DecodeCache", "Q8Cache", "Rope", "make_params"]

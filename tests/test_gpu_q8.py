@@ -461,6 +461,113 @@ def test_far_offsets(dev):
     assert np.array_equal(vo[0, 1, :, 0].cpu().numpy(), V[1].astype(np.float32))
 
 
+# ---- a step in one call -------------------------------------------------------------
+
+def _twins(rng_seed, dev, *a, **kw):
+    return [_filled(np.random.default_rng(rng_seed), dev, *a, **kw)[0] for _ in range(2)]
+
+
+def _same_caches(a, b):
+    torch.cuda.synchronize()
+    for n in ("k_codes", "v_codes", "k_scale", "v_scale", "k_tail", "v_tail", "len"):
+        assert torch.equal(getattr(a, n).view(torch.uint8), getattr(b, n).view(torch.uint8)), n
+
+
+ROPES = [None, dict(), dict(pairing=1), dict(rot=32, sections=(6, 5, 5), layout=1),
+         dict(rot=48, sections=(0, 12, 12), pairing=1, scale=0.5)]
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("d,G", [(64, 4), (128, 7), (128, 16), (64, 1)])
+@pytest.mark.parametrize("turn", range(len(ROPES)))
+@pytest.mark.parametrize("fp32", [True, False])
+def test_step_is_its_three_calls(dev, fmt, d, G, turn, fp32):
+    """viscache_q8_step against viscache_rope, _append and _attend: every buffer and
+    output bit for bit, over units that are empty, full, about to be sealed."""
+    from paper_2608_24063_amd.tensors import Rope
+    rng = np.random.default_rng(d + G + turn)
+    L, B, Hkv = 2, 2, 3
+    Hq = G * Hkv
+    lens = [0, 1, 61, 62, 63, 64, 126, 127, 128, 500, 63, 64]
+    a, b = _twins(turn, dev, L, B, Hq, Hkv, d, lens, fmt, extra=2)
+    for c in (a, b):
+        c.cap[10:] = torch.tensor([63, 64], dtype=torch.int32, device=dev)  # full ones
+    rope = None if ROPES[turn] is None else Rope(d, theta=1e4, **ROPES[turn])
+    for t in range(4):
+        q, k, v = (_t(_values(rng, (L, B, 1, h, d)), dev) for h in (Hq, Hkv, Hkv))
+        pos = torch.from_numpy(rng.integers(0, 9000, (3, B, 1)).astype(np.int32)).to(dev)
+        typ = torch.float32 if fp32 else torch.bfloat16
+        oa, ob = (torch.full((L, B, 1, Hq, d), 7.0, dtype=typ, device=dev) for _ in range(2))
+        keep = [x.clone() for x in (q, k, v)]
+        a.step(q, k, v, oa, 0.11, rope=rope, pos=pos)
+        assert all(torch.equal(x, y) for x, y in zip((q, k, v), keep))
+        if rope is not None:
+            rope.apply(pos, q, k)
+        b.append(k, v)
+        b.attend(q, ob, 0.11)
+        assert torch.equal(oa, ob), t
+        _same_caches(a, b)
+    assert a.len.cpu().tolist() == [min(n + 4, n + 2) if i < 10 else n for i, n in enumerate(lens)]
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+def test_step_over_cut_units(dev, fmt):
+    """Few long units, whose rows go to several workgroups: the last one appends,
+    the join advances the lengths; across a sealing, on strided inputs."""
+    rng = np.random.default_rng(21)
+    L, B, Hq, Hkv, d = 1, 2, 14, 2, 128
+    lens = [6398, 6399, 12, 8063]
+    a, b = _twins(3, dev, L, B, Hq, Hkv, d, lens, fmt, extra=5)
+    for t in range(4):
+        wide = _t(_values(rng, (L, B, 1, Hq + 2 * Hkv, d)), dev)
+        q, k, v = wide[:, :, :, :Hq], wide[:, :, :, Hq:Hq + Hkv], wide[:, :, :, Hq + Hkv:]
+        oa, ob = (torch.zeros((L, B, 1, Hq, d), dtype=torch.float32, device=dev) for _ in range(2))
+        a.step(q, k, v, oa, 0.09)
+        b.append(k, v)
+        b.attend(q, ob, 0.09)
+        assert torch.equal(oa, ob), t
+        _same_caches(a, b)
+    assert a.len.cpu().tolist() == [n + 4 for n in lens]
+
+
+def test_step_past_its_row_bound(dev):
+    """A row bound below the lengths bounds what is attended, not what is appended."""
+    import paper_2608_24063_amd as vc
+    rng = np.random.default_rng(22)
+    lens = [100, 63, 64, 200]
+    a, b = _twins(4, dev, 1, 2, 8, 2, 64, lens, "int8", extra=3)
+    q, k, v = (_t(_values(rng, (1, 2, 1, h, 64)), dev) for h in (8, 2, 2))
+    oa, ob = (torch.zeros((1, 2, 1, 8, 64), dtype=torch.float32, device=dev) for _ in range(2))
+    ws, nbytes = a._workspace(1, 64)
+    r = lambda t: vc.vc_rows(t.data_ptr(), *t.stride()[:4])  # noqa: E731
+    vc.viscache_q8_step(a.shape, a.c, None, 0, r(q), r(k), r(v), r(oa), 1, 0.125, 64, ws, nbytes,
+                        torch.cuda.current_stream().cuda_stream)
+    b.append(k, v)
+    b.attend(q, ob, 0.125, max_rows=64)
+    assert torch.equal(oa, ob)
+    _same_caches(a, b)
+
+
+def test_step_of_several_tokens(dev):
+    """Prompts and drafts through step(): three calls, the inputs left alone."""
+    from paper_2608_24063_amd.tensors import Rope
+    rng = np.random.default_rng(23)
+    a, b = _twins(5, dev, 1, 2, 8, 2, 64, [100, 63, 64, 0], "e4m3", extra=70)
+    rope = Rope(64, sections=(8, 12, 12))
+    for n in (2, 66):
+        q, k, v = (_t(_values(rng, (1, 2, n, h, 64)), dev) for h in (8, 2, 2))
+        pos = torch.from_numpy(rng.integers(0, 9000, (3, 2, n)).astype(np.int32)).to(dev)
+        oa, ob = (torch.zeros((1, 2, n, 8, 64), dtype=torch.bfloat16, device=dev) for _ in range(2))
+        keep = q.clone()
+        a.step(q, k, v, oa, 0.125, rope=rope, pos=pos)
+        assert torch.equal(q, keep)
+        rope.apply(pos, q, k)
+        b.append(k, v)
+        b.attend(q, ob, 0.125)
+        assert torch.equal(oa, ob)
+        _same_caches(a, b)
+
+
 # ---- streams, graphs, runs of them together ------------------------------------------
 
 def test_other_stream(dev):
@@ -496,7 +603,7 @@ def test_graph_of_steps(dev, fmt):
     pos = torch.zeros_like(ps[0])
     oa = torch.zeros((L, B, 1, Hq, d), dtype=torch.float32, device=dev)
     ob, oc = torch.zeros_like(oa), torch.zeros_like(oa)
-    qr, kr = torch.zeros_like(buf["q"]), torch.zeros_like(buf["k"])
+    qr = torch.zeros_like(buf["q"])
     pq = _t(_values(rng, (L, B, 9, Hq, d)), dev)
     po, pe = torch.zeros((L, B, 9, Hq, d), dtype=torch.bfloat16, device=dev), torch.zeros((L, B, 9, Hq, d), dtype=torch.bfloat16, device=dev)
     a._workspace(9, a.max_cap), a._workspace(1, a.max_cap)
@@ -504,14 +611,14 @@ def test_graph_of_steps(dev, fmt):
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):  # once before the capture
-        a.step(buf["q"], buf["k"], buf["v"], oa, 0.125, rope=rope, pos=pos, q_out=qr, k_out=kr)
+        a.step(buf["q"], buf["k"], buf["v"], oa, 0.125, rope=rope, pos=pos)
         a.attend(pq, po, 0.125)
     torch.cuda.current_stream().wait_stream(side)
     for n, x in keep.items():
         getattr(a, n).view(torch.uint8).copy_(x)
     g1, g2 = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
     with torch.cuda.graph(g1):
-        a.step(buf["q"], buf["k"], buf["v"], oa, 0.125, rope=rope, pos=pos, q_out=qr, k_out=kr)
+        a.step(buf["q"], buf["k"], buf["v"], oa, 0.125, rope=rope, pos=pos)
     with torch.cuda.graph(g2):
         a.attend(pq, po, 0.125)
     torch.cuda.synchronize()
@@ -522,7 +629,8 @@ def test_graph_of_steps(dev, fmt):
         g1.replay()
         g2.replay()
         torch.cuda.synchronize()
-        b.step(xs["q"][t].clone(), xs["k"][t].clone(), xs["v"][t], ob, 0.125, rope=rope, pos=ps[t].contiguous())
+        b.step(xs["q"][t], xs["k"][t], xs["v"][t], ob, 0.125, rope=rope, pos=ps[t].contiguous())
+        rope.apply(pos, buf["q"], q_out=qr)
         b.attend(pq, pe, 0.125)
         a.attend(qr, oc, 0.125)  # eager, on the graphs' workspace
         torch.cuda.synchronize()
@@ -573,7 +681,10 @@ def test_pruned_cache_to_decode(dev, sg):
         pos = np.broadcast_to(max(n) + 20 * t + np.arange(cnt), (3, w.B, cnt)).astype(np.int32)
         tq, tk = _t(q, dev), _t(k, dev)
         out = torch.full((w.L, w.B, cnt, w.Hq, w.d), 7.0, dtype=torch.float32, device=dev)
-        c.step(tq, tk, _t(v, dev), out, w.d ** -0.5, rope=rope, pos=_t(pos, dev, torch.int32))
+        tp = _t(pos, dev, torch.int32)
+        c.step(tq, tk, _t(v, dev), out, w.d ** -0.5, rope=rope, pos=tp)
+        assert np.array_equal(tq.float().cpu().numpy(), q) and np.array_equal(tk.float().cpu().numpy(), k)
+        rope.apply(tp, tq, tk)  # the rows as the step turned them
         torch.cuda.synchronize()
         # the rotation, to half a step of bf16 (2^-8) and the roundings of an fp32 rotation
         gq, gk = tq.float().cpu().numpy(), tk.float().cpu().numpy()

@@ -67,6 +67,13 @@ def _attend(vc, shape=None, cache=None, q=None, out=None, n=1, causal=1, fp32=0,
                    out or _rows(vc), n, 0, causal, fp32, scale, rows, ws, bytes_, 0)
 
 
+def _step(vc, shape=None, cache=None, rope=None, pos=0, q=None, k=None, v=None, out=None, fp32=0, scale=0.1, rows=100,
+          ws=P16, bytes_=1 << 40):
+    r = [x or _rows(vc) for x in (q, k, v, out)]
+    return _status(vc, vc.viscache_q8_step, shape or _shape(vc), cache or _cache(vc), rope, pos, *r, fp32, scale, rows,
+                   ws, bytes_, 0)
+
+
 def _rope_args(vc, **kw):
     a = dict(rot=128, s=(16, 24, 24), layout=0, pairing=0, fp32=0, inverse=0, scale=1.0, theta=1e4, inv_freq=None)
     a.update(kw)
@@ -82,21 +89,21 @@ def _rope(vc, shape=None, n=4, pos=P16, q=(1, 1), k=(1, 1), rows=None, **kw):
 @pytest.mark.parametrize("kw,want", BAD_SHAPES)
 def test_bad_shapes(vc, kw, want):
     s, want = _shape(vc, **kw), getattr(vc, "VC_ERR_" + want)
-    assert _append(vc, s) == _read(vc, s) == _attend(vc, s) == _rope(vc, s) == want
+    assert _append(vc, s) == _read(vc, s) == _attend(vc, s) == _rope(vc, s) == _step(vc, s) == want
     assert vc.viscache_q8_attend_workspace_bytes(s, 1, 100) == 0
 
 
 @pytest.mark.parametrize("name", ["k_codes", "v_codes", "k_scale", "v_scale", "k_tail", "v_tail", "row_off", "cap", "len"])
 def test_null_cache_members(vc, name):
     c = _cache(vc, **{name: None})
-    assert _append(vc, cache=c) == _read(vc, cache=c) == _attend(vc, cache=c) == vc.VC_ERR_ARG
+    assert _append(vc, cache=c) == _read(vc, cache=c) == _attend(vc, cache=c) == _step(vc, cache=c) == vc.VC_ERR_ARG
 
 
 @pytest.mark.parametrize("kw", [dict(format=2), dict(format=-1), dict(k_codes=P16 + 8), dict(v_codes=P16 + 4),
                                 dict(k_tail=P16 + 2), dict(v_tail=P16 + 8)])
 def test_bad_cache(vc, kw):
     c = _cache(vc, **kw)
-    assert _append(vc, cache=c) == _read(vc, cache=c) == _attend(vc, cache=c) == vc.VC_ERR_ARG
+    assert _append(vc, cache=c) == _read(vc, cache=c) == _attend(vc, cache=c) == _step(vc, cache=c) == vc.VC_ERR_ARG
 
 
 @pytest.mark.parametrize("kw", [dict(data=None), dict(data=P16 + 8), dict(layer=-8), dict(seq=4), dict(token=1001),
@@ -113,6 +120,18 @@ def test_outputs_on_themselves(vc, kw):
     """Strides under d (0 among them) repeat rows: refused for outputs."""
     r, A = _rows(vc, **kw), vc.VC_ERR_ARG
     assert _read(vc, k=r) == _read(vc, v=r) == _attend(vc, out=r, n=2) == _rope(vc, rows=r) == A
+
+
+def test_step_refusals(vc):
+    A, W = vc.VC_ERR_ARG, vc.VC_ERR_WORKSPACE
+    for kw in (dict(data=None), dict(data=P16 + 8), dict(layer=-8), dict(seq=4), dict(head=-128)):
+        r = _rows(vc, **kw)
+        assert _step(vc, q=r) == _step(vc, k=r) == _step(vc, v=r) == _step(vc, out=r) == A
+    assert _step(vc, out=_rows(vc, head=64)) == _step(vc, rows=-1) == _step(vc, fp32=2) == _step(vc, scale=0.0) == A
+    assert _step(vc, ws=0) == _step(vc, ws=P16 + 128) == W
+    assert _step(vc, bytes_=vc.viscache_q8_attend_workspace_bytes(_shape(vc), 1, 100) - 1) == W
+    assert _step(vc, rope=_rope_args(vc), pos=0) == _step(vc, rope=_rope_args(vc, fp32=1), pos=P16) == A
+    assert _step(vc, rope=_rope_args(vc, rot=144), pos=P16) == _step(vc, rope=_rope_args(vc, theta=0.0), pos=P16) == A
 
 
 def test_scalars(vc):
