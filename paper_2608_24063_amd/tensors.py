@@ -4,6 +4,7 @@ stream.  No computation happens here."""
 from __future__ import annotations
 
 import ctypes
+import struct
 
 import torch
 
@@ -227,12 +228,10 @@ class DecodeCache:
 
 # ---- the 8-bit cache and the rotary positions ---------------------------------
 # A call of a few microseconds on the GPU is soon bound by what is done for it
-# here, so descriptors are packed as plain integers (a vc_rows is five of them)
-# and a tensor is looked at once.
+# here, so a tensor is looked at once and its vc_rows is packed as bytes.
 
-_Rows2, _Rows4 = ctypes.c_int64 * 10, ctypes.c_int64 * 20
-_ROWS_BYTES = 40
-assert ctypes.sizeof(vc_rows) == _ROWS_BYTES
+_pack_rows = struct.Struct("5q").pack
+assert ctypes.sizeof(vc_rows) == struct.calcsize("5q")
 _current_device = getattr(torch._C, "_cuda_getDevice", None)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _BF16, _FP32 = torch.bfloat16, torch.float32
@@ -242,15 +241,17 @@ def _refuse(t, name, shape, typ, index):
     raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype} on {t.device}, need {tuple(shape)} {typ} on GPU {index}")
 
 
-def _take(t: torch.Tensor, name: str, shape, typ, index: int):
-    """(address, strides of the first four dimensions) of a tensor of this shape,
-    type and GPU whose rows are contiguous."""
+def _take(t: torch.Tensor, name: str, shape, typ, index: int, head_major: bool = False) -> bytes:
+    """The vc_rows of a tensor [L, B, n, H, d] ([L, B, H, n, d] with head_major) of
+    this shape, type and GPU, its rows contiguous."""
     if t.shape != shape or t.dtype is not typ or t.get_device() != index or index < 0:
         _refuse(t, name, shape, typ, index)
     s = t.stride()
     if s[4] != 1:
         raise ValueError(f"{name}: rows must be contiguous")
-    return t.data_ptr(), s[0], s[1], s[2], s[3]
+    if head_major:
+        return _pack_rows(t.data_ptr(), s[0], s[1], s[3], s[2])
+    return _pack_rows(t.data_ptr(), s[0], s[1], s[2], s[3])
 
 
 def _ints(t, name: str, shape, index: int) -> int:
@@ -309,8 +310,7 @@ class Rope:
         L, B, n, _, d = ref.shape
         if (typ is not _BF16 and typ is not _FP32) or d != self.d:
             _refuse(ref, "q" if q is not None else "k", ref.shape[:-1] + (self.d,), "bf16 or fp32", max(index, 0))
-        none = (0, 0, 0, 0, 0)
-        qi = qo = ki = ko = none
+        qi = qo = ki = ko = None
         Hq = Hkv = 0
         if q is not None:
             qi = _take(q, "q", ref.shape, typ, index)
@@ -329,12 +329,8 @@ class Rope:
         shape = self._shapes.get(key)
         if shape is None:
             shape = self._shapes[key] = vc_decode_shape(B, L, Hq or Hkv, Hkv or Hq, d)
-        rows = _Rows4(*qi, *qo, *ki, *ko)
-        r = ctypes.addressof(rows)
-        rq, rk = (r if Hq else 0), (r + 2 * _ROWS_BYTES if Hkv else 0)
         _enqueue("viscache_rope", self._f, index, ctypes.addressof(shape),
-                 self._address[typ is _FP32][bool(inverse)], n, at, cnt, rq, rq and rq + _ROWS_BYTES, rk,
-                 rk and rk + _ROWS_BYTES)
+                 self._address[typ is _FP32][bool(inverse)], n, at, cnt, qi, qo, ki, ko)
         return q_out, k_out
 
 
@@ -418,22 +414,14 @@ class Q8Cache:
         cnt = _ints(count, "count", (self.L * self.B,), self._index)
         if n == 0:
             return
-        rows = _Rows2(*kr, *vr)
-        r = ctypes.addressof(rows)
-        _enqueue("viscache_q8_append", self._lib.viscache_q8_append, self._index, self._shape_at, self._cache_at, r,
-                 r + _ROWS_BYTES, n, cnt, 0)
+        _enqueue("viscache_q8_append", self._lib.viscache_q8_append, self._index, self._shape_at, self._cache_at, kr,
+                 vr, n, cnt, 0)
 
     def _pair(self, k, v, head_major, typ):
         """The descriptors of keys and values [L, B, n, Hkv, d] (or [L, B, Hkv, n, d]), and n."""
-        if head_major:
-            n = k.shape[3]
-            want = (self.L, self.B, self.Hkv, n, self.d)
-            (p, s0, s1, s2, s3), (pv, v0, v1, v2, v3) = (_take(k, "k", want, typ, self._index),
-                                                         _take(v, "v", want, typ, self._index))
-            return (p, s0, s1, s3, s2), (pv, v0, v1, v3, v2), n
-        n = k.shape[2]
-        want = (self.L, self.B, n, self.Hkv, self.d)
-        return _take(k, "k", want, typ, self._index), _take(v, "v", want, typ, self._index), n
+        n = k.shape[3 if head_major else 2]
+        want = (self.L, self.B, self.Hkv, n, self.d) if head_major else (self.L, self.B, n, self.Hkv, self.d)
+        return (_take(k, "k", want, typ, self._index, head_major), _take(v, "v", want, typ, self._index, head_major), n)
 
     def load_pruned(self, pc: "PruneCall") -> None:
         """Appends what pc.run() left in its outputs (bf16 values): every
@@ -475,10 +463,8 @@ class Q8Cache:
             raise ValueError(f"max_rows {m} exceeds the {rows} rows of k")
         if rows == 0:
             return
-        rows = _Rows2(*kr, *vr)
-        r = ctypes.addressof(rows)
-        _enqueue("viscache_q8_read", self._lib.viscache_q8_read, self._index, self._shape_at, self._cache_at, m, r,
-                 r + _ROWS_BYTES, 0, int(typ is _FP32))
+        _enqueue("viscache_q8_read", self._lib.viscache_q8_read, self._index, self._shape_at, self._cache_at, m, kr, vr,
+                 0, int(typ is _FP32))
 
     def attend(self, q, out, scale: float, count=None, causal: bool = True, max_rows=None) -> None:
         """Attention of q bf16 [L, B, n, Hq, d] over the cache into out (bf16 or
@@ -486,16 +472,14 @@ class Q8Cache:
         n = q.shape[2]
         want = (self.L, self.B, n, self.Hq, self.d)
         fp32 = out.dtype is _FP32
-        packed = _Rows2(*_take(q, "q", want, _BF16, self._index),
-                        *_take(out, "out", want, _FP32 if fp32 else _BF16, self._index))
+        qr, outr = _take(q, "q", want, _BF16, self._index), _take(out, "out", want, _FP32 if fp32 else _BF16, self._index)
         cnt = _ints(count, "count", (self.B,), self._index)
         if n == 0:
             return
         rows = self.max_cap if max_rows is None else int(max_rows)
         ws = self._workspace(n, rows)
-        r = ctypes.addressof(packed)
-        _enqueue("viscache_q8_attend", self._lib.viscache_q8_attend, self._index, self._shape_at, self._cache_at, r,
-                 r + _ROWS_BYTES, n, cnt, int(causal), int(fp32), scale, rows, ws[0], ws[1])
+        _enqueue("viscache_q8_attend", self._lib.viscache_q8_attend, self._index, self._shape_at, self._cache_at, qr,
+                 outr, n, cnt, int(causal), int(fp32), scale, rows, ws[0], ws[1])
 
     def step(self, q, k, v, out, scale: float, rope: Rope | None = None, pos=None, q_out=None, k_out=None) -> None:
         """A serving step: rotates q and k by pos int32 [3, B, n] (with `rope`),
@@ -512,18 +496,16 @@ class Q8Cache:
             return
         want, kv = (self.L, self.B, 1, self.Hq, self.d), (self.L, self.B, 1, self.Hkv, self.d)
         fp32 = out.dtype is _FP32
-        packed = _Rows4(*_take(q, "q", want, _BF16, index), *_take(k, "k", kv, _BF16, index),
-                        *_take(v, "v", kv, _BF16, index), *_take(out, "out", want, _FP32 if fp32 else _BF16, index))
-        r = ctypes.addressof(packed)
+        rows = (_take(q, "q", want, _BF16, index), _take(k, "k", kv, _BF16, index), _take(v, "v", kv, _BF16, index),
+                _take(out, "out", want, _FP32 if fp32 else _BF16, index))
         turn, at = 0, 0
         if rope is not None:
             if rope.d != self.d or pos is None:
                 raise ValueError("the rotation is of another head dim, or has no positions")
             turn, at = rope._address[0][0], _ints(pos, "pos", (3, self.B, 1), index)
         ws = self._workspace(1, self.max_cap)
-        _enqueue("viscache_q8_step", self._lib.viscache_q8_step, index, self._shape_at, self._cache_at, turn, at, r,
-                 r + _ROWS_BYTES, r + 2 * _ROWS_BYTES, r + 3 * _ROWS_BYTES, int(fp32), scale, self.max_cap, ws[0],
-                 ws[1])
+        _enqueue("viscache_q8_step", self._lib.viscache_q8_step, index, self._shape_at, self._cache_at, turn, at, *rows,
+                 int(fp32), scale, self.max_cap, ws[0], ws[1])
 
 
 __all__ = ["PruneCall", "DecodeCache", "Q8Cache", "Rope", "make_params"]
