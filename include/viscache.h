@@ -436,8 +436,8 @@ typedef enum { VC_Q8_INT8 = 0, VC_Q8_E4M3 = 1 } vc_q8_format; /* e4m3: finite on
 
 /* Unit u = (l*B + b)*Hkv + g owns rows [row_off[u], row_off[u] + 64 ceil(cap[u]
  * / 64)) of the code pools and the entries of those blocks (row / 64) of the
- * scale arrays, and holds len[u] <= cap[u] rows; row_off[u] must be a multiple
- * of 64, and units must not overlap.  With block = row_off[u] / 64 + i / 64 and
+ * scale arrays, and holds len[u] <= cap[u] rows (at most 2^31 - 129); row_off[u]
+ * must be a multiple of 64, and units must not overlap.  With block = row_off[u] / 64 + i / 64 and
  * j = i % 64, row i of a sealed block has its key codes at k_codes + (block*64 +
  * j)*d (row-major) and the code of value channel c at v_codes + block*64*d +
  * c*64 + j (channel-major).  Row i of the open block is row j of the unit's tail.

@@ -29,7 +29,7 @@ __global__ __launch_bounds__(kThreads) void k_append_rows(Q8Rows p) {
   constexpr int CPR = D / 16;                     // 16-channel chunks per row
   const int u = (int)(blockIdx.x / (uint32_t)p.nj), j = (int)(blockIdx.x % (uint32_t)p.nj);
   const int side = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 8), tid = threadIdx.x & 255;
-  const int len0 = max(ldg(p.c.len + u), 0), cap = ldg(p.c.cap + u);
+  const int len0 = max(ldg(p.c.len + u), 0), cap = min(ldg(p.c.cap + u), kQ8MaxRows);
   const int want = p.count ? min(max(ldg(p.count + u / p.Hkv), 0), p.n) : p.n;
   const int m = min(want, max(cap - len0, 0));
   if (m <= 0) return;
@@ -81,7 +81,7 @@ __global__ __launch_bounds__(256) void k_append_len(Q8Rows p) {
   if (u >= p.units) return;
   const int len0 = max(ldg(p.c.len + u), 0);
   const int want = p.count ? min(max(ldg(p.count + u / p.Hkv), 0), p.n) : p.n;
-  const int m = min(want, max(ldg(p.c.cap + u) - len0, 0));
+  const int m = min(want, max(min(ldg(p.c.cap + u), kQ8MaxRows) - len0, 0));
   if (m > 0) stg(p.c.len + u, len0 + m);
 }
 
@@ -107,7 +107,7 @@ __global__ __launch_bounds__(kThreads) void k_read_rows(Q8Rows p) {
   __shared__ uint32_t vt[D * VP / 4];
   const int u = (int)(blockIdx.x / (uint32_t)p.nj), j = (int)(blockIdx.x % (uint32_t)p.nj);
   const int side = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 8), tid = threadIdx.x & 255;
-  const int len = max(min(ldg(p.c.len + u), ldg(p.c.cap + u)), 0);
+  const int len = rows_held(ldg(p.c.len + u), ldg(p.c.cap + u));
   const int rows = min(min(len, p.n) - j * kQ8Block, kQ8Block);
   if (rows <= 0) return;
   const int64_t blk = ldg(p.c.row_off + u) / kQ8Block + j;

@@ -190,8 +190,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_decode8(Q8Attn p) {
   // What the unit is, in one round trip.
   const int len_ = ldg(p.c.len + u), cap_ = ldg(p.c.cap + u), cnt_ = p.count ? ldg(p.count + b) : p.n;
   const int64_t row_off = ldg(p.c.row_off + u);
-  const int len0 = max(min(len_, cap_), 0), cnt = min(max(cnt_, 0), p.n);
-  const bool room = STEP && len_ >= 0 && len_ < cap_;  // a step appends a row
+  const int len0 = rows_held(len_, cap_), cnt = min(max(cnt_, 0), p.n);
+  const bool room = STEP && len_ >= 0 && len_ < min(cap_, kQ8MaxRows);  // a step appends a row
   const int len = len0 + room;
   const int cols = cnt * p.G;
   const int emax = cols > 0 ? min(len, p.max_rows) : 0;  // rows any column sees

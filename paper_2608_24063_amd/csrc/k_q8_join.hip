@@ -55,7 +55,7 @@ __global__ __launch_bounds__(256) void k_join(Q8Attn p) {
       ns = v & 0x3FFFFFFF;
       if (col == 0 && (v >> 30) && lane == 0 && w % WPC == 0) stg(p.c.len + u, ldg(p.c.len + u) + 1);
     } else {
-      const int rows = min(max(min(ldg(p.c.len + u), ldg(p.c.cap + u)), 0), p.max_rows);
+      const int rows = min(rows_held(ldg(p.c.len + u), ldg(p.c.cap + u)), p.max_rows);
       ns = ((rows + kQ8Block - 1) / kQ8Block + p.piece - 1) / p.piece;
     }
     at = (int64_t)u * p.npmax * p.qcols + col;

@@ -83,7 +83,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt8(Q8Attn p) {
   const int u = sh.u, qt = sh.qt, sp = sh.sp, ns = sh.ns;
   if (u < 0) return;
   const int b = u / p.Hkv % p.B;
-  const int len = max(min(ldg(p.c.len + u), ldg(p.c.cap + u)), 0);
+  const int len = rows_held(ldg(p.c.len + u), ldg(p.c.cap + u));
   const int cnt = p.count ? min(max(ldg(p.count + b), 0), p.n) : p.n;
   const int cols = cnt * p.G;
   const int c0 = qt * p.qcols;
@@ -398,7 +398,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt8(Q8Attn p) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) big = fmaxf(big, fabsf(O[cb][i]));
     big = max_halves(big);
-    const int k = big > 0.f ? (int)(__float_as_uint(big) >> 23) - 127 - 14 : 0;
+    const int k = big > 0.f ? max((int)(__float_as_uint(big) >> 23) - 127 - 14, -126) : 0;
     const float down = ldexpf(1.f, -k);
     m += (float)k;
     l *= down;

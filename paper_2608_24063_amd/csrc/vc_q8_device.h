@@ -212,6 +212,11 @@ __device__ __forceinline__ void seal_block(uint32_t (&red)[4], uint8_t *lds, int
   }
 }
 
+// Rows a unit holds: its length within its capacity, and so that the end of
+// its last block still is a row index.
+constexpr int kQ8MaxRows = INT32_MAX - 2 * kQ8Block;
+__device__ __forceinline__ int rows_held(int len, int cap) { return max(min(min(len, cap), kQ8MaxRows), 0); }
+
 // First element of row i of unit u = (l*B + b)*Hkv + g in a strided tensor.
 __device__ __forceinline__ int64_t unit_base(const RowsDesc &r, const int64_t *unit_off, int u, int B, int Hkv) {
   if (unit_off) return ldg(unit_off + u);

@@ -421,6 +421,51 @@ def test_values_of_unlike_blocks(dev, n, fp32):
             assert np.abs(out[0, 0, n - 1, h] - want).max() <= tol, (j, h)
 
 
+@pytest.mark.parametrize("B,Hkv,G,n,rows", [(130, 1, 4, 8, 700), (70, 2, 7, 40, 600), (3, 1, 16, 20, 9000)])
+@pytest.mark.parametrize("fp32", [True, False])
+def test_ragged_batches_cut_along_their_rows(dev, B, Hkv, G, n, rows, fp32):
+    """Counts of many sequences, some without queries, whose tiles' workgroups go
+    to the others as further splits."""
+    rng = np.random.default_rng(B)
+    L = 2 if B == 70 else 1
+    counts = [int(x) for x in rng.integers(0, n + 1, B)]
+    counts[0], counts[-1], counts[B // 2] = n, n, 0
+    lens = [int(x) for x in rng.integers(rows // 2, rows, L * B * Hkv)]
+    c, K, V = _filled(rng, dev, L, B, G * Hkv, Hkv, 64, lens, "int8")
+    q = ref.bf16(rng.standard_normal((L, B, n, G * Hkv, 64)))
+    out = _run_attend(c, q, dev, fp32, 0.125, counts)
+    _check_attend(out, q, K, V, lens, L, B, G * Hkv, Hkv, 0.125, counts, True, sample=[0, n - 1])
+    none = _run_attend(c, q, dev, fp32, 0.125, [0] * B)
+    assert (none == 7.0).all()
+
+
+def test_parts_of_almost_nothing(dev):
+    """A split whose values are zero but for rows of almost no weight: its part is
+    tiny, not lost and not infinite."""
+    rng = np.random.default_rng(24)
+    d, rows, n = 64, 64 * 40, 20
+    k, v = _values(rng, (1, 1, rows, 1, d)), np.zeros((1, 1, rows, 1, d), dtype=np.float32)
+    k[0, 0, :, 0] = 0
+    k[0, 0, ::2, 0, 0] = 1.0
+    v[0, 0, 1::128, 0] = 1.0  # on rows of the small weight alone
+    c = _make(1, 1, 4, 1, d, [rows], dev, "e4m3")
+    c.append(_t(k, dev), _t(v, dev))
+    K, V = ref.read_back(k[0, 0, :, 0], "e4m3"), ref.read_back(v[0, 0, :, 0], "e4m3")
+    for pull in (1.0, 20.0, 60.0, 80.0):  # weights of e^-pull
+        q = np.zeros((1, 1, n, 4, d), dtype=np.float32)
+        q[..., 0] = pull
+        for fp32 in (True, False):
+            out = _run_attend(c, q, dev, fp32, 1.0, None, False)
+            want, reach = ref.attend(q[0, 0, 0, 0], K, V, 1.0, rows)
+            # Every term is positive, so the roundings are relative to the sum; but
+            # weights are held in fp16, whose smallest step is 2^-24: half of it where
+            # the largest weight is 2^14 (fp32 outputs) or at least 2^8, for each of
+            # the 20 rows with values (the sum of the weights is at least 1).
+            tol = ref.tolerance(rows, d, reach, 1.0, fp32) * np.abs(want).max() * 4
+            tol += 20 * 2.0 ** -25 / (2.0 ** 14 if fp32 else 2.0 ** 8)
+            assert np.isfinite(out).all() and float(np.abs(np.asarray(out[0, 0]) - want).max()) <= tol
+
+
 def test_shared_and_strided_rows(dev):
     """Queries repeated by a stride of 0, outputs inside a wider tensor."""
     import paper_2608_24063_amd as vc
