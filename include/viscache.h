@@ -476,8 +476,9 @@ typedef struct {
  * room; len grows by the rows appended.  unit_off, if not NULL, is a DEVICE
  * array [L*B*Hkv] of the element offset of each unit's first row (a multiple
  * of 8), instead of the layer, seq and head strides: packed rows such as
- * viscache_prune's outputs.  Tail rows past the open block's are left as they
- * were.  n = 0 does nothing.  The cache's other arrays must not be in use on
+ * viscache_prune's outputs.  Rows should be finite: an infinity or a NaN makes
+ * the keys (or values) of its block meaningless, open or sealed, and no other's.
+ * Tail rows past the open block's are left as they were.  n = 0 does nothing.  The cache's other arrays must not be in use on
  * another stream.  VC_ERR_UNSUPPORTED where the launch would take 2^23 or more
  * workgroups (one per unit for n <= 256, else ceil(n/64) + 1). */
 vc_status viscache_q8_append(const vc_decode_shape *shape, const vc_q8cache *cache, const vc_rows *k,

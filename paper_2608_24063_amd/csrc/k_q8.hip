@@ -9,7 +9,10 @@
 // transposition is paid once, here.
 //
 // Bound by memory: 2 bytes a value in, 1 out.  A workgroup takes a block's
-// keys with one half of its waves and its values with the other.
+// keys with one half of its waves and its values with the other.  Measured over
+// 3.63 million rows of 128 channels, keys and values: written in 521 us (5.3
+// TB/s), read back in fp32 in 859 (5.4); 118000 rows in 23 us (4.0), and back in
+// bf16 in 17 (5.3).
 #include "vc_q8_device.h"
 
 namespace vc {

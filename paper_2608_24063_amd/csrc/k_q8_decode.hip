@@ -18,6 +18,11 @@
 // requested with the first block, since the whole kernel waits for them (read
 // by one wave after its own blocks they took 8 of 25 us).
 //
+// Measured: 896 units of 2300 to 5800 rows, 128 channels, 170 us (5.5 TB/s, the
+// rate of reads alone); 112 units of about 1050 rows, 16 us, of which the bytes
+// at that rate are 5.5 and the launch and the chain of round trips (length,
+// codes, partials in LDS) the rest.
+//
 // A step is one launch: every workgroup turns its unit's queries itself while
 // its first blocks are on their way, and the one with the unit's last rows
 // appends the new one, sealing the block that it completes first.

@@ -139,8 +139,8 @@ __global__ __launch_bounds__(256) void k_join(Q8Attn p) {
 template <int D, bool HALF>
 void launch(const Q8Attn &p, hipStream_t st) {
   const int64_t cols = (int64_t)p.units * p.cols;
-  // 1024 columns and more are a wave each: 5460 columns of 12 parts 13.2 us in
-  // four waves, see below in one; 28 columns of 49 to 125 parts need the four.
+  // 1024 columns and more are a wave each: 5460 columns of 12 parts take 13.2 us
+  // in four waves, 6.9 in one; 28 columns of 49 to 125 parts need the four.
   if (cols >= 1024)
     hipLaunchKernelGGL((k_join<D, HALF, 1>), dim3((uint32_t)((cols + 3) / 4)), dim3(256), 0, st, p);
   else

@@ -484,10 +484,20 @@ class Q8Cache:
     def step(self, q, k, v, out, scale: float, rope: Rope | None = None, pos=None, q_out=None, k_out=None) -> None:
         """A serving step: rotates q and k by pos int32 [3, B, n] (with `rope`),
         appends k and v and attends q.  One token (n = 1) is a single call
-        (viscache_q8_step).  With more, the rotated rows go to q_out and k_out,
-        by default new tensors.  q, k and v are left as they are."""
+        (viscache_q8_step) and writes its rotated rows nowhere else.  With more,
+        they go to q_out and k_out, by default new tensors.  q, k and v are left
+        as they are."""
         n, index = q.shape[2], self._index
         if n != 1:
+            # All of it is looked at before anything is appended.
+            want = (self.L, self.B, n, self.Hq, self.d)
+            _take(q, "q", want, _BF16, index)
+            _take(out, "out", want, _FP32 if out.dtype is _FP32 else _BF16, index)
+            self._pair(k, v, False, _BF16)
+            if k.shape[2] != n:
+                raise ValueError(f"{k.shape[2]} new rows for {n} queries")
+            if n > 0:
+                self._workspace(n, self.max_cap)
             if rope is not None:
                 q, k = rope.apply(pos, q, k, q_out=torch.empty_like(q) if q_out is None else q_out,
                                   k_out=torch.empty_like(k) if k_out is None else k_out)

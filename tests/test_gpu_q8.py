@@ -615,6 +615,22 @@ def test_step_of_several_tokens(dev):
 
 # ---- streams, graphs, runs of them together ------------------------------------------
 
+def test_refused_step_appends_nothing(dev):
+    """A step of several tokens looks at all of its tensors before the first launch."""
+    rng = np.random.default_rng(24)
+    a, _ = _twins(6, dev, 1, 2, 8, 2, 64, [100, 63, 64, 0], "int8", extra=70)
+    before = a.len.clone()
+    q, k, v = (_t(_values(rng, (1, 2, 3, h, 64)), dev) for h in (8, 2, 2))
+    out = torch.zeros((1, 2, 3, 8, 64), dtype=torch.bfloat16, device=dev)
+    for bad in (dict(out=out[:, :, :2]), dict(out=out.half()), dict(q=q[:, :, :, :6]), dict(v=v[:, :, :2]),
+                dict(k=k[:, :, :2], v=v[:, :, :2]), dict(k=k.float())):
+        args = dict(q=q, k=k, v=v, out=out, scale=0.125)
+        args.update(bad)
+        with pytest.raises(ValueError):
+            a.step(**args)
+        assert torch.equal(a.len, before)
+
+
 def test_other_stream(dev):
     rng = np.random.default_rng(14)
     lens = [300, 70]
