@@ -44,8 +44,6 @@ __global__ __launch_bounds__(256) void k_join(Q8Attn p) {
   const int grp = w % WPC * GPW + lane / TPG, ch = lane % TPG * 4;
   const int g = u % p.Hkv, lb = u / p.Hkv, b = lb % p.B;
   const int cnt_ = p.count ? ldg(p.count + b) : p.n;
-  int2 tiles = make_int2(0, 0);
-  if (p.npmax == 1 && p.count) tiles = count_tiles(p, b, lane);
   if (cg >= (int64_t)p.units * p.cols || col >= min(max(cnt_, 0), p.n) * p.G) return;
   int64_t at;  // part 0 of the column
   int ns;
@@ -60,13 +58,9 @@ __global__ __launch_bounds__(256) void k_join(Q8Attn p) {
     }
     at = (int64_t)u * p.npmax * p.qcols + col;
   } else {
-    int64_t tile = (int64_t)u * p.nqt;
-    ns = p.ns;
-    if (p.count) {  // as share_of has them
-      ns = splits_of(p, tiles.x, (uint32_t)p.wgs);
-      tile = ((int64_t)(lb / p.B) * tiles.x + tiles.y) * p.Hkv + (int64_t)g * tiles_of(p, b);
-    }
-    at = (tile + col / p.qcols) * ns * p.qcols + col % p.qcols;
+    const u32x2 v = ld8(reinterpret_cast<const uint32_t *>(p.np) + 2 * (u * p.nqt + col / p.qcols));
+    ns = (int)v.y;
+    at = (int64_t)v.x * p.qcols + col % p.qcols;
   }
   if (ns <= 1) return;  // written already
   Part t{kNegInf, 0.f, {0.f, 0.f, 0.f, 0.f}};

@@ -84,15 +84,10 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt8(Q8Attn p) {
   __shared__ Values<D> tv[2] __attribute__((aligned(16)));
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int ln = lane & 31, hf = lane >> 5;
-  // Workgroups of a unit follow each other on one XCD and share its L2.
-  const uint32_t id = xcd_block(blockIdx.x, gridDim.x);
-  const Share sh = share_of(p, id, (uint32_t)p.wgs, lane);
+  const Share sh = share_of(p, blockIdx.x, lane);
   const int u = sh.u, qt = sh.qt, sp = sh.sp, ns = sh.ns;
   if (u < 0) return;
-  const int b = u / p.Hkv % p.B;
-  const int len = rows_held(ldg(p.c.len + u), ldg(p.c.cap + u));
-  const int cnt = p.count ? min(max(ldg(p.count + b), 0), p.n) : p.n;
-  const int cols = cnt * p.G;
+  const int len = sh.len, cnt = sh.cnt, cols = cnt * p.G;
   const int c0 = qt * p.qcols;
   if (c0 >= cols) return;
   const int cl = min(c0 + p.qcols, cols) - 1;  // last column of the workgroup
@@ -105,33 +100,13 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt8(Q8Attn p) {
   const int end = rows_seen(min(col, cl));
   const int wmin = rows_seen(min(c0 + 32 * w, cl));  // fewest rows a column of the wave sees
   const bool live = c0 + 32 * w <= cl;  // the wave has columns (the others only stage)
-  const int64_t blk0 = ldg(p.c.row_off + u) / kQ8Block;
+  const int64_t blk0 = sh.blk0;
   const int nsealed = len / kQ8Block;
   const int g = u % p.Hkv, lb = u / p.Hkv;
   auto row_of = [&](const RowsDesc &r, int cc) {
     return (int64_t)(lb / p.B) * r.layer + (int64_t)(lb % p.B) * r.seq + (int64_t)(cc / p.G) * r.token +
            (int64_t)(g * p.G + cc % p.G) * r.head;
   };
-
-  f16x8 q[KS];
-  float cq;
-  {
-    const uint16_t *qp = reinterpret_cast<const uint16_t *>(p.q.base) + row_of(p.q, min(col, cl));
-    u32x4 x[KS];
-    uint32_t mag = 0u;
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      x[s] = ld16(qp + 16 * s + 8 * hf);
-      mag = max_mag(max_mag(max_mag(max_mag(mag, x[s].x), x[s].y), x[s].z), x[s].w);
-    }
-    uint32_t mm = max(mag & 0xFFFFu, mag >> 16);
-    mm = max(mm, (uint32_t)__shfl_xor((int)mm, 32, 64));
-    const float qs = open_scale(mm);
-    cq = p.sc * qs;
-    const float inv = 1.f / qs;
-#pragma unroll
-    for (int s = 0; s < KS; ++s) q[s] = half8_of_bf16(x[s], inv);
-  }
 
   u32x4 rk[IT], rv[IT];
   auto fetch_k = [&](int t) {
@@ -144,6 +119,32 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt8(Q8Attn p) {
 #pragma unroll
     for (int it = 0; it < IT; ++it) rv[it] = ld16(v + 16 * (kPart ? min(tid, kItems - 1) : tid + NT * it));
   };
+  // The queries' requests and the first block's, before anything waits.
+  const int Tc = max(min(t0 + T, nsealed) - t0, 0);  // sealed blocks
+  f16x8 q[KS];
+  float cq;
+  {
+    const uint16_t *qp = reinterpret_cast<const uint16_t *>(p.q.base) + row_of(p.q, min(col, cl));
+    u32x4 x[KS];
+    uint32_t mag = 0u;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) x[s] = ld16(qp + 16 * s + 8 * hf);
+    if (Tc > 0) {
+      fetch_k(t0);
+      fetch_v(t0);
+    }
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+      mag = max_mag(max_mag(max_mag(max_mag(mag, x[s].x), x[s].y), x[s].z), x[s].w);
+    uint32_t mm = max(mag & 0xFFFFu, mag >> 16);
+    mm = max(mm, (uint32_t)__shfl_xor((int)mm, 32, 64));
+    const float qs = open_scale(mm);
+    cq = p.sc * qs;
+    const float inv = 1.f / qs;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) q[s] = half8_of_bf16(x[s], inv);
+  }
+
   auto stage_k = [&](int buf) {
     if (kPart && tid >= kItems) return;
 #pragma unroll
@@ -166,7 +167,6 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt8(Q8Attn p) {
   };
   // The open block: bf16 rows scaled by their powers of two, zeros past its end.
   const int orows = len - nsealed * kQ8Block;
-  const int Tc = max(min(t0 + T, nsealed) - t0, 0);  // sealed blocks
   auto open_rows = [&](const uint16_t *tail, const float *scale, auto put) {
     const float inv = 1.f / ldg(scale + blk0 + nsealed);
     for (int e = tid; e < kQ8Block * D / 8; e += NT) {
@@ -308,8 +308,6 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt8(Q8Attn p) {
   auto scale_at = [&](const float *scale, int i) { return ldg(scale + blk0 + t0 + min(i, Tc - 1)); };
 
   if (Tc > 0) {
-    fetch_k(t0);
-    fetch_v(t0);
     stage_k(0);
     fetch_k(t0 + min(1, Tc - 1));
     __syncthreads();
@@ -367,6 +365,9 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt8(Q8Attn p) {
   }
   l = sum_halves(l);
   if (F32) l *= 16384.f;  // the factor that P's two parts carry
+  // (Here, since a store before the loop would keep its scales out of scalar loads.)
+  if (p.ns > 1 && sp == 0 && tid == 0)
+    st8(reinterpret_cast<uint32_t *>(p.np) + 2 * (u * p.nqt + qt), u32x2{(uint32_t)sh.id, (uint32_t)ns});
   if (col > cl) return;
   if (ns == 1) {
     const float inv = l > 0.f ? 1.f / l : 0.f;
@@ -386,7 +387,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt8(Q8Attn p) {
       }
     return;
   }
-  const int64_t at = (int64_t)id * p.qcols + 32 * w + ln;
+  const int64_t at = (int64_t)sh.id * p.qcols + 32 * w + ln;
   if (F32) {
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb)

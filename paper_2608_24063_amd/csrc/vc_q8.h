@@ -8,6 +8,8 @@
 namespace vc {
 
 constexpr int kQ8Block = 64;  // rows that share a scale (VC_Q8_BLOCK)
+constexpr int kQ8SplitTiles = 256;  // most column tiles of a prompt that are cut along their rows
+constexpr int kQ8SplitBlocks = 4;   // fewest blocks a cut leaves together
 
 // Row (l, b, i, h) of a strided tensor starts at base + l*layer + b*seq +
 // i*token + h*head elements.
@@ -58,19 +60,19 @@ struct Q8Attn {
   float sc;              // scale * log2(e)
   // One token at a time (cols <= 16): pieces of `piece` blocks, at most npmax
   // a unit (qcols 16).  Prompts (npmax 1): nqt column tiles of qcols columns,
-  // each in ns key splits, or, where counts leave tiles empty, as many (up to
-  // nsmax) as the launch's workgroups allow.
+  // each in as many key splits as the launch's workgroups allow (ns 1: whole).
   int32_t piece, npmax;
-  int32_t qcols, nqt, ns, nsmax;
+  int32_t qcols, nqt, ns;
   float *part_o;         // partial results: [part][qcols][d], [part][qcols]
   float2 *part_ml;
   // A step (step = 1; else attention alone): the new rows, the rotation of queries and
-  // new keys, and, where units are cut, the units' pieces for the join, which
-  // then advances the lengths (bit 30: by a row).
+  // new keys.
   int32_t step;
   RowsDesc k, v;
   RopeTable rope;
   const int32_t *pos;    // [3][B]
+  // For the join: a step's pieces of each unit, whose lengths it then advances
+  // (bit 30: by a row); a prompt's first part and number of parts of each tile.
   int32_t *np;
 };
 

@@ -72,7 +72,7 @@ Q8Cache bind(const vc_q8cache *c) {
 // How an attention call is cut, and what it needs of the workspace: partial O,
 // (max, sum), and the units' pieces of a step.
 struct Cut {
-  int32_t piece = 0, npmax = 1, qcols = 0, nqt = 0, ns = 1, nsmax = 1;
+  int32_t piece = 0, npmax = 1, qcols = 0, nqt = 0, ns = 1;
   int64_t wgs = 0, slots = 0;  // workgroups; columns of partial results
   size_t ml = 0, np = 0, total = 0;
 };
@@ -104,15 +104,17 @@ bool attend_cut(const vc_decode_shape *s, int32_t n, int32_t max_rows, Cut &c) {
     if (tiles >= kMaxWg) return false;
     const int64_t resident = c.qcols == 256 ? 256 : 512;
     c.nqt = (int32_t)nqt;
-    c.nsmax = (int32_t)std::max<int64_t>(1, nt / 4);
-    c.ns = (int32_t)std::max<int64_t>(1, std::min<int64_t>(resident / tiles, c.nsmax));
-    c.wgs = tiles * c.ns;
+    // Workgroups that the card holds at once share the tiles' rows where that
+    // is two a tile or more.
+    c.ns = tiles * 2 <= resident && nt >= 2 * kQ8SplitBlocks ? 2 : 1;
+    c.wgs = c.ns > 1 ? std::min(resident, tiles * (nt / kQ8SplitBlocks)) : tiles;
     c.slots = c.ns > 1 ? c.wgs * c.qcols : 0;
   }
   if (c.wgs >= kMaxWg || (c.slots && units * cols >= 2 * kMaxWg)) return false;  // (the join: 256 threads a column)
   c.ml = align_up(sizeof(float) * (size_t)c.slots * (size_t)s->d);
   c.np = c.ml + align_up(sizeof(float2) * (size_t)c.slots);
-  c.total = std::max(c.np + (cols <= kCols ? align_up(sizeof(int32_t) * (size_t)units) : 0), kAlign);
+  const int64_t words = cols <= kCols ? units : c.ns > 1 ? 2 * units * c.nqt : 0;
+  c.total = std::max(c.np + align_up(sizeof(int32_t) * (size_t)words), kAlign);
   return true;
 }
 
@@ -185,7 +187,7 @@ vc_status attend_plan(const vc_decode_shape *s, const vc_q8cache *c, const vc_ro
   p.sc = scale * 1.4426950408889634f;
   p.wgs = (int32_t)cut.wgs;
   p.piece = cut.piece; p.npmax = cut.npmax;
-  p.qcols = cut.qcols; p.nqt = cut.nqt; p.ns = cut.ns; p.nsmax = cut.nsmax;
+  p.qcols = cut.qcols; p.nqt = cut.nqt; p.ns = cut.ns;
   uint8_t *ws = static_cast<uint8_t *>(workspace);
   p.part_o = reinterpret_cast<float *>(ws);
   p.part_ml = reinterpret_cast<float2 *>(ws + cut.ml);

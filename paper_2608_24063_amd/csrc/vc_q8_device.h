@@ -224,62 +224,102 @@ __device__ __forceinline__ int64_t unit_base(const RowsDesc &r, const int64_t *u
   return (int64_t)(lb / B) * r.layer + (int64_t)(lb % B) * r.seq + (int64_t)g * r.head;
 }
 
-// Which column tile and key split a prompt's workgroup takes, and where the
-// partial results of a tile's splits begin.
+// Sum over a wave.
+__device__ __forceinline__ float wave_sum(float x) {
+  const auto bits = [&] { return (int)__float_as_uint(x); };
+  // (shifts and broadcasts as in wave_incl_scan)
+  x += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, bits(), 0x111, 0xF, 0xF, false));
+  x += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, bits(), 0x112, 0xF, 0xF, false));
+  x += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, bits(), 0x114, 0xF, 0xF, false));
+  x += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, bits(), 0x118, 0xF, 0xF, false));
+  x += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, bits(), 0x142, 0xA, 0xF, false));
+  x += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, bits(), 0x143, 0xC, 0xF, false));
+  return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), 63));
+}
+
+// Which column tile and key split a prompt's workgroup takes, of how many, and
+// what the tile's unit is.
 struct Share {
   int u, qt, sp, ns;  // unit (-1: nothing to do), tile, split of ns
+  int id;             // where its partial results go
+  int len, cnt;       // rows held, queries
+  int64_t blk0;       // the unit's first block
 };
 
-// Column tiles of sequence b.
-__device__ __forceinline__ int tiles_of(const Q8Attn &p, int b) {
-  const int cnt = p.count ? min(max(ldg(p.count + b), 0), p.n) : p.n;
-  return (cnt * p.G + p.qcols - 1) / p.qcols;
-}
-
-// Tiles of all sequences of a layer and head, and of those before sequence
-// `b`; every lane of the wave takes part.
-__device__ __forceinline__ int2 count_tiles(const Q8Attn &p, int b, int lane) {
-  int all = 0, before = 0;
-  for (int b0 = 0; b0 < p.B; b0 += 64) {
-    const int q = b0 + lane < p.B ? tiles_of(p, b0 + lane) : 0;
-    all += __builtin_amdgcn_readlane((int)wave_incl_scan((uint32_t)q), 63);
-    before += __builtin_amdgcn_readlane((int)wave_incl_scan((uint32_t)(b0 + lane < b ? q : 0)), 63);
+// Workgroup `bid` of a prompt: tiles in the order of their units, splits
+// innermost, those of a unit on one XCD (they share its L2); every lane of the
+// wave takes part.  Where few tiles are cut along
+// their rows, as many blocks go to each workgroup as make no more splits than
+// workgroups: sequences without queries take none, longer units take more.  (us,
+// with as many splits for every tile and so: four sequences of 3000 to 12801
+// rows with 40 queries each 56.5, 47.8, with up to 40 44.6, 36.5; three of 9001 to
+// 12801 with up to 65 51.6, 48.9; one of 12544 with 30 23.7, 24.0, with 1024 202,
+// 205.)
+__device__ __forceinline__ Share share_of(const Q8Attn &p, uint32_t bid, int lane) {
+  auto queries = [&](int u) { return p.count ? min(max(ldg(p.count + u / p.Hkv % p.B), 0), p.n) : p.n; };
+  if (p.ns == 1) {
+    const int id = (int)xcd_block(bid, (uint32_t)p.wgs), u = id / p.nqt;
+    return Share{u, id % p.nqt, 0, 1, id, rows_held(ldg(p.c.len + u), ldg(p.c.cap + u)), queries(u),
+                 ldg(p.c.row_off + u) / kQ8Block};
   }
-  return make_int2(all, before);
-}
-// Key splits where `all` tiles a layer and head are not empty.
-__device__ __forceinline__ int splits_of(const Q8Attn &p, int all, uint32_t wgs) {
-  const int64_t live = (int64_t)all * p.L * p.Hkv;
-  return (int)min(max((int64_t)wgs / max(live, (int64_t)1), (int64_t)1), (int64_t)p.nsmax);
-}
-
-// Workgroup `id` of `wgs`: tiles in the order of their units, splits innermost.
-// With counts, the empty tiles' workgroups go to the others as further splits.
-__device__ __forceinline__ Share share_of(const Q8Attn &p, uint32_t id, uint32_t wgs, int lane) {
-  if (!p.count || p.ns == 1) {
-    const uint32_t per = (uint32_t)(p.nqt * p.ns), rest = id % per;
-    return Share{(int)(id / per), (int)(rest / (uint32_t)p.ns), (int)(rest % (uint32_t)p.ns), p.ns};
+  // Lane: tiles K lane .. K lane + K - 1, by their blocks.
+  constexpr int KM = kQ8SplitTiles / 64;
+  const int tiles = p.units * p.nqt, K = (tiles + 63) / 64;
+  int nb[KM], held[KM], cnt[KM];
+  int64_t off[KM];
+  float all = 0.f;
+#pragma unroll
+  for (int k = 0; k < KM; ++k) {
+    if (k >= K) break;  // uniform
+    const int t = K * lane + k, u = (int)((uint32_t)min(t, tiles - 1) / (uint32_t)p.nqt);
+    held[k] = rows_held(ldg(p.c.len + u), ldg(p.c.cap + u));
+    cnt[k] = queries(u);
+    off[k] = ldg(p.c.row_off + u);
+    const int c0 = (t - u * p.nqt) * p.qcols, cl = min(c0 + p.qcols, cnt[k] * p.G) - 1;
+    const int seen = min(p.causal ? held[k] - cnt[k] + 1 + (int)((uint32_t)max(cl, 0) / (uint32_t)p.G) : held[k], p.max_rows);
+    nb[k] = t < tiles && cl >= c0 ? max((seen + kQ8Block - 1) / kQ8Block, 1) : 0;
+    all += (float)nb[k];
   }
-  const int all = count_tiles(p, 0, lane).x;
-  const int ns = splits_of(p, all, wgs);
-  const int tile = (int)(id / (uint32_t)ns), per = all * p.Hkv;
-  Share s{-1, 0, (int)(id % (uint32_t)ns), ns};
-  if (per == 0 || tile >= per * p.L) return s;
-  const int l = tile / per, r = tile % per, x = r / p.Hkv;  // x: which of the sequences' tiles
-  int base = 0;
-  for (int b0 = 0; b0 < p.B; b0 += 64) {
-    const int q = b0 + lane < p.B ? tiles_of(p, b0 + lane) : 0;
-    const int inc = (int)wave_incl_scan((uint32_t)q), a = base + inc - q;
-    const uint64_t hit = __builtin_amdgcn_ballot_w64(a <= x && x < a + q);
-    if (hit) {
-      const int src = __builtin_ctzll(hit);
-      const int qb = __builtin_amdgcn_readlane(q, src), rr = r - p.Hkv * __builtin_amdgcn_readlane(a, src);
-      s.u = (l * p.B + b0 + src) * p.Hkv + rr / qb;
-      s.qt = rr % qb;
-    }
-    base += __builtin_amdgcn_readlane(inc, 63);
+  all = wave_sum(all);
+  // The fewest blocks a split: sum ceil(nb / q) <= wgs, which q >= sum nb /
+  // (wgs - tiles) always meets.
+  int lo = max(kQ8SplitBlocks, (int)(all / (float)p.wgs));
+  int hi = max(lo, (int)(all * 1.0001f / (float)(p.wgs - tiles)) + 1);
+  auto splits = [&](int q) {
+    int s = 0;
+#pragma unroll
+    for (int k = 0; k < KM; ++k)
+      if (k < K) s += (int)((uint32_t)(nb[k] + q - 1) / (uint32_t)q);
+    return s;
+  };
+  while (lo < hi) {
+    const int q = lo + (hi - lo) / 2;
+    if (__builtin_amdgcn_readlane((int)wave_incl_scan((uint32_t)splits(q)), 63) <= p.wgs)
+      hi = q;
+    else
+      lo = q + 1;
   }
-  return s;
+  const int own = splits(lo);
+  int first = (int)wave_incl_scan((uint32_t)own);
+  const uint32_t used = (uint32_t)__builtin_amdgcn_readlane(first, 63);
+  Share s{-1, 0, 0, 0, 0, 0, 0, 0};
+  if (bid >= used) return s;
+  const int id = (int)xcd_block(bid, used);
+  first -= own;
+  const uint64_t hit = __builtin_amdgcn_ballot_w64(first <= id && id < first + own);
+  int t = 0;
+#pragma unroll
+  for (int k = 0; k < KM; ++k) {
+    if (k >= K) break;
+    const int ns = (int)((uint32_t)(nb[k] + lo - 1) / (uint32_t)lo);
+    if (first <= id && id < first + ns) t = K * lane + k, s = Share{0, 0, id - first, ns, id, held[k], cnt[k], off[k]};
+    first += ns;
+  }
+  const int src = __builtin_ctzll(hit);
+  auto of = [&](int x) { return __builtin_amdgcn_readlane(x, src); };
+  t = of(t);
+  const uint64_t at = (uint32_t)of((int)s.blk0) | (uint64_t)(uint32_t)of((int)(s.blk0 >> 32)) << 32;
+  return Share{t / p.nqt, t % p.nqt, of(s.sp), of(s.ns), id, of(s.len), of(s.cnt), (int64_t)at / kQ8Block};
 }
 
 }  // namespace vc
