@@ -439,6 +439,22 @@ def test_ragged_batches_cut_along_their_rows(dev, B, Hkv, G, n, rows, fp32):
     assert (none == 7.0).all()
 
 
+@pytest.mark.parametrize("L,B,Hkv,G,n,d", [(1, 40, 2, 4, 20, 64), (1, 3, 2, 8, 70, 128), (2, 25, 5, 16, 2, 64)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_unlike_lengths_cut_along_their_rows(dev, L, B, Hkv, G, n, d, causal):
+    """Units of no row to thousands whose rows are shared out, with one tile or
+    several a unit, with and without counts, and with a bound below the longest."""
+    rng = np.random.default_rng(B + causal)
+    lens = [int(x) for x in np.exp(rng.uniform(0, np.log(4000), L * B * Hkv))]
+    lens[0], lens[1], lens[-1], lens[-2] = 4000, 0, 1, 64
+    c, K, V = _filled(rng, dev, L, B, G * Hkv, Hkv, d, lens, "e4m3")
+    q = ref.bf16(rng.standard_normal((L, B, n, G * Hkv, d)))
+    for counts, most in ((None, 4000), (None, 1500), ([int(x) for x in rng.integers(0, n + 1, B)], 4000)):
+        out = _run_attend(c, q, dev, False, d ** -0.5, counts, causal, max_rows=most)
+        _check_attend(out, q, K, V, lens, L, B, G * Hkv, Hkv, d ** -0.5, counts or [n] * B, causal, most,
+                      sample=[0, n - 1])
+
+
 def test_parts_of_almost_nothing(dev):
     """A split whose values are zero but for rows of almost no weight: its part is
     tiny, not lost and not infinite."""
