@@ -120,12 +120,15 @@ __device__ __forceinline__ void turn(float &x1, float &x2, float2 cs) {
   x2 = fmaf(b, cs.x, a * cs.y);
 }
 // scale (cos, sin) of the angle of a position: reduced in 64 bits as a number
-// of turns, then 32.
+// of turns, then 32; what that rounding leaves of the angle (e, below 2^-23)
+// turns the result.
 __device__ __forceinline__ float2 turn_of(const RopeTable &t, int i, int pos) {
-  const double a = (double)pos * t.turns[i];
+  double a = (double)pos * t.turns[i];
+  a -= rint(a);
+  const float h = (float)a, e = 6.2831853f * (float)(a - h);
   float s, c;
-  sincospif(2.f * (float)(a - rint(a)), &s, &c);
-  return make_float2(c * t.scale, s * t.scale * t.sgn);
+  sincospif(2.f * h, &s, &c);
+  return make_float2(fmaf(-s, e, c) * t.scale, fmaf(c, e, s) * t.scale * t.sgn);
 }
 // The axis of frequency i.
 __device__ __forceinline__ int axis_of(const RopeTable &t, int i) {
