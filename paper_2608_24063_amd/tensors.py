@@ -243,8 +243,10 @@ def _refuse(t, name, shape, typ, index):
 
 def _take(t: torch.Tensor, name: str, shape, typ, index: int, head_major: bool = False) -> bytes:
     """The vc_rows of a tensor [L, B, n, H, d] ([L, B, H, n, d] with head_major) of
-    this shape, type and GPU, its rows contiguous."""
-    if t.shape != shape or t.dtype is not typ or t.get_device() != index or index < 0:
+    this type and GPU and, unless that is known (None), this shape, its rows
+    contiguous."""
+    if (shape is not None and t.shape != shape) or t.dtype is not typ or t.get_device() != index or index < 0:
+        shape = t.shape if shape is None else shape
         _refuse(t, name, shape, typ, index)
     s = t.stride()
     if s[4] != 1:
@@ -307,28 +309,31 @@ class Rope:
         if ref is None:
             raise ValueError("nothing to rotate")
         typ, index = ref.dtype, ref.get_device()
-        L, B, n, _, d = ref.shape
+        L, B, n, Hq, d = was = ref.shape
         if (typ is not _BF16 and typ is not _FP32) or d != self.d:
             _refuse(ref, "q" if q is not None else "k", ref.shape[:-1] + (self.d,), "bf16 or fp32", max(index, 0))
         qi = qo = ki = ko = None
-        Hq = Hkv = 0
+        Hkv = Hq  # of the one that there is
         if q is not None:
-            qi = _take(q, "q", ref.shape, typ, index)
-            qo = qi if q_out is None else _take(q_out, "q_out", q.shape, typ, index)
-            Hq = q.shape[3]
+            qi = _take(q, "q", None, typ, index)
+            qo = qi if q_out is None else _take(q_out, "q_out", was, typ, index)
         if k is not None:
-            Hkv = k.shape[3]
-            ki = _take(k, "k", (L, B, n, Hkv, d), typ, index)
-            ko = ki if k_out is None else _take(k_out, "k_out", k.shape, typ, index)
+            if k is not ref:
+                was = k.shape
+                Hkv = was[3] if len(was) == 5 else 0
+                if was != (L, B, n, Hkv, d):
+                    _refuse(k, "k", (L, B, n, "heads", d), typ, index)
+            ki = _take(k, "k", None, typ, index)
+            ko = ki if k_out is None else _take(k_out, "k_out", was, typ, index)
         cnt = _ints(count, "count", (B,), index)
         at = _ints(pos, "pos", (3, B, n), index)
         q_out, k_out = q if q_out is None else q_out, k if k_out is None else k_out
-        if ref.numel() == 0:
+        if L == 0 or B == 0 or n == 0:
             return q_out, k_out
-        key = (L, B, Hq or Hkv, Hkv or Hq)
+        key = (L, B, Hq, Hkv)
         shape = self._shapes.get(key)
         if shape is None:
-            shape = self._shapes[key] = vc_decode_shape(B, L, Hq or Hkv, Hkv or Hq, d)
+            shape = self._shapes[key] = vc_decode_shape(B, L, Hq, Hkv, d)
         _enqueue("viscache_rope", self._f, index, ctypes.addressof(shape),
                  self._address[typ is _FP32][bool(inverse)], n, at, cnt, qi, qo, ki, ko)
         return q_out, k_out

@@ -176,3 +176,30 @@ def test_graph_replays(dev):
         r.apply(pos, q=x, q_out=want)
         torch.cuda.synchronize()
         assert torch.equal(out, want), t
+
+
+def test_refusals_and_empty(dev):
+    """Tensors that do not belong together are refused before a launch; no tokens
+    are nothing to do, no heads an error."""
+    import paper_2608_24063_amd as vc
+    from paper_2608_24063_amd.tensors import Rope
+    rope = Rope(64)
+    z = lambda *s, t=torch.bfloat16: torch.ones(s, dtype=t, device=dev)  # noqa: E731
+    pos = torch.ones((3, 2, 5), dtype=torch.int32, device=dev)
+    q, k = z(1, 2, 5, 4, 64), z(1, 2, 5, 2, 64)
+    for bad in (dict(k=z(1, 2, 4, 2, 64)), dict(k=z(2, 5, 2, 64)), dict(k=z(1, 2, 5, 2, 128)),
+                dict(k=z(1, 2, 5, 2, 64, t=torch.float32)), dict(q_out=z(1, 2, 5, 2, 64)), dict(k_out=z(1, 2, 5, 4, 64)),
+                dict(q=z(1, 2, 5, 4, 128)), dict(q=z(1, 2, 5, 4, 64, t=torch.float16)), dict(k=k.cpu()),
+                dict(q=z(1, 2, 5, 64, 4).transpose(3, 4)), dict(pos=pos[:, :, :4]), dict(pos=pos.long()),
+                dict(count=torch.ones(3, dtype=torch.int32, device=dev))):
+        args = dict(pos=pos, q=q, k=k)
+        args.update(bad)
+        with pytest.raises(ValueError):
+            rope.apply(**args)
+    with pytest.raises(vc.VisCacheError):
+        rope.apply(pos, q, z(1, 2, 5, 0, 64))
+    with pytest.raises(vc.VisCacheError):
+        rope.apply(None, q, k)
+    torch.cuda.synchronize()
+    assert (q == 1).all() and (k == 1).all()
+    rope.apply(pos[:, :, :0].contiguous(), z(1, 2, 0, 4, 64), z(1, 2, 0, 2, 64))
