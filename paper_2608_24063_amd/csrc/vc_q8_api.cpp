@@ -85,15 +85,17 @@ bool attend_cut(const vc_decode_shape *s, int32_t n, int32_t max_rows, Cut &c) {
   if (cols <= kCols) {
     // Units are cut into pieces of a multiple of four blocks (one per wave and
     // turn), as many as make about 256 workgroups, one a CU, and not where that
-    // were two a unit.  (us: 4 units of 12544 rows in pieces of 4, 8, 16, 48 blocks
-    // 12.4, 13.3, 15.7, 26.1; 32 of 2300 to 5800 rows in 4, 8, 12, 24: 21.1, 19.2,
-    // 16.4, 19.7; 112 of 620 to 1490 in 12 and uncut 17.1, 16.2; 160 of 800 to
-    // 1900 in 20 and uncut 19.7, 18.5; 896 of 2300 to 5800 in 24, 48 and uncut
-    // 199, 198, 188.)
+    // were two a unit or three short ones, which save less than the join costs.
+    // (us: 4 units of 12544 rows in pieces of 4, 8, 16, 48 blocks 12.4, 13.3, 15.7,
+    // 26.1; 32 of 2300 to 5800 rows in 4, 8, 12, 24: 21.1, 19.2, 16.4, 19.7; 112 of
+    // 620 to 1490 in 12 and uncut 17.1, 16.2; 160 of 800 to 1900 in 20 and uncut
+    // 19.7, 18.5; 896 of 2300 to 5800 in 24, 48 and uncut 199, 198, 188; 8 of 9, 12,
+    // 16, 20 blocks in 4 10.3, 11.3, 11.3, 11.4, uncut 9.7, 10.8, 12.1, 13.4; 32 of
+    // them in 4 10.7, 11.6, 12.1, 12.7, uncut 9.8, 11.0, 12.2, 14.3.)
     const int64_t want = units * nt / 256;
     c.qcols = kCols;
     c.piece = (int32_t)std::min<int64_t>(std::max<int64_t>(4, (want + 3) / 4 * 4), int64_t(1) << 26);
-    if (nt <= 2 * (int64_t)c.piece) c.piece = (int32_t)nt;
+    if (nt <= std::max<int64_t>(2 * (int64_t)c.piece, 12)) c.piece = (int32_t)nt;
     c.npmax = (int32_t)((nt + c.piece - 1) / c.piece);
     c.wgs = units * c.npmax;
     c.slots = c.npmax > 1 ? c.wgs * kCols : 0;
