@@ -424,9 +424,12 @@ class Q8Cache:
 
     def _pair(self, k, v, head_major, typ):
         """The descriptors of keys and values [L, B, n, Hkv, d] (or [L, B, Hkv, n, d]), and n."""
-        n = k.shape[3 if head_major else 2]
+        was = k.shape
+        n = was[3 if head_major else 2]
         want = (self.L, self.B, self.Hkv, n, self.d) if head_major else (self.L, self.B, n, self.Hkv, self.d)
-        return (_take(k, "k", want, typ, self._index, head_major), _take(v, "v", want, typ, self._index, head_major), n)
+        if was != want:
+            _refuse(k, "k", want, typ, self._index)
+        return (_take(k, "k", None, typ, self._index, head_major), _take(v, "v", want, typ, self._index, head_major), n)
 
     def load_pruned(self, pc: "PruneCall") -> None:
         """Appends what pc.run() left in its outputs (bf16 values): every
@@ -474,10 +477,13 @@ class Q8Cache:
     def attend(self, q, out, scale: float, count=None, causal: bool = True, max_rows=None) -> None:
         """Attention of q bf16 [L, B, n, Hq, d] over the cache into out (bf16 or
         fp32, the same shape); count int32 [B]: the queries of each sequence."""
-        n = q.shape[2]
+        was = q.shape
+        n = was[2]
         want = (self.L, self.B, n, self.Hq, self.d)
+        if was != want:
+            _refuse(q, "q", want, _BF16, self._index)
         fp32 = out.dtype is _FP32
-        qr, outr = _take(q, "q", want, _BF16, self._index), _take(out, "out", want, _FP32 if fp32 else _BF16, self._index)
+        qr, outr = _take(q, "q", None, _BF16, self._index), _take(out, "out", want, _FP32 if fp32 else _BF16, self._index)
         cnt = _ints(count, "count", (self.B,), self._index)
         if n == 0:
             return
