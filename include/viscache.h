@@ -505,7 +505,10 @@ size_t viscache_q8_attend_workspace_bytes(const vc_decode_shape *shape, int32_t 
  * with K_t and V_t as they read back (before any rounding to bf16).  q: bf16; out:
  * bf16 (out_fp32 = 0) or fp32; both indexed by the query head.  Logits, maxima and
  * sums are fp32.  Weights: with n * Hq/Hkv <= 16 or fp32 outputs, 22 bits of them,
- * and steps of 2^-38 of the query's largest where they are less than 2^-14 of it.  A query that
+ * and steps of 2^-38 of the query's largest where they are less than 2^-14 of it.
+ * With more columns and bf16 outputs each weight is rounded to fp16 before it
+ * meets its value: 2^-12 of itself, or 2^-33 of the query's largest weight times
+ * value scale where that is more; a caller that needs more asks for fp32 outputs.  A query that
  * sees no row gives zeros; rows i >= c of out are left as they were.  max_rows
  * bounds every len (rows past it are not attended).  One launch, and a second
  * that joins partial results where few (unit, query) tiles are cut along their

@@ -34,7 +34,7 @@ __device__ __forceinline__ void add(Part &a, const Part &b) {
 
 // WPC waves take a column: four where columns are few and parts many, one
 // where the columns fill the chip.
-template <int D, bool HALF, int WPC>
+template <int D, int WPC>
 __global__ __launch_bounds__(256) void k_join(Q8Attn p) {
   constexpr int TPG = D / 4, GPW = 64 / TPG, NG = GPW * WPC, U = 4;
   __shared__ Part sp[WPC][TPG];
@@ -71,17 +71,11 @@ __global__ __launch_bounds__(256) void k_join(Q8Attn p) {
     for (int k = 0; k < U; ++k) {
       const int64_t a = at + (int64_t)min(s0 + k * NG, ns - 1) * p.qcols;
       ml[k] = ldg(p.part_ml + a);
-      if (HALF) {
-        const f16x4 h = __builtin_bit_cast(f16x4, ld8(reinterpret_cast<const _Float16 *>(p.part_o) + a * D + ch));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[k][i] = (float)h[i];
-      } else {
-        const u32x4 v = ld16(p.part_o + a * D + ch);
-        x[k][0] = __uint_as_float(v.x);
-        x[k][1] = __uint_as_float(v.y);
-        x[k][2] = __uint_as_float(v.z);
-        x[k][3] = __uint_as_float(v.w);
-      }
+      const u32x4 v = ld16(p.part_o + a * D + ch);
+      x[k][0] = __uint_as_float(v.x);
+      x[k][1] = __uint_as_float(v.y);
+      x[k][2] = __uint_as_float(v.z);
+      x[k][3] = __uint_as_float(v.w);
     }
     float M = t.M;
 #pragma unroll
@@ -130,25 +124,24 @@ __global__ __launch_bounds__(256) void k_join(Q8Attn p) {
     st8(reinterpret_cast<uint16_t *>(p.out.base) + to, u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])});
 }
 
-template <int D, bool HALF>
+template <int D>
 void launch(const Q8Attn &p, hipStream_t st) {
   const int64_t cols = (int64_t)p.units * p.cols;
   // 1024 columns and more are a wave each: 5460 columns of 12 parts take 13.2 us
   // in four waves, 6.9 in one; 28 columns of 49 to 125 parts need the four.
   if (cols >= 1024)
-    hipLaunchKernelGGL((k_join<D, HALF, 1>), dim3((uint32_t)((cols + 3) / 4)), dim3(256), 0, st, p);
+    hipLaunchKernelGGL((k_join<D, 1>), dim3((uint32_t)((cols + 3) / 4)), dim3(256), 0, st, p);
   else
-    hipLaunchKernelGGL((k_join<D, HALF, 4>), dim3((uint32_t)cols), dim3(256), 0, st, p);
+    hipLaunchKernelGGL((k_join<D, 4>), dim3((uint32_t)cols), dim3(256), 0, st, p);
 }
 
 }  // namespace
 
 hipError_t launch_q8_join(const Q8Attn &p, hipStream_t st) {
-  const bool half = p.npmax == 1 && !p.fp32;  // a prompt's parts of bf16 outputs
   if (p.d == 128)
-    half ? launch<128, true>(p, st) : launch<128, false>(p, st);
+    launch<128>(p, st);
   else
-    half ? launch<64, true>(p, st) : launch<64, false>(p, st);
+    launch<64>(p, st);
   return hipGetLastError();
 }
 

@@ -15,9 +15,13 @@
 // scale goes into the exponent, p' = exp2(c s + log2 vs_b - m), m the running
 // maximum of the same quantity, and the sum takes it out again,
 // l += sum(p') / vs_b: O needs no pass of its own per block, and no block's p'
-// exceeds the range of fp16.  p' is one fp16 value (2^-12 relative, against the
-// output's 2^-9).  With fp32 outputs P is split in two fp16 parts and each
-// block's product is scaled into O in fp32.
+// exceeds the range of fp16.  p' is one fp16 value: 2^-12 of itself, and half of
+// fp16's smallest step, 2^-33 of the column's largest weight times value scale.
+// That is a choice of speed: the errors of a column's weights average out and
+// stay under the half step of a bf16 output (2^-9 of it and more), unless its
+// values cancel; a second part would make half as many products again.  With fp32
+// outputs P is split in two fp16 parts (22 bits) and each block's product is scaled
+// into O in fp32.  Sums, maxima, O and the partial results are fp32 in both.
 //
 // Measured: 2048 queries of 64 heads over 23040 rows, 128 channels, int8: 1340 to
 // 1410 us, 1.05 to 1.1 PFLOP/s, 0.9 of a large library product's rate.  Of a SIMD's
@@ -387,38 +391,13 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt8(Q8Attn p) {
     return;
   }
   const int64_t at = (int64_t)sh.id * p.qcols + 32 * w + ln;
-  if (F32) {
 #pragma unroll
-    for (int cb = 0; cb < CB; ++cb)
+  for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        st16(p.part_o + at * D + 32 * cb + 8 * i + 4 * hf,
-             u32x4{__float_as_uint(O[cb][4 * i]), __float_as_uint(O[cb][4 * i + 1]), __float_as_uint(O[cb][4 * i + 2]),
-                   __float_as_uint(O[cb][4 * i + 3])});
-  } else {
-    // Half the traffic: fp16 (2^-12 of the value), the column's largest brought
-    // to [2^14, 2^15) by a power of two 2^-k; (m, l) become (m + k, l 2^-k), so
-    // that the parts still join by 2^m.
-    float big = 0.f;
-#pragma unroll
-    for (int cb = 0; cb < CB; ++cb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) big = fmaxf(big, fabsf(O[cb][i]));
-    big = max_halves(big);
-    const int k = big > 0.f ? max((int)(__float_as_uint(big) >> 23) - 127 - 14, -126) : 0;
-    const float down = ldexpf(1.f, -k);
-    m += (float)k;
-    l *= down;
-    _Float16 *to = reinterpret_cast<_Float16 *>(p.part_o) + at * D;
-#pragma unroll
-    for (int cb = 0; cb < CB; ++cb)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const f16x4 h = {(_Float16)(O[cb][4 * i] * down), (_Float16)(O[cb][4 * i + 1] * down),
-                         (_Float16)(O[cb][4 * i + 2] * down), (_Float16)(O[cb][4 * i + 3] * down)};
-        st8(to + 32 * cb + 8 * i + 4 * hf, __builtin_bit_cast(u32x2, h));
-      }
-  }
+    for (int i = 0; i < 4; ++i)
+      st16(p.part_o + at * D + 32 * cb + 8 * i + 4 * hf,
+           u32x4{__float_as_uint(O[cb][4 * i]), __float_as_uint(O[cb][4 * i + 1]), __float_as_uint(O[cb][4 * i + 2]),
+                 __float_as_uint(O[cb][4 * i + 3])});
   if (hf == 0) stg(p.part_ml + at, make_float2(m, l));
 }
 

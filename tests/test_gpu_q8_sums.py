@@ -34,3 +34,30 @@ def test_bf16_step_is_the_fp32_step_rounded(dev, fmt):  # noqa: F811
     a.step(q, k, v, oa, 0.09)
     b.step(q, k, v, ob, 0.09)
     assert torch.equal(oa.to(torch.bfloat16), ob)
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("d,G,n", [(64, 4, 20), (128, 8, 40), (128, 7, 3)])
+def test_partial_sums_of_prompts(dev, fmt, d, G, n):  # noqa: F811
+    """Equal weights over whole-number values, blocks of either sign, whose scales are all
+    1: every weight is a power of two, every sum exact in 32 bits, the division and the
+    parts' join take a few roundings of 2^-24, and so the output is the mean rounded to
+    bf16 wherever the mean is not within 2^-20 of itself of a tie."""
+    rng = np.random.default_rng(34 + d)
+    rows = 64 * 150
+    top = ref.TOP[fmt]
+    v = 8.0 * rng.integers(8, 16, (1, 1, rows, 1, d)).astype(np.float32)
+    v *= np.repeat(rng.choice([-1.0, 1.0], rows // 64), 64)[None, None, :, None, None]
+    v[0, 0, ::64, 0, 5] = top  # the largest of every block: scale 1
+    k = _values(rng, (1, 1, rows, 1, d))
+    from paper_2608_24063_amd.tensors import Q8Cache
+    c = Q8Cache(1, 1, G, 1, d, [rows], dev, format=fmt)
+    c.append(_t(k, dev), _t(v, dev))
+    assert (c.v_scale == 1).all()
+    out = np.asarray(_run_attend(c, np.zeros((1, 1, n, G, d), dtype=np.float32), dev, False, 0.1, None, False))
+    v = ref.read_back(v[0, 0, :, 0], fmt)
+    assert (v == np.rint(v)).all()
+    mean = v.sum(axis=0) / rows
+    want, lo, hi = (ref.bf16((mean * f).astype(np.float32)) for f in (1, 1 - 2.0 ** -20, 1 + 2.0 ** -20))
+    sure = lo == hi
+    assert sure.mean() > 0.95 and (out[..., sure] == want[sure]).all()
