@@ -453,10 +453,14 @@ typedef struct {
   const int64_t *row_off; /* [L*B*Hkv] */
   const int32_t *cap;
   int32_t *len;
-  const int32_t *order;   /* [L*B*Hkv]: the units in the order in which attention
-                             starts on them, or NULL; longest first evens out
-                             units of different lengths.  A permutation: a unit
-                             that it leaves out is not attended. */
+  const int32_t *order;   /* [L*B*Hkv]: the units in the order in which calls of n *
+                             Hq/Hkv <= 16 start on them, or NULL; longest first
+                             evens out units of different lengths.  No unit may
+                             appear twice.  A unit that it leaves out (entries
+                             outside [0, L*B*Hkv) are passed over) is neither
+                             attended nor, by viscache_q8_step, appended to.
+                             Append, read back and calls of more columns take all
+                             units and do not read it. */
 } vc_q8cache;
 
 /* A strided DEVICE tensor of rows of d contiguous values: row (layer l,

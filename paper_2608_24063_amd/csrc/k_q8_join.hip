@@ -40,7 +40,11 @@ __global__ __launch_bounds__(256) void k_join(Q8Attn p) {
   __shared__ Part sp[WPC][TPG];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t cg = (int64_t)blockIdx.x * (4 / WPC) + w / WPC;
-  const int u = (int)min(cg / p.cols, (int64_t)p.units - 1), col = (int)(cg % p.cols);
+  const int i = (int)min(cg / p.cols, (int64_t)p.units - 1), col = (int)(cg % p.cols);
+  // The units that the attention's launch took: nothing has written the parts of one
+  // that its order leaves out.  (Prompts take all.)
+  const int u = p.npmax > 1 && p.c.order ? ldg(p.c.order + i) : i;
+  if (u < 0 || u >= p.units) return;
   const int grp = w % WPC * GPW + lane / TPG, ch = lane % TPG * 4;
   const int g = u % p.Hkv, lb = u / p.Hkv, b = lb % p.B;
   const int cnt_ = p.count ? ldg(p.count + b) : p.n;
