@@ -338,35 +338,43 @@ def _ref(x):
     return ctypes.byref(x) if x is not None else None
 
 
+def _int32(x) -> int:
+    """An int32 argument: the nearest one, where ctypes would keep the low 32 bits.  A row
+    bound past the largest is no bound, and no other argument of that size is accepted."""
+    return max(min(int(x), 2 ** 31 - 1), -2 ** 31)
+
+
 def viscache_q8_append(shape: vc_decode_shape, cache: vc_q8cache, k: vc_rows, v: vc_rows, n: int, count: int,
                        unit_off: int, stream: int) -> None:
     """count, unit_off: device addresses, 0 for none."""
-    st = lib().viscache_q8_append(_ref(shape), _ref(cache), _ref(k), _ref(v), n, count, unit_off, stream)
+    st = lib().viscache_q8_append(_ref(shape), _ref(cache), _ref(k), _ref(v), _int32(n), count, unit_off,
+                                  stream)
     _check(st, "viscache_q8_append")
 
 
 def viscache_q8_read(shape: vc_decode_shape, cache: vc_q8cache, max_rows: int, k: vc_rows, v: vc_rows, unit_off: int,
                      out_fp32: int, stream: int) -> None:
-    st = lib().viscache_q8_read(_ref(shape), _ref(cache), max_rows, _ref(k), _ref(v), unit_off, out_fp32, stream)
+    st = lib().viscache_q8_read(_ref(shape), _ref(cache), _int32(max_rows), _ref(k), _ref(v), unit_off, out_fp32,
+                                stream)
     _check(st, "viscache_q8_read")
 
 
 def viscache_q8_attend_workspace_bytes(shape: vc_decode_shape, n: int, max_rows: int) -> int:
-    return int(lib().viscache_q8_attend_workspace_bytes(ctypes.byref(shape), n, max_rows))
+    return int(lib().viscache_q8_attend_workspace_bytes(ctypes.byref(shape), _int32(n), _int32(max_rows)))
 
 
 def viscache_q8_attend(shape: vc_decode_shape, cache: vc_q8cache, q: vc_rows, out: vc_rows, n: int, count: int,
                        causal: int, out_fp32: int, scale: float, max_rows: int, workspace: int, workspace_bytes: int,
                        stream: int) -> None:
-    st = lib().viscache_q8_attend(_ref(shape), _ref(cache), _ref(q), _ref(out), n, count, causal, out_fp32, scale,
-                                  max_rows, workspace, workspace_bytes, stream)
+    st = lib().viscache_q8_attend(_ref(shape), _ref(cache), _ref(q), _ref(out), _int32(n), count, causal, out_fp32,
+                                  scale, _int32(max_rows), workspace, workspace_bytes, stream)
     _check(st, "viscache_q8_attend")
 
 
 def viscache_rope(shape: vc_decode_shape, rope: vc_rope, n: int, pos: int, count: int, q_in, q_out, k_in, k_out,
                   stream: int) -> None:
     """q_in ... k_out: vc_rows or None."""
-    st = lib().viscache_rope(_ref(shape), _ref(rope), n, pos, count, _ref(q_in), _ref(q_out), _ref(k_in), _ref(k_out),
+    st = lib().viscache_rope(_ref(shape), _ref(rope), _int32(n), pos, count, _ref(q_in), _ref(q_out), _ref(k_in), _ref(k_out),
                              stream)
     _check(st, "viscache_rope")
 
@@ -376,7 +384,7 @@ def viscache_q8_step(shape: vc_decode_shape, cache: vc_q8cache, rope, pos: int, 
                      stream: int) -> None:
     """rope: vc_rope or None."""
     st = lib().viscache_q8_step(_ref(shape), _ref(cache), _ref(rope), pos, _ref(q), _ref(k), _ref(v), _ref(out),
-                                out_fp32, scale, max_rows, workspace, workspace_bytes, stream)
+                                out_fp32, scale, _int32(max_rows), workspace, workspace_bytes, stream)
     _check(st, "viscache_q8_step")
 
 

@@ -8,7 +8,7 @@ import struct
 
 import torch
 
-from . import (VC_PRUNE_EVENTS, VC_Q8_BLOCK, VisCacheError, lib, VC_Q8_E4M3, VC_Q8_INT8, VC_RANK_GLOBAL, make_params, make_prune_io, make_shape, prune_with_io, vc_cache,
+from . import (VC_PRUNE_EVENTS, VC_Q8_BLOCK, VisCacheError, _int32, lib, VC_Q8_E4M3, VC_Q8_INT8, VC_RANK_GLOBAL, make_params, make_prune_io, make_shape, prune_with_io, vc_cache,
                vc_decode_shape, vc_q8cache, vc_qcache, vc_rope, vc_rows, viscache_append_kv, viscache_budget, viscache_decode_attn,
                viscache_decode_plan, viscache_decode_step, viscache_decode_step_noalloc,
                viscache_decode_step_planned, viscache_decode_step_q4,
@@ -412,6 +412,10 @@ class Q8Cache:
             ws = self._ws_of[n, max_rows] = self._ws.data_ptr(), self._ws.numel()
         return ws
 
+    def _bound(self, max_rows) -> int:
+        """The row bound of a call: no unit holds more rows than it has room for."""
+        return self.max_cap if max_rows is None else min(_int32(max_rows), self.max_cap)
+
     def append(self, k, v, count=None, head_major: bool = False) -> None:
         """Appends k, v bf16 [L, B, n, Hkv, d] ([L, B, Hkv, n, d] with
         head_major); count int32 [L*B]: the rows of each layer and sequence."""
@@ -429,7 +433,8 @@ class Q8Cache:
         want = (self.L, self.B, self.Hkv, n, self.d) if head_major else (self.L, self.B, n, self.Hkv, self.d)
         if was != want:
             _refuse(k, "k", want, typ, self._index)
-        return (_take(k, "k", None, typ, self._index, head_major), _take(v, "v", want, typ, self._index, head_major), n)
+        return (_take(k, "k", None, typ, self._index, head_major), _take(v, "v", want, typ, self._index, head_major),
+                _int32(n))
 
     def load_pruned(self, pc: "PruneCall") -> None:
         """Appends what pc.run() left in its outputs (bf16 values): every
@@ -466,7 +471,7 @@ class Q8Cache:
         if typ is not _BF16 and typ is not _FP32:
             _refuse(k, "k", k.shape, "bf16 or fp32", self._index)
         kr, vr, rows = self._pair(k, v, head_major, typ)
-        m = rows if max_rows is None else int(max_rows)
+        m = rows if max_rows is None else _int32(max_rows)
         if m > rows:
             raise ValueError(f"max_rows {m} exceeds the {rows} rows of k")
         if rows == 0:
@@ -476,7 +481,9 @@ class Q8Cache:
 
     def attend(self, q, out, scale: float, count=None, causal: bool = True, max_rows=None) -> None:
         """Attention of q bf16 [L, B, n, Hq, d] over the cache into out (bf16 or
-        fp32, the same shape); count int32 [B]: the queries of each sequence."""
+        fp32, the same shape); count int32 [B]: the queries of each sequence.
+        max_rows: rows past it are not attended (by default, and at most, the largest
+        capacity)."""
         was = q.shape
         n = was[2]
         want = (self.L, self.B, n, self.Hq, self.d)
@@ -487,7 +494,7 @@ class Q8Cache:
         cnt = _ints(count, "count", (self.B,), self._index)
         if n == 0:
             return
-        rows = self.max_cap if max_rows is None else int(max_rows)
+        rows = self._bound(max_rows)
         ws = self._workspace(n, rows)
         _enqueue("viscache_q8_attend", self._lib.viscache_q8_attend, self._index, self._shape_at, self._cache_at, qr,
                  outr, n, cnt, int(causal), int(fp32), scale, rows, ws[0], ws[1])
