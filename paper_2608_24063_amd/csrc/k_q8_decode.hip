@@ -413,8 +413,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_decode8(Q8Attn p) {
       f32x4 o = {0.f, 0.f, 0.f, 0.f};
       o = mfma16x4(a, f16x4{hi[0], hi[1], hi[2], hi[3]}, o);
       o = mfma16x4(a, f16x4{lo[0], lo[1], lo[2], lo[3]}, o);
+      // (A column that sees no row of the block takes nothing of it: its weights
+      // are zero, but an infinity or a NaN among the values is not.)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) st.O[mb][i] = fmaf(o[i], vse, st.O[mb][i]);
+      for (int i = 0; i < 4; ++i) st.O[mb][i] = fmaf(end > nsealed * kQ8Block ? o[i] : 0.f, vse, st.O[mb][i]);
     }
   }
 

@@ -231,6 +231,25 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt8(Q8Attn p) {
           O[cb] = mfma32(*reinterpret_cast<const f16x8 *>(&V.v[32 * cb + ln][16 * s + 8 * hf]), hi[s], O[cb]);
     }
   };
+  // The open block's into O, for the columns that see a row of it: the weights of the
+  // others are zero, but an infinity or a NaN among its values is not.
+  auto open_outputs = [&](const Values<D> &V) {
+    const bool sees = end > nsealed * kQ8Block;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+      f32x16 acc;
+#pragma unroll
+      for (int k = 0; k < 16; ++k) acc[k] = 0.f;
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const f16x8 a = *reinterpret_cast<const f16x8 *>(&V.v[32 * cb + ln][16 * s + 8 * hf]);
+        acc = mfma32(a, hi[s], acc);
+        if (F32) acc = mfma32(a, lo[s], acc);
+      }
+#pragma unroll
+      for (int k = 0; k < 16; ++k) O[cb][k] = fmaf(sees ? acc[k] : 0.f, F32 ? vprev : 1.f, O[cb][k]);
+    }
+  };
   // The matrix part of block i: its logits, and the block before it into O; the
   // operands' reads run kAhead products ahead.
   auto products = [&](int i) {
@@ -363,7 +382,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt8(Q8Attn p) {
       const float ks = ldg(p.c.ks + blk0 + nsealed), vs = ldg(p.c.vs + blk0 + nsealed);
       logits(tk[Tc & 1]);
       weights(Tc, ks, vs);
-      outputs(tv[Tc & 1]);
+      open_outputs(tv[Tc & 1]);
     }
   }
   l = sum_halves(l);
