@@ -443,7 +443,16 @@ typedef enum { VC_Q8_INT8 = 0, VC_Q8_E4M3 = 1 } vc_q8_format; /* e4m3: finite on
  * c*64 + j (channel-major).  Row i of the open block is row j of the unit's tail.
  * The open block's scale entries hold the power of two that puts the largest
  * magnitude of its rows into [2^14, 2^15), at least 2^-60.  A cache starts with
- * len 0 and any other contents.  All pointers DEVICE; code pools and tails
+ * len 0 and any other contents.
+ * A caller may lower len[u] to take rows back (a draft's rejected tokens), but
+ * only to a multiple of 64 or within the open block, that is to no less than 64
+ * floor(len / 64): a sealed block's rows are no longer there one by one, and the
+ * tail's first rows are the open block's.  So a draft that may cross a multiple of
+ * 64 and be taken back is appended only as far as it was accepted.  After a
+ * length is lowered within the open block the block's scale entries go on
+ * counting the rows taken back until it is sealed or starts anew; attention then
+ * takes its values exactly down to 2^-31 of the largest one so counted and loses
+ * them below 2^-39 (all of them, if that was not finite).  All pointers DEVICE; code pools and tails
  * 16-byte aligned. */
 typedef struct {
   int32_t format;         /* vc_q8_format */

@@ -349,6 +349,9 @@ class Q8Cache:
     k_scale, v_scale, k_tail, v_tail, row_off, cap, len), laid out as vc_q8cache
     has them, where a program keeps them itself.
 
+    A program may lower `len` itself to take rows back, to a multiple of 64 or
+    within the open block; no other length can be gone back to.
+
     Calls go to the current stream of the cache's device.  Calls that attend
     share one workspace and must not overlap."""
 
