@@ -529,7 +529,8 @@ size_t viscache_q8_attend_workspace_bytes(const vc_decode_shape *shape, int32_t 
  * n = 0 does nothing.  `workspace`: DEVICE, at least
  * viscache_q8_attend_workspace_bytes bytes, 256-byte aligned; its contents on
  * entry do not matter and none are kept, so calls, captured ones among them,
- * may share one as long as they do not overlap.  VC_ERR_UNSUPPORTED for n *
+ * may share one as long as they do not overlap.  VC_ERR_WORKSPACE comes after all
+ * other checks: a call without a workspace only asks for them.  VC_ERR_UNSUPPORTED for n *
  * Hq/Hkv > 2^24, 2^23 or more workgroups, or 2^24 or more columns to join. */
 vc_status viscache_q8_attend(const vc_decode_shape *shape, const vc_q8cache *cache, const vc_rows *q,
                              const vc_rows *out, int32_t n, const int32_t *count, int32_t causal, int32_t out_fp32,

@@ -8,7 +8,7 @@ import struct
 
 import torch
 
-from . import (VC_PRUNE_EVENTS, VC_Q8_BLOCK, VisCacheError, _int32, lib, VC_Q8_E4M3, VC_Q8_INT8, VC_RANK_GLOBAL, make_params, make_prune_io, make_shape, prune_with_io, vc_cache,
+from . import (VC_ERR_WORKSPACE, VC_PRUNE_EVENTS, VC_Q8_BLOCK, VisCacheError, _int32, lib, VC_Q8_E4M3, VC_Q8_INT8, VC_RANK_GLOBAL, make_params, make_prune_io, make_shape, prune_with_io, vc_cache,
                vc_decode_shape, vc_q8cache, vc_qcache, vc_rope, vc_rows, viscache_append_kv, viscache_budget, viscache_decode_attn,
                viscache_decode_plan, viscache_decode_step, viscache_decode_step_noalloc,
                viscache_decode_step_planned, viscache_decode_step_q4,
@@ -517,11 +517,19 @@ class Q8Cache:
             self._pair(k, v, False, _BF16)
             if k.shape[2] != n:
                 raise ValueError(f"{k.shape[2]} new rows for {n} queries")
+            if rope is not None:
+                q_out = torch.empty_like(q) if q_out is None else q_out
+                k_out = torch.empty_like(k) if k_out is None else k_out
             if n > 0:
+                # Without a workspace attention launches nothing and says so last.
+                fp32, qr = out.dtype is _FP32, _take(q if rope is None else q_out, "q_out", want, _BF16, index)
+                st = self._lib.viscache_q8_attend(self._shape_at, self._cache_at, qr, _take(out, "out", None, out.dtype, index),
+                                                  n, 0, 1, int(fp32), scale, self.max_cap, 0, 0, 0)
+                if st != VC_ERR_WORKSPACE:
+                    raise VisCacheError(st, "viscache_q8_attend")
                 self._workspace(n, self.max_cap)
             if rope is not None:
-                q, k = rope.apply(pos, q, k, q_out=torch.empty_like(q) if q_out is None else q_out,
-                                  k_out=torch.empty_like(k) if k_out is None else k_out)
+                q, k = rope.apply(pos, q, k, q_out=q_out, k_out=k_out)
             self.append(k, v)
             self.attend(q, out, scale)
             return

@@ -20,6 +20,16 @@ def test_arguments_past_32_bits(vc, high, low):  # noqa: F811
     assert _attend(vc, rows=x, bytes_=need - 1) == _step(vc, rows=x, bytes_=need - 1) == (W if far else A)
 
 
+def test_workspace_is_checked_last(vc):  # noqa: F811
+    """A call without a workspace asks for the other checks."""
+    big, none = _shape(vc, B=1 << 20, L=8, Hq=1, Hkv=1), dict(ws=0, bytes_=0)
+    row = vc.vc_rows(0x10000, 1 << 38, 1 << 18, 128, 128)
+    for n in (1, 3, 40):
+        assert _attend(vc, n=n, **none) == vc.VC_ERR_WORKSPACE
+        assert _attend(vc, n=n, scale=0.0, **none) == _attend(vc, n=n, q=vc.vc_rows(8), **none) == vc.VC_ERR_ARG
+    assert _attend(vc, n=1 << 23, **none) == _attend(vc, big, q=row, out=row, **none) == vc.VC_ERR_UNSUPPORTED
+
+
 def test_bound_of_a_cache():
     from paper_2608_24063_amd.tensors import Q8Cache
     c = Q8Cache(1, 1, 4, 2, 64, [5, 70], "cpu")
