@@ -463,8 +463,7 @@ def _own(s, c):
         s["cache"].attend(s["q"], s["out"], s["scale"], count=s["count"], causal=c["causal"])
     else:
         s["len"].copy_(s["before"])
-        s["cache"].step(s["q"], s["k"], s["v"], s["out"], s["scale"], rope=s["rope"], pos=s["pos"],
-                        q_out=s["q_out"], k_out=s["k_out"])
+        s["cache"].step(s["q"], s["k"], s["v"], s["out"], s["scale"], rope=s["rope"], pos=s["pos"])
 
 
 def run(s):
