@@ -505,11 +505,11 @@ class Q8Cache:
     def step(self, q, k, v, out, scale: float, rope: Rope | None = None, pos=None, q_out=None, k_out=None) -> None:
         """A serving step: rotates q and k by pos int32 [3, B, n] (with `rope`),
         appends k and v and attends q.  One token (n = 1) is a single call
-        (viscache_q8_step) and writes its rotated rows nowhere else.  With more,
-        they go to q_out and k_out, by default new tensors.  q, k and v are left
-        as they are."""
+        (viscache_q8_step), which turns q and k on its way; several tokens are three
+        calls, and so is one whose rotated rows are asked for, in q_out or k_out.
+        q, k and v are left as they are, unless one of those is q or k."""
         n, index = q.shape[2], self._index
-        if n != 1:
+        if n != 1 or (rope is not None and (q_out is not None or k_out is not None)):
             # All of it is looked at before anything is appended.
             want = (self.L, self.B, n, self.Hq, self.d)
             _take(q, "q", want, _BF16, index)

@@ -2,7 +2,7 @@
 import numpy as np
 import pytest
 
-from tests.test_gpu_q8 import _filled, _t, _values, dev  # noqa: F401
+from tests.test_gpu_q8 import _filled, _same_caches, _t, _values, dev  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -52,3 +52,33 @@ def test_more_queries_than_attention_takes(dev):  # noqa: F811
         c.step(one.expand(1, 1, n, 4, 64), kv, kv, out, 0.1)
     assert e.value.status == vc.VC_ERR_UNSUPPORTED
     assert c.len.tolist() == [0]
+
+
+@pytest.mark.parametrize("n", [1, 3, 20])
+def test_rotated_rows_are_left_where_asked(dev, n):  # noqa: F811
+    """q_out and k_out, either or both, whatever the number of tokens; refused before
+    anything is appended where they do not fit."""
+    from paper_2608_24063_amd.tensors import Rope
+    a = _filled(np.random.default_rng(73), dev, 1, 2, 8, 2, 64, [100, 63, 64, 0], "e4m3", extra=90)[0]
+    args, rope = _args(dev, n), Rope(64, sections=(8, 12, 12))
+    pos = torch.from_numpy(np.random.default_rng(74).integers(0, 9000, (3, 2, n)).astype(np.int32)).to(dev)
+    q, k = args["q"].clone(), args["k"].clone()
+    wq, wk = rope.apply(pos, q, k)
+    for names in (("q_out",), ("k_out",), ("q_out", "k_out")):
+        given = {x: torch.full_like(wq if x == "q_out" else wk, 7.0) for x in names}
+        a.step(**args, rope=rope, pos=pos, **given)
+        assert all(torch.equal(t, wq if x == "q_out" else wk) for x, t in given.items())
+    # in place, and the same results as a step that is not asked for them
+    b = _filled(np.random.default_rng(73), dev, 1, 2, 8, 2, 64, [100, 63, 64, 0], "e4m3", extra=90)[0]
+    c = _filled(np.random.default_rng(73), dev, 1, 2, 8, 2, 64, [100, 63, 64, 0], "e4m3", extra=90)[0]
+    ob = torch.zeros_like(args["out"])
+    b.step(args["q"], args["k"], args["v"], ob, 0.125, rope=rope, pos=pos)
+    q, k = args["q"].clone(), args["k"].clone()
+    c.step(q, k, args["v"], args["out"], 0.125, rope=rope, pos=pos, q_out=q, k_out=k)
+    assert torch.equal(q, wq) and torch.equal(k, wk) and torch.equal(ob, args["out"])
+    _same_caches(b, c)
+    before = a.len.clone()
+    for bad in (dict(q_out=wk), dict(k_out=wq), dict(q_out=wq.float()), dict(k_out=wk.cpu())):
+        with pytest.raises(ValueError):
+            a.step(**args, rope=rope, pos=pos, **bad)
+    assert torch.equal(a.len, before)
