@@ -349,6 +349,12 @@ class Q8Cache:
     k_scale, v_scale, k_tail, v_tail, row_off, cap, len), laid out as vc_q8cache
     has them, where a program keeps them itself.
 
+    How a call's rows go to workgroups, and which units single tokens start with,
+    follow from the capacities, not from the lengths, which only the device knows;
+    a program that knows a bound well below the capacities passes it as max_rows
+    (8 units with room for 32000 rows and 1024 in each: a step 15.0 us, 11.3 with
+    max_rows = 1088; attention 12.2, 10.1).
+
     A program may lower `len` itself to take rows back, to a multiple of 64 or
     within the open block; no other length can be gone back to.
 
@@ -502,13 +508,15 @@ class Q8Cache:
         _enqueue("viscache_q8_attend", self._lib.viscache_q8_attend, self._index, self._shape_at, self._cache_at, qr,
                  outr, n, cnt, int(causal), int(fp32), scale, rows, ws[0], ws[1])
 
-    def step(self, q, k, v, out, scale: float, rope: Rope | None = None, pos=None, q_out=None, k_out=None) -> None:
+    def step(self, q, k, v, out, scale: float, rope: Rope | None = None, pos=None, q_out=None, k_out=None,
+             max_rows=None) -> None:
         """A serving step: rotates q and k by pos int32 [3, B, n] (with `rope`),
         appends k and v and attends q.  One token (n = 1) is a single call
         (viscache_q8_step), which turns q and k on its way; several tokens are three
         calls, and so is one whose rotated rows are asked for, in q_out or k_out.
-        q, k and v are left as they are, unless one of those is q or k."""
-        n, index = q.shape[2], self._index
+        q, k and v are left as they are, unless one of those is q or k.  max_rows as
+        for attend; it bounds what is attended, not what is appended."""
+        n, index, most = q.shape[2], self._index, self._bound(max_rows)
         if n != 1 or (rope is not None and (q_out is not None or k_out is not None)):
             # All of it is looked at before anything is appended.
             want = (self.L, self.B, n, self.Hq, self.d)
@@ -524,14 +532,14 @@ class Q8Cache:
                 # Without a workspace attention launches nothing and says so last.
                 fp32, qr = out.dtype is _FP32, _take(q if rope is None else q_out, "q_out", want, _BF16, index)
                 st = self._lib.viscache_q8_attend(self._shape_at, self._cache_at, qr, _take(out, "out", None, out.dtype, index),
-                                                  n, 0, 1, int(fp32), scale, self.max_cap, 0, 0, 0)
+                                                  n, 0, 1, int(fp32), scale, most, 0, 0, 0)
                 if st != VC_ERR_WORKSPACE:
                     raise VisCacheError(st, "viscache_q8_attend")
-                self._workspace(n, self.max_cap)
+                self._workspace(n, most)
             if rope is not None:
                 q, k = rope.apply(pos, q, k, q_out=q_out, k_out=k_out)
             self.append(k, v)
-            self.attend(q, out, scale)
+            self.attend(q, out, scale, max_rows=most)
             return
         want, kv = (self.L, self.B, 1, self.Hq, self.d), (self.L, self.B, 1, self.Hkv, self.d)
         fp32 = out.dtype is _FP32
@@ -542,9 +550,9 @@ class Q8Cache:
             if rope.d != self.d or pos is None:
                 raise ValueError("the rotation is of another head dim, or has no positions")
             turn, at = rope._address[0][0], _ints(pos, "pos", (3, self.B, 1), index)
-        ws = self._workspace(1, self.max_cap)
+        ws = self._workspace(1, most)
         _enqueue("viscache_q8_step", self._lib.viscache_q8_step, index, self._shape_at, self._cache_at, turn, at, *rows,
-                 int(fp32), scale, self.max_cap, ws[0], ws[1])
+                 int(fp32), scale, most, ws[0], ws[1])
 
 
 __all__ = ["PruneCall", "DecodeCache", "Q8Cache", "Rope", "make_params"]

@@ -82,3 +82,21 @@ def test_rotated_rows_are_left_where_asked(dev, n):  # noqa: F811
         with pytest.raises(ValueError):
             a.step(**args, rope=rope, pos=pos, **bad)
     assert torch.equal(a.len, before)
+
+
+@pytest.mark.parametrize("n", [1, 3])
+@pytest.mark.parametrize("most", [0, 64, 150, 2 ** 40])
+def test_row_bound_of_a_step(dev, n, most):  # noqa: F811
+    """max_rows bounds what a step attends, and nothing else."""
+    a, b = (_filled(np.random.default_rng(75), dev, 1, 2, 8, 2, 64, [100, 63, 64, 300], "int8", extra=90)[0]
+            for _ in range(2))
+    args = _args(dev, n)
+    want = torch.zeros_like(args["out"])
+    a.step(**args, max_rows=most)
+    b.append(args["k"], args["v"])
+    b.attend(args["q"], want, 0.125, max_rows=most)
+    assert torch.equal(args["out"], want)
+    _same_caches(a, b)
+    with pytest.raises(Exception):
+        a.step(**args, max_rows=-1)
+    _same_caches(a, b)
