@@ -235,6 +235,7 @@ assert ctypes.sizeof(vc_rows) == struct.calcsize("5q")
 _current_device = getattr(torch._C, "_cuda_getDevice", None)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _BF16, _FP32 = torch.bfloat16, torch.float32
+_changed = torch._C._increment_version  # tensors written through their addresses
 
 
 def _refuse(t, name, shape, typ, index):
@@ -304,7 +305,19 @@ class Rope:
         None; both bf16 or fp32) by pos int32 [3, B, n] into q_out and k_out, by
         default in place, on the current stream of their GPU.  count int32 [B]:
         the tokens of each sequence.  `inverse` turns back, which is the
-        gradient.  Returns (q_out, k_out)."""
+        gradient.  Returns (q_out, k_out).
+
+        Autograd does not see the rotation, so tensors that require grad are refused
+        where it records (a program calls this in the forward and backward of an
+        autograd function of its own, or under no_grad); outputs count as changed in
+        place."""
+        if ((q is not None and q.requires_grad) or (k is not None and k.requires_grad) or
+                (q_out is not None and q_out.requires_grad) or (k_out is not None and k_out.requires_grad)):
+            if torch.is_grad_enabled():
+                raise ValueError("a tensor requires grad: autograd does not see the rotation")
+        return self._turn(pos, q, k, q_out, k_out, inverse, count)
+
+    def _turn(self, pos, q, k, q_out, k_out, inverse=False, count=None):
         ref = q if q is not None else k
         if ref is None:
             raise ValueError("nothing to rotate")
@@ -333,10 +346,13 @@ class Rope:
         key = (L, B, Hq, Hkv)
         shape = self._shapes.get(key)
         if shape is None:
-            shape = self._shapes[key] = vc_decode_shape(B, L, Hq, Hkv, d)
-        _enqueue("viscache_rope", self._f, index, ctypes.addressof(shape),
-                 self._address[typ is _FP32][bool(inverse)], n, at, cnt, qi, qo, ki, ko)
-        return q_out, k_out
+            shape = vc_decode_shape(B, L, Hq, Hkv, d)
+            shape = self._shapes[key] = ctypes.addressof(shape), shape
+        _enqueue("viscache_rope", self._f, index, shape[0], self._address[typ is _FP32][bool(inverse)], n, at, cnt, qi,
+                 qo, ki, ko)
+        out = q_out, k_out
+        _changed(out if q is not None and k is not None else (q_out,) if k is None else (k_out,))
+        return out
 
 
 _Q8_BUFFERS = ("k_codes", "v_codes", "k_scale", "v_scale", "k_tail", "v_tail", "row_off", "cap", "len")
@@ -537,7 +553,7 @@ class Q8Cache:
                     raise VisCacheError(st, "viscache_q8_attend")
                 self._workspace(n, most)
             if rope is not None:
-                q, k = rope.apply(pos, q, k, q_out=q_out, k_out=k_out)
+                q, k = rope._turn(pos, q, k, q_out, k_out)
             self.append(k, v)
             self.attend(q, out, scale, max_rows=most)
             return
