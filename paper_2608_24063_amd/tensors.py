@@ -463,7 +463,9 @@ class Q8Cache:
 
     def load_pruned(self, pc: "PruneCall") -> None:
         """Appends what pc.run() left in its outputs (bf16 values): every
-        layer's kept rows, a launch or two a layer.  Evicted layers get none."""
+        layer's kept rows, a launch or two a layer.  Evicted layers get none.  Refused,
+        with nothing appended, where a unit has too little room (the lengths are read
+        back for that, so not in a capture)."""
         if (pc.L, pc.B, pc.Hkv, pc.d) != (self.L, self.B, self.Hkv, self.d) or pc.params.v_out_fp32:
             raise ValueError("the pruned cache has another shape, or fp32 values")
         per = self.B * self.Hkv
@@ -472,6 +474,14 @@ class Q8Cache:
         off = torch.tensor([[pc.unit_rows(l, b, g)[0] * self.d for b in range(pc.B) for g in range(pc.Hkv)]
                             for l in range(pc.L)], dtype=torch.int64)
         most = count.amax(dim=1).tolist()
+        if any(m and t.get_device() != self._index for m, t in zip(most, pc.k_out)):
+            raise ValueError("the pruned cache is on another device")
+        room = (self.cap - self.len).cpu().view(self.L, self.B, self.Hkv)
+        lacks = ((count[..., None] > room) & (count[..., None] > 0)).flatten().nonzero().flatten()
+        if len(lacks):
+            u = int(lacks[0])
+            raise ValueError(f"unit {u} has room for {max(int(room.flatten()[u]), 0)} rows of "
+                             f"{int(count.flatten()[u // self.Hkv])}, and {len(lacks) - 1} others have too little")
         count, off = count.to(self.device), off.to(self.device)
         with torch.cuda.device(self._index):
             stream = _raw_stream(self._index)
@@ -482,8 +492,6 @@ class Q8Cache:
                                self.k_tail[l * per:].data_ptr(), self.v_tail[l * per:].data_ptr(),
                                self.row_off[l * per:].data_ptr(), self.cap[l * per:].data_ptr(),
                                self.len[l * per:].data_ptr(), 0)
-                if pc.k_out[l].get_device() != self._index:
-                    raise ValueError("the pruned cache is on another device")
                 k = vc_rows(pc.k_out[l].data_ptr(), 0, 0, self.d, 0)
                 v = vc_rows(pc.v_out[l].data_ptr(), 0, 0, self.d, 0)
                 viscache_q8_append(one, c, k, v, most[l], count[l].data_ptr(), off[l].data_ptr(), stream)
