@@ -568,7 +568,11 @@ typedef struct {
  * input (the same data and strides); otherwise they must not overlap.  pos:
  * DEVICE int32 [3][B][n], shared by the layers.  count: DEVICE int32 [B] or
  * NULL; tokens i >= count[b] are left alone.  n = 0 does nothing.
- * VC_ERR_UNSUPPORTED for 2^24 or more tokens over all layers and sequences. */
+ * VC_ERR_UNSUPPORTED for 2^24 or more tokens over all layers and sequences.  The
+ * shape is held to what attention takes, also where a pair is NULL: d 64 or 128, Hq
+ * a multiple of Hkv (VC_ERR_SHAPE) and at most 16 times it (VC_ERR_UNSUPPORTED).
+ * Other head counts are rotated in a call for the queries and one for the keys,
+ * each with its own heads as Hq and Hkv. */
 vc_status viscache_rope(const vc_decode_shape *shape, const vc_rope *rope, int32_t n, const int32_t *pos,
                         const int32_t *count, const vc_rows *q_in, const vc_rows *q_out, const vc_rows *k_in,
                         const vc_rows *k_out, void *stream);

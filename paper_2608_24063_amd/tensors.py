@@ -305,7 +305,8 @@ class Rope:
         None; both bf16 or fp32) by pos int32 [3, B, n] into q_out and k_out, by
         default in place, on the current stream of their GPU.  count int32 [B]:
         the tokens of each sequence.  `inverse` turns back, which is the
-        gradient.  Returns (q_out, k_out).
+        gradient.  Returns (q_out, k_out).  In one call Hq is a multiple of Hkv and at
+        most 16 times it; other heads take a call for q and one for k.
 
         Autograd does not see the rotation, so tensors that require grad are refused
         where it records (a program calls this in the forward and backward of an
