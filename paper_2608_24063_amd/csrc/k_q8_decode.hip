@@ -52,18 +52,6 @@ __device__ __forceinline__ f16x8 pack8(const _Float16 *h) {
   return f16x8{h[0], h[1], h[2], h[3], h[4], h[5], h[6], h[7]};
 }
 
-// Eight bf16 values times a power of two, as fp16.
-__device__ __forceinline__ f16x8 half8_of_bf16(u32x4 w, float f) {
-  const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
-  f16x8 r;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    r[2 * i] = (_Float16)(bf16_lo(ws[i]) * f);
-    r[2 * i + 1] = (_Float16)(bf16_hi(ws[i]) * f);
-  }
-  return r;
-}
-
 constexpr int kWaves = 4;
 
 template <int D>

@@ -43,17 +43,6 @@ __device__ __forceinline__ f32x16 mfma32(f16x8 a, f16x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
 
-__device__ __forceinline__ f16x8 half8_of_bf16(u32x4 w, float f) {
-  const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
-  f16x8 r;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    r[2 * i] = (_Float16)(bf16_lo(ws[i]) * f);
-    r[2 * i + 1] = (_Float16)(bf16_hi(ws[i]) * f);
-  }
-  return r;
-}
-
 // Pitches in halves: 16-byte reads of 32 rows without conflicts.
 template <int D>
 struct Keys {

@@ -99,10 +99,22 @@ __device__ __forceinline__ uint32_t max_mag(uint32_t m, uint32_t w) {
 
 // The power of two that puts a largest magnitude (bf16 bits) into [2^14,
 // 2^15), at least 2^-60: with it a row's bf16 values are exact in fp16 down to
-// 2^-28 of the largest.
+// 2^-31 of the largest.
 __device__ __forceinline__ float open_scale(uint32_t mag) {
   const int e = max((int)(mag >> 7) - 14, 127 - 60);
   return __uint_as_float((uint32_t)e << 23);
+}
+
+// Eight bf16 values times a power of two, as fp16.
+__device__ __forceinline__ f16x8 half8_of_bf16(u32x4 w, float f) {
+  const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+  f16x8 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    r[2 * i] = (_Float16)(bf16_lo(ws[i]) * f);
+    r[2 * i + 1] = (_Float16)(bf16_hi(ws[i]) * f);
+  }
+  return r;
 }
 
 // 4 x 4 bytes transposed: byte j of word i becomes byte i of word j.
