@@ -5,12 +5,12 @@
 // in 32 bits a position of 2^20 would leave 2^-4 of a turn unknown.  Sine and
 // cosine of the reduced angle and the rotation itself are in 32 bits, rounded
 // once to the output's type (fp32 rows at positions below 2^20 are 4.1e-8 of
-// themselves off; 5.5e-8 without the angle's last bits).  The gradient of the rotation is the rotation by
-// -a (the sign of the sine).
+// themselves off; 5.5e-8 without the angle's last bits).  The gradient of the
+// rotation is the rotation by -a (the sign of the sine).
 //
-// Bound by memory: every value is read and written once, streamed (12608 tokens
-// of 28 + 4 bf16 heads 43.4 -> 39.7 us, 5.2 TB/s; 8198 of 64 + 8 fp32 ones 120 ->
-// 112, 5.4).  A token's d/2
+// Bound by memory: every value is read and written once, streamed.  12608 tokens
+// of 28 + 4 bf16 heads take 35.8 us (5.8 TB/s), 8198 of 64 + 8 fp32 ones 103 (5.9).
+// (Streaming: 43.4 -> 39.7 and 120 -> 112, with four tokens a workgroup.)  A token's d/2
 // (sine, cosine) pairs serve all of its heads, so they are computed once per
 // token and layer, one per thread, and shared through LDS; a lane then keeps
 // the pairs of its own channels in registers while it walks the heads.
@@ -123,7 +123,15 @@ __global__ __launch_bounds__(256) void k_rope(RopePlan p) {
 template <bool F32, bool ADJ>
 hipError_t launch(const RopePlan &p, hipStream_t st) {
   const int64_t toks = (int64_t)p.B * p.n;
-  if (toks * p.L >= 4 * 2048) {
+  // A wave's pass takes as many heads as chunk pairs of a row leave lanes for.  Four
+  // tokens a workgroup, a wave each, where that is two passes of a wave or fewer and
+  // the tokens fill the chip; else a token a workgroup.  (us, one token and four:
+  // bf16, 128 channels, 32000 tokens of 2, 10, 16, 32 heads 41.3 20.2, 54.0 29.9, 57.0
+  // 45.0, 83.8 92.7; 2000 of 16 and 32 6.8 6.1, 8.8 9.2; 500 of 2 and 16 4.8 4.9, 4.3 4.9.
+  // fp32, 128 channels, 32000 of 8, 16, 32 heads 56.0 43.9, 83.7 87.3, 169 191; bf16, 64
+  // channels, 16 and 32 heads 45.0 28.7, 58.5 57.4.)
+  const int lanes = p.d / (2 * Chunk<F32>::N), heads = 64 / lanes;  // lanes of a row, heads of a pass
+  if (p.Hq + p.Hkv <= 2 * heads && toks * p.L >= 2048) {
     const int64_t grid = (toks + 3) / 4 * p.L;
     hipLaunchKernelGGL((k_rope<F32, ADJ, 4>), dim3((uint32_t)grid), dim3(256), 0, st, p);
   } else {
