@@ -91,7 +91,11 @@ bool attend_cut(const vc_decode_shape *s, int32_t n, int32_t max_rows, Cut &c) {
     // 620 to 1490 in 12 and uncut 17.1, 16.2; 160 of 800 to 1900 in 20 and uncut
     // 19.7, 18.5; 896 of 2300 to 5800 in 24, 48 and uncut 199, 198, 188; 8 of 9, 12,
     // 16, 20 blocks in 4 10.3, 11.3, 11.3, 11.4, uncut 9.7, 10.8, 12.1, 13.4; 32 of
-    // them in 4 10.7, 11.6, 12.1, 12.7, uncut 9.8, 11.0, 12.2, 14.3.)
+    // them in 4 10.7, 11.6, 12.1, 12.7, uncut 9.8, 11.0, 12.2, 14.3.  Far longer units
+    // would gain from two even pieces, by what the cut makes of them now and in two:
+    // 128 of 4000, 8000, 16000, 32000 rows 31.2 30.7, 50.5 48.2, 108 100, 220 191; 112 of
+    // 3000, 8000, 32000 26.0 23.9, 43.3 41.9, 173 161; but 160 of 8000, 32000 62.8 72.9, 232
+    // 280 and 200 of them 77.2 87.0, 280 303.)
     const int64_t want = units * nt / 256;
     c.qcols = kCols;
     c.piece = (int32_t)std::min<int64_t>(std::max<int64_t>(4, (want + 3) / 4 * 4), int64_t(1) << 26);
@@ -107,7 +111,12 @@ bool attend_cut(const vc_decode_shape *s, int32_t n, int32_t max_rows, Cut &c) {
     const int64_t resident = c.qcols == 256 ? 256 : 512;
     c.nqt = (int32_t)nqt;
     // Workgroups that the card holds at once share the tiles' rows where that
-    // is two a tile or more.
+    // is two a tile or more.  (us, whole tiles and shared ones: 132, 152 and 168 tiles of
+    // 12544 rows 334 340, 301 346, 324 341; 136 and 152 of 23040 540 604, 546 617: shares
+    // of one tile each are whole tiles with a join.  Sequences of unlike lengths would
+    // gain, four of 2250 to 9000 rows in 144 tiles 220 144, but their lengths are not
+    // known here.  Whole tiles leave the more workgroups idle the fewer they are, 124 of
+    // 256 at 132.)
     c.ns = tiles * 2 <= resident && nt >= 2 * kQ8SplitBlocks ? 2 : 1;
     c.wgs = c.ns > 1 ? std::min(resident, tiles * (nt / kQ8SplitBlocks)) : tiles;
     c.slots = c.ns > 1 ? c.wgs * c.qcols : 0;
@@ -152,7 +161,12 @@ vc_status rope_table(const vc_rope *r, int32_t d, RopeTable &t) {
 }
 
 // Workgroups a unit of an append: one where its blocks are few, which then also
-// advances the length; else a block each.
+// advances the length; else a block each, and the lengths in a launch of their own.
+// (us, keys and values of 128 channels in int8, one workgroup and a block each: 8 units of
+// 64, 128, 200, 256, 400 rows 2.5 4.3, 5.7 5.6, 8.0 6.2, 9.0 5.5, 13.3 6.0; 112 of 128,
+// 200, 256, 400, 640 rows 6.3 7.4, 8.9 9.5, 10.3 9.5, 14.3 12.6, 22.4 14.1; 896 of 128,
+// 256, 400, 640 rows 16.3 19.8, 26.6 30.8, 38.0 53.0, 83.1 66.8.  They meet at 128 rows of
+// few units and between 400 and 640 of many; 256 lies between.)
 int64_t append_groups(int64_t n) {
   return n <= 4 * kQ8Block ? 1 : (n + kQ8Block - 1) / kQ8Block + 1;
 }
