@@ -7,7 +7,8 @@
 // trips.  A launch of its own costs less than the last workgroup's joining them
 // in the attention's launch did: there the partials need device-coherent
 // stores, a wait for them and an atomic, and one workgroup joins a whole unit
-// (4 units of 12544 rows: 18.5 us in one launch, 13.0 in two).  After a step it
+// (4 units of 12544 rows, about 49 parts each: 18.5 us in one launch, 13.0 in two;
+// units of few parts were not timed in one).  After a step it
 // also advances the lengths, which every piece of a unit reads.
 #include "vc_q8_device.h"
 
