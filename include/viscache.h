@@ -522,10 +522,11 @@ size_t viscache_q8_attend_workspace_bytes(const vc_decode_shape *shape, int32_t 
  * With more columns and bf16 outputs each weight is rounded to fp16 before it
  * meets its value: 2^-12 of itself, or 2^-33 of the query's largest weight times
  * value scale where that is more; a caller that needs more asks for fp32 outputs.  A query that
- * sees no row gives zeros; rows i >= c of out are left as they were.  max_rows
- * bounds every len (rows past it are not attended).  One launch, and a second
- * that joins partial results where few (unit, query) tiles are cut along their
- * rows; n * Hq/Hkv <= 16 (single tokens, short drafts) has kernels of its own.
+ * sees no row gives zeros, one with a NaN otherwise NaN; rows i >= c of out are
+ * left as they were.  max_rows bounds every len (rows past it are not attended).
+ * One launch, and a second that joins partial results where few (unit, query)
+ * tiles are cut along their rows; n * Hq/Hkv <= 16 (single tokens, short drafts)
+ * has kernels of its own.
  * n = 0 does nothing.  `workspace`: DEVICE, at least
  * viscache_q8_attend_workspace_bytes bytes, 256-byte aligned; its contents on
  * entry do not matter and none are kept, so calls, captured ones among them,

@@ -431,18 +431,18 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_decode8(Q8Attn p) {
     float M = kNegInf;
 #pragma unroll
     for (int k = 0; k < kWaves; ++k) M = fmaxf(M, sm.ml[k][col].x);
+    // (Without a maximum there are no rows, all zeros, or only NaN, which stay.)
+    const float ref = M == kNegInf ? 0.f : M;
     float o = 0.f, s = 0.f;
-    if (M != kNegInf) {
 #pragma unroll
-      for (int k = 0; k < kWaves; ++k) {
-        const float f = fast_exp2(sm.ml[k][col].x - M);
-        o += f * wo[k][col][x];
-        s += f * sm.ml[k][col].y;
-      }
+    for (int k = 0; k < kWaves; ++k) {
+      const float f = fast_exp2(sm.ml[k][col].x - ref);
+      o += f * wo[k][col][x];
+      s += f * sm.ml[k][col].y;
     }
     o *= 0x1p-14f;
     if (np == 1) {
-      put(p, out_row(p, p.out, u, col) + x, s > 0.f ? o / s : 0.f);
+      put(p, out_row(p, p.out, u, col) + x, s == 0.f ? 0.f : o / s);
     } else {
       stg(p.part_o + (part * 16 + col) * D + x, o);
       if (x == 0) stg(p.part_ml + part * 16 + col, make_float2(M, s));

@@ -22,11 +22,14 @@ struct Part {
   float M, l, o[4];
 };
 
+// What the parts' maxima are taken against: anything finite where there are no rows
+// (their sums are zeros, or NaN, which stay).
+__device__ __forceinline__ float against(float M) { return M == kNegInf ? 0.f : M; }
+
 // b into a.
 __device__ __forceinline__ void add(Part &a, const Part &b) {
-  const float M = fmaxf(a.M, b.M);
-  if (M == kNegInf) return;
-  const float fa = fast_exp2(a.M - M), fb = fast_exp2(b.M - M);
+  const float M = fmaxf(a.M, b.M), r = against(M);
+  const float fa = fast_exp2(a.M - r), fb = fast_exp2(b.M - r);
   a.M = M;
   a.l = fa * a.l + fb * b.l;
 #pragma unroll
@@ -86,15 +89,15 @@ __global__ __launch_bounds__(256) void k_join(Q8Attn p) {
 #pragma unroll
     for (int k = 0; k < U; ++k)
       if (s0 + k * NG < ns) M = fmaxf(M, ml[k].x);
-    if (M == kNegInf) continue;
-    const float f0 = fast_exp2(t.M - M);
+    const float r = against(M), f0 = fast_exp2(t.M - r);
     t.M = M;
     t.l *= f0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) t.o[i] *= f0;
 #pragma unroll
     for (int k = 0; k < U; ++k) {
-      const float f = s0 + k * NG < ns ? fast_exp2(ml[k].x - M) : 0.f;
+      if (s0 + k * NG >= ns) continue;
+      const float f = fast_exp2(ml[k].x - r);
       t.l += f * ml[k].y;
 #pragma unroll
       for (int i = 0; i < 4; ++i) t.o[i] += f * x[k][i];
@@ -118,7 +121,7 @@ __global__ __launch_bounds__(256) void k_join(Q8Attn p) {
     for (int k = 1; k < WPC; ++k) add(t, sp[k][lane % TPG]);
   }
   if (lane >= TPG) return;
-  const float inv = t.l > 0.f ? 1.f / t.l : 0.f;
+  const float inv = t.l == 0.f ? 0.f : 1.f / t.l;
   const int64_t to = (int64_t)(lb / p.B) * p.out.layer + (int64_t)b * p.out.seq + (int64_t)(col / p.G) * p.out.token +
                      (int64_t)(g * p.G + col % p.G) * p.out.head + ch;
   const float v[4] = {t.o[0] * inv, t.o[1] * inv, t.o[2] * inv, t.o[3] * inv};

@@ -381,7 +381,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt8(Q8Attn p) {
     st8(reinterpret_cast<uint32_t *>(p.np) + 2 * (u * p.nqt + qt), u32x2{(uint32_t)sh.id, (uint32_t)ns});
   if (col > cl) return;
   if (ns == 1) {
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
     const int64_t at = row_of(p.out, col);
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb)

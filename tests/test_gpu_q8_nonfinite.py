@@ -68,3 +68,31 @@ def test_appended_rows(dev, fmt, n):  # noqa: F811
     for c, o in ((a, oa), (b, ob)):
         c.attend(q, o, 0.1, causal=False, max_rows=64 * 6)  # up to the open block of the first, past none of the second
     assert torch.equal(oa, ob)
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("d,G,n,lens", [(64, 4, 1, [200, 90]), (128, 7, 1, [64 * 90 + 3, 64 * 40]), (64, 8, 2, [64 * 90, 5]),
+                                        (64, 4, 9, [64 * 3, 64 * 30 + 9]), (128, 8, 70, [64 * 60, 64 * 9 + 30])])
+@pytest.mark.parametrize("fp32", [True, False])
+def test_query_with_a_nan(dev, fmt, d, G, n, lens, fp32):  # noqa: F811
+    """NaN for the query's head and no other, of units that are cut along their rows and
+    whole ones; zeros still for one that sees no row."""
+    c = _filled(np.random.default_rng(65), dev, 1, 1, 2 * G, 2, d, lens, fmt)[0]
+    x = _values(np.random.default_rng(66), (1, 1, n, 2 * G, d))
+    typ = torch.float32 if fp32 else torch.bfloat16
+    clean, out = (torch.full((1, 1, n, 2 * G, d), 7.0, dtype=typ, device=dev) for _ in range(2))
+    c.attend(_t(x, dev), clean, 0.1)
+    x[0, 0, n - 1, ::2, 5] = np.nan
+    c.attend(_t(x, dev), out, 0.1)
+    torch.cuda.synchronize()
+    assert out[0, 0, n - 1, ::2].isnan().all()
+    same = torch.ones(out.shape, dtype=torch.bool, device=dev)
+    same[0, 0, n - 1, ::2] = False
+    if fp32 or n * G <= 16:
+        assert torch.equal(out[same], clean[same])
+    else:  # a wave's columns may be rescaled together, which moves roundings
+        a, b = out[same].float(), clean[same].float()
+        assert ((a - b).abs() <= 2.0 ** -7 * b.abs() + 2.0 ** -10 * b.abs().max()).all()
+    c.len.zero_()
+    c.attend(_t(x, dev), out, 0.1)
+    assert (out == 0).all()
