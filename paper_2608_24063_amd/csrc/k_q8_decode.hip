@@ -23,8 +23,8 @@
 // requested with the first block, since the whole kernel waits for them (read
 // by one wave after its own blocks they took 8 of 25 us).
 //
-// Measured: 896 units of 2300 to 5800 rows, 128 channels, 170 us (5.5 TB/s, the
-// rate of reads alone); 112 units of about 1050 rows, 16 us, of which the bytes
+// Measured: 896 units of 2300 to 5800 rows, 128 channels, 169 to 174 us (5.5 TB/s, the
+// rate of reads alone); 112 units of about 1050 rows, 15 to 16 us, of which the bytes
 // at that rate are 5.5 and the launch and the chain of round trips (length,
 // codes, partials in LDS) the rest.
 //

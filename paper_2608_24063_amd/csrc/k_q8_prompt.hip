@@ -23,11 +23,13 @@
 // outputs P is split in two fp16 parts (22 bits) and each block's product is scaled
 // into O in fp32.  Sums, maxima, O and the partial results are fp32 in both.
 //
-// Measured: 2048 queries of 64 heads over 23040 rows, 128 channels, int8: 1340 to
-// 1410 us, 1.05 to 1.1 PFLOP/s, 0.9 of a large library product's rate.  Of a SIMD's
-// cycles 54% are matrix instructions'; the vector unit's come on top of them, and
-// the clock falls to 1.9 GHz.  Three ragged questions of up to 65 tokens over 9001
-// to 12801 rows: 43 us and 6 to join, 8.5 of them before the first block is in LDS.
+// Measured: 2048 queries of 64 heads over 23040 rows, 128 channels, int8: 1315 to
+// 1395 us on several machines, 1.06 to 1.13 PFLOP/s, 0.86 to 0.91 of a large library
+// product's rate (1418 to 1435 us under the profiler).  Of a SIMD's cycles 54% are
+// matrix instructions'; the vector unit's come on top of them, and the clock falls to
+// 1.9 GHz.  Three ragged questions of up to 65 tokens over 9001 to 12801 rows: 46 us
+// a call; under the profiler 42, 8.5 of them before the first block is in LDS, and 8
+// to join.
 #include "vc_q8_device.h"
 
 namespace vc {

@@ -266,7 +266,7 @@ struct Share {
 // wave takes part.  Where few tiles are cut along
 // their rows, as many blocks go to each workgroup as make no more splits than
 // workgroups: sequences without queries take none, longer units take more.  (us,
-// with as many splits for every tile and so: four sequences of 3000 to 12801
+// with partial results in fp16, with as many splits for every tile and so: four sequences of 3000 to 12801
 // rows with 40 queries each 56.5, 47.8, with up to 40 44.6, 36.5; three of 9001 to
 // 12801 with up to 65 51.6, 48.9; one of 12544 with 30 23.7, 24.0, with 1024 202,
 // 205.)
