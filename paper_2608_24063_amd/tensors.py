@@ -429,11 +429,15 @@ class Q8Cache:
         ws = self._ws_of.get((n, max_rows))
         if ws is None:
             need = viscache_q8_attend_workspace_bytes(self.shape, n, max_rows)
-            if self._ws is None or self._ws.numel() < need:
+            had = 0 if self._ws is None else self._ws.numel()
+            if self._ws is None or had < need:
                 if torch.cuda.is_current_stream_capturing():
                     raise RuntimeError("the workspace is too small: run the call once before it is captured")
-                self._ws = torch.empty((need,), dtype=torch.uint8, device=self.device)
+                # By half at least, so that all that are kept come to three times the largest.
+                self._ws = torch.empty((max(need, had + had // 2),), dtype=torch.uint8, device=self.device)
                 self._kept.append(self._ws)  # a graph captured before this goes on using the one it knows
+                self._ws_of.clear()
+            elif len(self._ws_of) >= 4096:  # bounds that change with every call
                 self._ws_of.clear()
             ws = self._ws_of[n, max_rows] = self._ws.data_ptr(), self._ws.numel()
         return ws
