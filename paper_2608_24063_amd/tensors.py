@@ -364,7 +364,9 @@ class Q8Cache:
     Hkv heads: unit u = (l*B + b)*Hkv + g has room for caps[u] rows.  format:
     "int8" or "e4m3".  `buffers`: the cache's tensors by name (k_codes, v_codes,
     k_scale, v_scale, k_tail, v_tail, row_off, cap, len), laid out as vc_q8cache
-    has them, where a program keeps them itself.
+    has them, where a program keeps them itself; row_off and cap have to hold the
+    units' first rows, whole blocks one unit after the other, and caps (they are
+    not read back to be checked).
 
     How a call's rows go to workgroups, and which units single tokens start with,
     follow from the capacities, not from the lengths, which only the device knows;
