@@ -592,6 +592,46 @@ vc_status viscache_q8_step(const vc_decode_shape *shape, const vc_q8cache *cache
                            const vc_rows *out, int32_t out_fp32, float scale, int32_t max_rows, void *workspace,
                            size_t workspace_bytes, void *stream);
 
+/* ---- normed rotations -----------------------------------------------------
+ * Models that norm their queries and keys before they turn: for each head's row x of
+ * d channels
+ *   r = (mean of x^2 + eps)^(-1/2),  y = w r x,  out = R(pos) y,
+ * w the weights of the layer's queries or keys and R the rotation of viscache_rope.
+ * All of it is fp32 (the angles 64 bits) and rounded once; squares past the range of
+ * fp32 (a row of magnitude 2^60 and more) give unspecified rows. */
+typedef struct {
+  float eps;                        /* finite, at least the smallest normal fp32 value */
+  int32_t weight_fp32;              /* type of both weights: 0 bf16, 1 fp32 */
+  const void *q_weight, *k_weight;  /* DEVICE [L][d], 16-byte aligned; not read without the rows they belong to */
+} vc_norm;
+
+/* Device, asynchronous.  Norm, weight and rotation of n tokens of every layer and
+ * sequence, in one pass; every other argument, limit and error as for viscache_rope,
+ * in place too, plus VC_ERR_ARG for a bad vc_norm. */
+vc_status viscache_norm_rope(const vc_decode_shape *shape, const vc_rope *rope, const vc_norm *norm, int32_t n,
+                             const int32_t *pos, const int32_t *count, const vc_rows *q_in, const vc_rows *q_out,
+                             const vc_rows *k_in, const vc_rows *k_out, void *stream);
+
+/* Host only.  Workspace bytes of the gradient; 0 where it refuses the call. */
+size_t viscache_norm_rope_grad_workspace_bytes(const vc_decode_shape *shape, int32_t n);
+
+/* Device, asynchronous.  The gradient of viscache_norm_rope with the same rope
+ * (`inverse` as in the forward call), norm, pos and count: from the rows that went in
+ * (q, k) and the gradients of the rows that came out (q_dout, k_dout), all of the rows'
+ * type, the gradients of the rows (q_din, k_din; rows of tokens i >= count[b] are left
+ * as they were) and of the weights (q_dweight, k_dweight: DEVICE fp32 [L][d], written,
+ * not added to; zeros where there are no tokens), summed in fp32 in an order that
+ * depends on the shape alone.  A side is left out by NULL for all four of its
+ * arguments.  q_din may be q or q_dout (the same data and strides), k_din likewise;
+ * otherwise they must not overlap.  `workspace`: DEVICE, 256-byte aligned, its
+ * contents on entry do not matter and none are kept.  Limits as for viscache_rope,
+ * and L < 2^17. */
+vc_status viscache_norm_rope_grad(const vc_decode_shape *shape, const vc_rope *rope, const vc_norm *norm, int32_t n,
+                                  const int32_t *pos, const int32_t *count, const vc_rows *q, const vc_rows *q_dout,
+                                  const vc_rows *q_din, float *q_dweight, const vc_rows *k, const vc_rows *k_dout,
+                                  const vc_rows *k_din, float *k_dweight, void *workspace, size_t workspace_bytes,
+                                  void *stream);
+
 /* Static text for a status code. */
 const char *viscache_strerror(vc_status s);
 

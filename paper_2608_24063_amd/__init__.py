@@ -71,6 +71,10 @@ class vc_rope(ctypes.Structure):
                 ("inverse", c_i32), ("scale", c_f32), ("theta", c_f64), ("inv_freq", P(c_f64))]
 
 
+class vc_norm(ctypes.Structure):
+    _fields_ = [("eps", c_f32), ("weight_fp32", c_i32), ("q_weight", c_vp), ("k_weight", c_vp)]
+
+
 class VisCacheError(RuntimeError):
     def __init__(self, status: int, what: str):
         super().__init__(f"{what}: {strerror(status)} (status {status})")
@@ -129,6 +133,10 @@ def lib() -> ctypes.CDLL:
         L.viscache_q8_step.argtypes = [c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_i32, c_f32, c_i32, c_vp,
                                        ctypes.c_size_t, c_vp]
         L.viscache_rope.argtypes = [c_vp, c_vp, c_i32, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp]
+        L.viscache_norm_rope.argtypes = [c_vp, c_vp, c_vp, c_i32] + [c_vp] * 7
+        L.viscache_norm_rope_grad_workspace_bytes.argtypes = [c_vp, c_i32]
+        L.viscache_norm_rope_grad_workspace_bytes.restype = ctypes.c_size_t
+        L.viscache_norm_rope_grad.argtypes = [c_vp, c_vp, c_vp, c_i32] + [c_vp] * 11 + [ctypes.c_size_t, c_vp]
         L.viscache_strerror.argtypes = [c_i32]
         L.viscache_strerror.restype = ctypes.c_char_p
         for name in ("viscache_budget", "viscache_out_rows", "viscache_prune", "viscache_prune_score_offsets",
@@ -136,7 +144,8 @@ def lib() -> ctypes.CDLL:
                      "viscache_append_kv", "viscache_decode_attn", "viscache_decode_step",
                      "viscache_decode_step_q4", "viscache_decode_step_noalloc", "viscache_decode_plan",
                      "viscache_decode_step_planned", "viscache_quantize_rows", "viscache_q8_append",
-                     "viscache_q8_read", "viscache_q8_attend", "viscache_q8_step", "viscache_rope"):
+                     "viscache_q8_read", "viscache_q8_attend", "viscache_q8_step", "viscache_rope",
+                     "viscache_norm_rope", "viscache_norm_rope_grad"):
             getattr(L, name).restype = c_i32
         _lib = L
     return _lib
@@ -388,6 +397,28 @@ def viscache_q8_step(shape: vc_decode_shape, cache: vc_q8cache, rope, pos: int, 
     _check(st, "viscache_q8_step")
 
 
+def viscache_norm_rope(shape: vc_decode_shape, rope: vc_rope, norm: vc_norm, n: int, pos: int, count: int, q_in, q_out,
+                       k_in, k_out, stream: int) -> None:
+    """q_in ... k_out: vc_rows or None."""
+    st = lib().viscache_norm_rope(_ref(shape), _ref(rope), _ref(norm), _int32(n), pos, count, _ref(q_in), _ref(q_out),
+                                  _ref(k_in), _ref(k_out), stream)
+    _check(st, "viscache_norm_rope")
+
+
+def viscache_norm_rope_grad_workspace_bytes(shape: vc_decode_shape, n: int) -> int:
+    return int(lib().viscache_norm_rope_grad_workspace_bytes(_ref(shape), _int32(n)))
+
+
+def viscache_norm_rope_grad(shape: vc_decode_shape, rope: vc_rope, norm: vc_norm, n: int, pos: int, count: int, q,
+                            q_dout, q_din, q_dweight: int, k, k_dout, k_din, k_dweight: int, workspace: int,
+                            workspace_bytes: int, stream: int) -> None:
+    """q ... k_din: vc_rows or None."""
+    st = lib().viscache_norm_rope_grad(_ref(shape), _ref(rope), _ref(norm), _int32(n), pos, count, _ref(q),
+                                       _ref(q_dout), _ref(q_din), q_dweight, _ref(k), _ref(k_dout), _ref(k_din),
+                                       k_dweight, workspace, workspace_bytes, stream)
+    _check(st, "viscache_norm_rope_grad")
+
+
 def viscache_strerror(status: int) -> str:
     return strerror(status)
 
@@ -399,4 +430,6 @@ EXPORTED = ("viscache_default_params", "viscache_budget", "viscache_out_rows",
             "viscache_decode_step", "viscache_decode_step_q4", "viscache_decode_step_noalloc",
             "viscache_decode_plan_bytes", "viscache_decode_plan", "viscache_decode_step_planned",
             "viscache_quantize_rows", "viscache_q8_append", "viscache_q8_read",
-            "viscache_q8_attend_workspace_bytes", "viscache_q8_attend", "viscache_rope", "viscache_q8_step", "viscache_strerror")
+            "viscache_q8_attend_workspace_bytes", "viscache_q8_attend", "viscache_rope", "viscache_q8_step",
+            "viscache_norm_rope", "viscache_norm_rope_grad_workspace_bytes", "viscache_norm_rope_grad",
+            "viscache_strerror")

@@ -1,0 +1,300 @@
+// k_norm_rope.hip -- norm of each query and key head, its weight and the rotation
+// by positions in one pass, and the gradient of all three:
+//   r = (mean x^2 + eps)^-1/2,  y = w x r,  out = R y,
+//   g = R^T dout,  n = x r,  dx = r (w g - n mean(w g n)),  dw = sum g n
+// over a layer's tokens and heads.  R is the rotation of k_rope.hip (its angles in 64
+// bits); all else is fp32, rounded once to the rows' type.  d is a power of two, so
+// the means are exact products.
+//
+// Bound by memory: every value is read and written once, streamed.  A row lies over d /
+// (2N) lanes (N values in 16 bytes), which exchange its sums by DPP.
+#include "vc_norm.h"
+#include "vc_q8_device.h"
+
+namespace vc {
+
+namespace {
+
+// x over the lane (lane & ~(PER - 1)) .. + PER - 1, in each of them.
+template <int PER>
+__device__ __forceinline__ float sum_lanes(float x) {
+  const auto dpp = [&](auto c) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), decltype(c)::value, 0xF,
+                                                                 0xF, false));
+  };
+  x += dpp(std::integral_constant<int, 0xB1>{});                  // lane ^ 1
+  x += dpp(std::integral_constant<int, 0x4E>{});                  // lane ^ 2
+  if (PER >= 8) x += dpp(std::integral_constant<int, 0x141>{});   // mirrored in 8: the other quad
+  if (PER >= 16) x += dpp(std::integral_constant<int, 0x140>{});  // mirrored in 16: the other 8
+  return x;
+}
+
+// A lane's place in the rows: chunks at elements o1 and o2, frequencies N c ...
+template <bool F32, bool ADJ, int D>
+struct Place {
+  using C = Chunk<F32>;
+  static constexpr int N = C::N, PER = D / (2 * N), HS = 64 / PER;  // lanes of a row, rows of a wave
+  int c, o1, o2;
+  bool rotated;
+  __device__ __forceinline__ Place(int lane, int rot) {
+    c = lane % PER;
+    rotated = c < rot / (2 * N);
+    o1 = rotated && !ADJ ? N * c : 2 * N * c;
+    o2 = rotated && !ADJ ? rot / 2 + N * c : 2 * N * c + N;
+  }
+  // The weights of the lane's channels.
+  __device__ __forceinline__ void weights(const void *w, int l, int w_fp32, float (&f)[2 * N]) const {
+    if (!w) {
+#pragma unroll
+      for (int i = 0; i < 2 * N; ++i) f[i] = 0.f;
+      return;
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int at = l * D + (h ? o2 : o1);
+      if (w_fp32) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+          const u32x4 v = ld16(static_cast<const float *>(w) + at + i);
+          f[h * N + i] = __uint_as_float(v.x);
+          f[h * N + i + 1] = __uint_as_float(v.y);
+          f[h * N + i + 2] = __uint_as_float(v.z);
+          f[h * N + i + 3] = __uint_as_float(v.w);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+          const u32x2 v = ld8(static_cast<const uint16_t *>(w) + at + i);
+          f[h * N + i] = bf16_lo(v.x);
+          f[h * N + i + 1] = bf16_hi(v.x);
+          f[h * N + i + 2] = bf16_lo(v.y);
+          f[h * N + i + 3] = bf16_hi(v.y);
+        }
+      }
+    }
+  }
+  static __device__ __forceinline__ void unpack(u32x4 a, u32x4 b, float (&f)[2 * N]) {
+    float x[N], y[N];
+    C::unpack(a, x);
+    C::unpack(b, y);
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = x[i], f[N + i] = y[i];
+  }
+  __device__ __forceinline__ void rotate(float (&f)[2 * N], const float2 (&w)[N]) const {
+    if (!rotated) return;
+    if (ADJ) {
+#pragma unroll
+      for (int m = 0; m < N; ++m) turn(f[2 * m], f[2 * m + 1], w[m]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < N; ++k) turn(f[k], f[N + k], w[k]);
+    }
+  }
+  // Rounded to the rows' type, the only rounding to fewer bits.
+  __device__ __forceinline__ void store(char *row, const float (&f)[2 * N]) const {
+    float x[N], y[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = f[i], y[i] = f[N + i];
+    st16_stream(row + sizeof(uint32_t) / (F32 ? 1 : 2) * o1, C::pack(x));
+    st16_stream(row + sizeof(uint32_t) / (F32 ? 1 : 2) * o2, C::pack(y));
+  }
+  static __device__ __forceinline__ float squares(const float (&f)[2 * N]) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 2 * N; ++i) s = fmaf(f[i], f[i], s);
+    return sum_lanes<PER>(s);
+  }
+};
+
+// (mean + eps)^-1/2 of a sum of squares, within 1.5 steps of fp32.
+template <int D>
+__device__ __forceinline__ float inv_rms(float sum, float eps) {
+  return __builtin_amdgcn_rsqf(fmaf(sum, 1.f / D, eps));
+}
+
+// A workgroup takes TPW tokens of one layer, each with 4 / TPW waves.
+template <bool F32, bool ADJ, int D, int TPW>
+__global__ __launch_bounds__(256) void k_norm_rope(NormPlan p) {
+  using Pl = Place<F32, ADJ, D>;
+  constexpr int N = Pl::N, HS = Pl::HS, kWaves = 4 / TPW;
+  __shared__ float2 cs[TPW][kRopeMaxHalf];
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t toks = (int64_t)p.B * p.n;
+  const int64_t groups = (toks + TPW - 1) / TPW;
+  const int64_t bid = blockIdx.x;
+  const int l = (int)(bid / groups);
+  const int64_t g0 = bid % groups * TPW;
+  const int half = p.t.rot / 2;
+  const Pl pl(lane, p.t.rot);
+  float wq[2 * N], wk[2 * N];
+  pl.weights(p.qw, l, p.w_fp32, wq);
+  pl.weights(p.kw, l, p.w_fp32, wk);
+  for (int e = tid; e < TPW * kRopeMaxHalf; e += 256) {
+    const int t = e / kRopeMaxHalf, i = e % kRopeMaxHalf;
+    const int64_t g = g0 + t;
+    if (i < half && g < toks) cs[t][i] = turn_of(p.t, i, ldg(p.pos + axis_of(p.t, i) * toks + g));
+  }
+  __syncthreads();
+  const int t = w / kWaves, sub = w % kWaves;
+  const int64_t g = g0 + t;
+  if (g >= toks) return;
+  const int b = (int)(g / p.n), i = (int)(g % p.n);
+  if (p.count && i >= ldg(p.count + b)) return;
+  float2 w2[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) w2[k] = pl.rotated ? cs[t][N * pl.c + k] : make_float2(1.f, 0.f);
+  const int H = p.Hq + p.Hkv;
+  constexpr int64_t E = F32 ? 4 : 2;
+  auto row0 = [&](const RowsDesc &r) { return r.base + E * (l * r.layer + b * r.seq + i * r.token); };
+  const uint64_t qi = row0(p.qi), qo = row0(p.qo), ki = row0(p.ki), ko = row0(p.ko);
+  const int64_t qih = E * p.qi.head, qoh = E * p.qo.head, kih = E * p.ki.head, koh = E * p.ko.head;
+  for (int h = sub * HS + lane / Pl::PER; h < H; h += kWaves * HS) {
+    const bool isq = h < p.Hq;
+    const int hh = isq ? h : h - p.Hq;
+    const char *src = reinterpret_cast<const char *>((isq ? qi : ki) + hh * (isq ? qih : kih));
+    char *dst = reinterpret_cast<char *>((isq ? qo : ko) + hh * (isq ? qoh : koh));
+    float x[2 * N];
+    Pl::unpack(ld16_stream(src + E * pl.o1), ld16_stream(src + E * pl.o2), x);
+    const float r = inv_rms<D>(Pl::squares(x), p.eps);
+#pragma unroll
+    for (int k = 0; k < 2 * N; ++k) x[k] = x[k] * r * (isq ? wq[k] : wk[k]);
+    pl.rotate(x, w2);
+    pl.store(dst, x);
+  }
+}
+
+// The gradient.  A wave takes every (4 groups)-th token of its layer, one at a time, the
+// queries and then the keys, and keeps its lanes' sums over all of them for dw; the
+// workgroup's sums go to `part`, and k_dweight adds those up in a fixed order.
+template <bool F32, bool ADJ, int D>
+__global__ __launch_bounds__(256) void k_norm_rope_grad(NormPlan p) {
+  using Pl = Place<F32, ADJ, D>;
+  constexpr int N = Pl::N, HS = Pl::HS, PER = Pl::PER;
+  constexpr int64_t E = F32 ? 4 : 2;
+  __shared__ float2 cs[4][kRopeMaxHalf];
+  __shared__ float sums[4][2][D];
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t toks = (int64_t)p.B * p.n;
+  const int l = (int)(blockIdx.x / (uint32_t)p.groups), grp = (int)(blockIdx.x % (uint32_t)p.groups);
+  const int half = p.t.rot / 2;
+  const Pl pl(lane, p.t.rot);
+  float ws[2][2 * N], dw[2][2 * N];
+  pl.weights(p.qw, l, p.w_fp32, ws[0]);
+  pl.weights(p.kw, l, p.w_fp32, ws[1]);
+#pragma unroll
+  for (int k = 0; k < 2 * N; ++k) dw[0][k] = dw[1][k] = 0.f;
+  for (int64_t g = (int64_t)grp * 4 + w; g < toks; g += 4 * (int64_t)p.groups) {
+    const int b = (int)(g / p.n), i = (int)(g % p.n);
+    if (p.count && i >= ldg(p.count + b)) continue;  // wave-uniform
+    if (lane < half) cs[w][lane] = turn_of(p.t, lane, ldg(p.pos + axis_of(p.t, lane) * toks + g));
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): the wave's own table is written
+    __builtin_amdgcn_wave_barrier();
+    float2 w2[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) w2[k] = pl.rotated ? cs[w][N * pl.c + k] : make_float2(1.f, 0.f);
+    auto side = [&](int H, const RowsDesc &xi, const RowsDesc &gi, const RowsDesc &xo, const float (&wt)[2 * N],
+                    float (&acc)[2 * N]) {
+      auto row0 = [&](const RowsDesc &r) { return r.base + E * (l * r.layer + b * r.seq + i * r.token); };
+      const uint64_t xb = row0(xi), gb = row0(gi), ob = row0(xo);
+      for (int h = lane / PER; h < H; h += HS) {
+        const char *xs = reinterpret_cast<const char *>(xb + E * h * xi.head);
+        const char *gs = reinterpret_cast<const char *>(gb + E * h * gi.head);
+        float x[2 * N], q[2 * N];
+        const u32x4 a0 = ld16_stream(xs + E * pl.o1), a1 = ld16_stream(xs + E * pl.o2);
+        const u32x4 b0 = ld16_stream(gs + E * pl.o1), b1 = ld16_stream(gs + E * pl.o2);
+        Pl::unpack(a0, a1, x);
+        Pl::unpack(b0, b1, q);
+        pl.rotate(q, w2);
+        const float r = inv_rms<D>(Pl::squares(x), p.eps);
+        float dot = 0.f;
+#pragma unroll
+        for (int k = 0; k < 2 * N; ++k) {
+          x[k] *= r;                           // n
+          acc[k] = fmaf(q[k], x[k], acc[k]);   // g n
+          q[k] *= wt[k];                       // w g
+          dot = fmaf(q[k], x[k], dot);
+        }
+        const float m = sum_lanes<PER>(dot) * (1.f / D);
+#pragma unroll
+        for (int k = 0; k < 2 * N; ++k) q[k] = r * fmaf(-x[k], m, q[k]);
+        pl.store(reinterpret_cast<char *>(ob + E * h * xo.head), q);
+      }
+    };
+    side(p.Hq, p.qi, p.qg, p.qo, ws[0], dw[0]);
+    side(p.Hkv, p.ki, p.kg, p.ko, ws[1], dw[1]);
+    __builtin_amdgcn_wave_barrier();
+  }
+  // The wave's lanes of the same channels, then the waves.
+#pragma unroll
+  for (int s = 0; s < 2; ++s)
+#pragma unroll
+    for (int k = 0; k < 2 * N; ++k) {
+      float v = dw[s][k];
+#pragma unroll
+      for (int m = PER; m < 64; m *= 2) v += shfl_xor(v, m);
+      if (lane < PER) sums[w][s][(k < N ? pl.o1 : pl.o2 - N) + k] = v;
+    }
+  __syncthreads();
+  float *to = p.part + (int64_t)blockIdx.x * 2 * D;
+  for (int e = tid; e < 2 * D; e += 256) {
+    const float *f = &sums[0][0][0] + e;
+    stg(to + e, (f[0] + f[2 * D]) + (f[4 * D] + f[6 * D]));
+  }
+}
+
+// dw of 16 channels of one layer and side: 64 threads a channel add up the groups' sums.
+template <int D>
+__global__ __launch_bounds__(1024) void k_dweight(NormPlan p) {
+  __shared__ float red[64][17];
+  const int tid = threadIdx.x, ch = tid % 16, j0 = tid / 16;
+  constexpr int CG = D / 16;
+  const int cg = (int)(blockIdx.x % CG), s = (int)(blockIdx.x / CG % 2), l = (int)(blockIdx.x / (2 * CG));
+  float *out = s ? p.dkw : p.dqw;
+  if (!out) return;  // (uniform)
+  const float *from = p.part + (int64_t)l * p.groups * 2 * D + s * D + cg * 16 + ch;
+  float v = 0.f;
+#pragma unroll 8
+  for (int j = j0; j < p.groups; j += 64) v += ldg(from + (int64_t)j * 2 * D);
+  red[j0][ch] = v;
+  __syncthreads();
+  for (int m = 32; m >= 1; m /= 2) {
+    if (j0 < m) red[j0][ch] += red[j0 + m][ch];
+    __syncthreads();
+  }
+  if (j0 == 0) stg(out + l * D + cg * 16 + ch, red[0][ch]);
+}
+
+template <bool F32, bool ADJ, int D>
+hipError_t launch(const NormPlan &p, bool grad, hipStream_t st) {
+  const int64_t toks = (int64_t)p.B * p.n;
+  if (grad) {
+    hipLaunchKernelGGL((k_norm_rope_grad<F32, ADJ, D>), dim3((uint32_t)(p.groups * p.L)), dim3(256), 0, st, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((k_dweight<D>), dim3((uint32_t)(p.L * 2 * (D / 16))), dim3(1024), 0, st, p);
+    return hipGetLastError();
+  }
+  // Tokens of a workgroup as for the rotation alone (launch_rope).
+  if (p.Hq + p.Hkv <= 2 * Place<F32, ADJ, D>::HS && toks * p.L >= 2048)
+    hipLaunchKernelGGL((k_norm_rope<F32, ADJ, D, 4>), dim3((uint32_t)((toks + 3) / 4 * p.L)), dim3(256), 0, st, p);
+  else
+    hipLaunchKernelGGL((k_norm_rope<F32, ADJ, D, 1>), dim3((uint32_t)(toks * p.L)), dim3(256), 0, st, p);
+  return hipGetLastError();
+}
+
+template <bool F32, bool ADJ>
+hipError_t launch(const NormPlan &p, bool grad, hipStream_t st) {
+  return p.d == 128 ? launch<F32, ADJ, 128>(p, grad, st) : launch<F32, ADJ, 64>(p, grad, st);
+}
+
+hipError_t launch(const NormPlan &p, bool grad, hipStream_t st) {
+  if (p.fp32) return p.t.adjacent ? launch<true, true>(p, grad, st) : launch<true, false>(p, grad, st);
+  return p.t.adjacent ? launch<false, true>(p, grad, st) : launch<false, false>(p, grad, st);
+}
+
+}  // namespace
+
+hipError_t launch_norm_rope(const NormPlan &p, hipStream_t st) { return launch(p, false, st); }
+hipError_t launch_norm_rope_grad(const NormPlan &p, hipStream_t st) { return launch(p, true, st); }
+
+}  // namespace vc

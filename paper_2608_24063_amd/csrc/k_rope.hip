@@ -20,30 +20,6 @@ namespace vc {
 
 namespace {
 
-// 16 bytes of a row as floats, and back.
-template <bool F32>
-struct Chunk {
-  static constexpr int N = F32 ? 4 : 8;
-  static __device__ __forceinline__ void unpack(u32x4 w, float (&f)[N]) {
-    const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (F32) {
-        f[i] = __uint_as_float(ws[i]);
-      } else {
-        f[(2 * i) % N] = bf16_lo(ws[i]);
-        f[(2 * i + 1) % N] = bf16_hi(ws[i]);
-      }
-    }
-  }
-  static __device__ __forceinline__ u32x4 pack(const float (&f)[N]) {
-    if (F32)
-      return u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
-    return u32x4{pack_bf16(f[0], f[1]), pack_bf16(f[2 % N], f[3 % N]), pack_bf16(f[4 % N], f[5 % N]),
-                 pack_bf16(f[6 % N], f[7 % N])};
-  }
-};
-
 // A workgroup takes TPW tokens of one layer, each with 4 / TPW waves.
 template <bool F32, bool ADJ, int TPW>
 __global__ __launch_bounds__(256) void k_rope(RopePlan p) {

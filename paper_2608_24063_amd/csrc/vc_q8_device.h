@@ -125,6 +125,30 @@ __device__ __forceinline__ u32x4 transpose4(uint32_t w0, uint32_t w1, uint32_t w
                __builtin_amdgcn_perm(t3, t2, 0x05040100u), __builtin_amdgcn_perm(t3, t2, 0x07060302u)};
 }
 
+// 16 bytes of a row as floats, and back.
+template <bool F32>
+struct Chunk {
+  static constexpr int N = F32 ? 4 : 8;
+  static __device__ __forceinline__ void unpack(u32x4 w, float (&f)[N]) {
+    const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (F32) {
+        f[i] = __uint_as_float(ws[i]);
+      } else {
+        f[(2 * i) % N] = bf16_lo(ws[i]);
+        f[(2 * i + 1) % N] = bf16_hi(ws[i]);
+      }
+    }
+  }
+  static __device__ __forceinline__ u32x4 pack(const float (&f)[N]) {
+    if (F32)
+      return u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
+    return u32x4{pack_bf16(f[0], f[1]), pack_bf16(f[2 % N], f[3 % N]), pack_bf16(f[4 % N], f[5 % N]),
+                 pack_bf16(f[6 % N], f[7 % N])};
+  }
+};
+
 // The pair (x1, x2) turned: cs = scale (cos a, sin a).
 __device__ __forceinline__ void turn(float &x1, float &x2, float2 cs) {
   const float a = x1, b = x2;

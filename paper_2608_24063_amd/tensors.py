@@ -9,7 +9,7 @@ import struct
 import torch
 
 from . import (VC_ERR_WORKSPACE, VC_PRUNE_EVENTS, VC_Q8_BLOCK, VisCacheError, _int32, lib, VC_Q8_E4M3, VC_Q8_INT8, VC_RANK_GLOBAL, make_params, make_prune_io, make_shape, prune_with_io, vc_cache,
-               vc_decode_shape, vc_q8cache, vc_qcache, vc_rope, vc_rows, viscache_append_kv, viscache_budget, viscache_decode_attn,
+               vc_decode_shape, vc_norm, vc_q8cache, vc_qcache, vc_rope, vc_rows, viscache_append_kv, viscache_budget, viscache_decode_attn,
                viscache_decode_plan, viscache_decode_step, viscache_decode_step_noalloc,
                viscache_decode_step_planned, viscache_decode_step_q4,
                viscache_decode_step_workspace_bytes,
@@ -232,6 +232,8 @@ class DecodeCache:
 
 _pack_rows = struct.Struct("5q").pack
 assert ctypes.sizeof(vc_rows) == struct.calcsize("5q")
+_pack_norm = struct.Struct("fi2q").pack
+assert ctypes.sizeof(vc_norm) == struct.calcsize("fi2q")
 _current_device = getattr(torch._C, "_cuda_getDevice", None)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _BF16, _FP32 = torch.bfloat16, torch.float32
@@ -354,6 +356,133 @@ class Rope:
         out = q_out, k_out
         _changed(out if q is not None and k is not None else (q_out,) if k is None else (k_out,))
         return out
+
+
+class NormRope:
+    """Norm of every query and key head, its weights and a rotation in one pass
+    (viscache_norm_rope), and their gradient.  rope: the Rope that turns the normed
+    rows."""
+
+    def __init__(self, rope: Rope, eps: float = 1e-6):
+        self.rope, self.d, self.eps = rope, rope.d, float(eps)
+        self._bytes = {}
+        self._lib = lib()
+
+    def _weight(self, w, name, L, typ, index) -> int:
+        """Address of contiguous weights [L, d]."""
+        if w.shape != (L, self.d) or w.dtype is not typ or w.get_device() != index or not w.is_contiguous():
+            _refuse(w, name, (L, self.d), f"contiguous {typ}", index)
+        return w.data_ptr()
+
+    def _call(self, pos, q, k, q_weight, k_weight, count):
+        """What both directions look at: the shape's address, (L, B, n), the rows' type
+        and GPU, the norm, and the addresses of pos and count."""
+        ref = q if q is not None else k
+        if ref is None:
+            raise ValueError("no rows")
+        if (q is None) != (q_weight is None) or (k is None) != (k_weight is None):
+            raise ValueError("rows without their weights, or weights without their rows")
+        typ, index = ref.dtype, ref.get_device()
+        L, B, n, Hq, d = ref.shape
+        if (typ is not _BF16 and typ is not _FP32) or d != self.d:
+            _refuse(ref, "q" if q is not None else "k", ref.shape[:-1] + (self.d,), "bf16 or fp32", max(index, 0))
+        Hkv = Hq  # of the one that there is
+        if k is not None and k is not ref:
+            Hkv = k.shape[3] if k.dim() == 5 else 0
+            if k.shape != (L, B, n, Hkv, d):
+                _refuse(k, "k", (L, B, n, "heads", d), typ, index)
+        w = q_weight if q_weight is not None else k_weight
+        wtyp = w.dtype
+        if wtyp is not _BF16 and wtyp is not _FP32:
+            _refuse(w, "q_weight" if q is not None else "k_weight", (L, self.d), "bf16 or fp32", index)
+        at = _ints(pos, "pos", (3, B, n), index), _ints(count, "count", (B,), index)
+        norm = _pack_norm(self.eps, wtyp is _FP32, 0 if q is None else self._weight(q_weight, "q_weight", L, wtyp, index),
+                          0 if k is None else self._weight(k_weight, "k_weight", L, wtyp, index))
+        shapes, key = self.rope._shapes, (L, B, Hq, Hkv)
+        shape = shapes.get(key)
+        if shape is None:
+            shape = vc_decode_shape(B, L, Hq, Hkv, d)
+            shape = shapes[key] = ctypes.addressof(shape), shape
+        return shape[0], (L, B, n), typ, index, norm, at
+
+    @staticmethod
+    def _no_grad(*tensors) -> None:
+        if torch.is_grad_enabled():
+            for t in tensors:
+                if t is not None and t.requires_grad:
+                    raise ValueError("a tensor requires grad: autograd does not see the normed rotation")
+
+    def apply(self, pos, q=None, k=None, q_weight=None, k_weight=None, q_out=None, k_out=None, inverse: bool = False,
+              count=None):
+        """Norms q [L, B, n, Hq, d] and k [L, B, n, Hkv, d] (either may be None; both
+        bf16 or fp32), multiplies them by their layers' q_weight and k_weight [L, d]
+        (bf16 or fp32, both of one type) and turns them by pos int32 [3, B, n] into q_out
+        and k_out, by default in place.  Every other argument, heads, streams and
+        autograd as for Rope.apply: tensors that require grad are refused where it
+        records, and a program calls apply and grad in an autograd function of its
+        own.  Returns (q_out, k_out)."""
+        self._no_grad(q, k, q_weight, k_weight, q_out, k_out)
+        shape, (L, B, n), typ, index, norm, at = self._call(pos, q, k, q_weight, k_weight, count)
+        qi = qo = ki = ko = None
+        out = []
+        if q is not None:
+            qi = _take(q, "q", None, typ, index)
+            qo = qi if q_out is None else _take(q_out, "q_out", q.shape, typ, index)
+            q_out = q if q_out is None else q_out
+            out.append(q_out)
+        if k is not None:
+            ki = _take(k, "k", None, typ, index)
+            ko = ki if k_out is None else _take(k_out, "k_out", k.shape, typ, index)
+            k_out = k if k_out is None else k_out
+            out.append(k_out)
+        if L == 0 or B == 0 or n == 0:
+            return q_out, k_out
+        _enqueue("viscache_norm_rope", self._lib.viscache_norm_rope, index, shape,
+                 self.rope._address[typ is _FP32][bool(inverse)], norm, n, *at, qi, qo, ki, ko)
+        _changed(out)
+        return q_out, k_out
+
+    def grad(self, pos, q=None, k=None, q_weight=None, k_weight=None, q_dout=None, k_dout=None, q_din=None, k_din=None,
+             inverse: bool = False, count=None):
+        """The gradient of apply with the same pos, q, k, weights, inverse and count, of
+        which q and k are what went in: from the outputs' gradients q_dout and k_dout
+        (the rows' type) to the rows' gradients, in q_din and k_din (by default new
+        tensors; q or q_dout itself is allowed; rows of tokens past count are left as they were, in new tensors
+        zeros), and the weights', new fp32 tensors [L, d].  Sums are formed
+        in an order that depends on the shape alone.  Returns (q_din, k_din, q_dweight,
+        k_dweight), None for a side without rows."""
+        self._no_grad(q, k, q_weight, k_weight, q_dout, k_dout, q_din, k_din)
+        shape, (L, B, n), typ, index, norm, at = self._call(pos, q, k, q_weight, k_weight, count)
+        if (q is None) != (q_dout is None) or (k is None) != (k_dout is None):
+            raise ValueError("rows without their outputs' gradients, or gradients without rows")
+        new = torch.zeros_like if count is not None else torch.empty_like
+        side, out, dw = [], [], [None, None]
+        for i, (x, g, o, name) in enumerate(((q, q_dout, q_din, "q"), (k, k_dout, k_din, "k"))):
+            if x is None:
+                side += [None, None, None, 0]
+                out.append(None)
+                continue
+            xr, gr = _take(x, name, None, typ, index), _take(g, name + "_dout", x.shape, typ, index)
+            if o is None:
+                o = new(x, memory_format=torch.contiguous_format)
+            dw[i] = torch.empty((L, self.d), dtype=_FP32, device=x.device)
+            side += [xr, gr, _take(o, name + "_din", x.shape, typ, index), dw[i].data_ptr()]
+            out.append(o)
+        if L == 0:
+            return (*out, *dw)
+        if B == 0 or n == 0:
+            return (*out, *[None if w is None else w.zero_() for w in dw])
+        need = self._bytes.get((shape, n))
+        if need is None:
+            if len(self._bytes) >= 4096:
+                self._bytes.clear()
+            need = self._bytes[shape, n] = self._lib.viscache_norm_rope_grad_workspace_bytes(shape, n)
+        # Of this call alone: the allocator orders its reuse after the stream's work.
+        ws = torch.empty((max(need, 1),), dtype=torch.uint8, device=dw[0 if q is not None else 1].device)
+        _enqueue("viscache_norm_rope_grad", self._lib.viscache_norm_rope_grad, index, shape,
+                 self.rope._address[typ is _FP32][bool(inverse)], norm, n, *at, *side, ws.data_ptr(), need)
+        _changed([o for o in out if o is not None])
+        return (*out, *dw)
 
 
 _Q8_BUFFERS = ("k_codes", "v_codes", "k_scale", "v_scale", "k_tail", "v_tail", "row_off", "cap", "len")
@@ -586,4 +715,4 @@ class Q8Cache:
                  int(fp32), scale, most, ws[0], ws[1])
 
 
-__all__ = ["PruneCall", "DecodeCache", "Q8Cache", "Rope", "make_params"]
+__all__ = ["PruneCall", "DecodeCache", "Q8Cache", "Rope", "NormRope", "make_params"]
