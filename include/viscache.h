@@ -632,6 +632,58 @@ vc_status viscache_norm_rope_grad(const vc_decode_shape *shape, const vc_rope *r
                                   const vc_rows *k_din, float *k_dweight, void *workspace, size_t workspace_bytes,
                                   void *stream);
 
+/* ---- a cache that keeps what its rows were given ----------------------------
+ * A decode cache (as vc_cache) with a mass per row: the attention weight that the row
+ * got from all queries and query heads of its group so far, old weight fading by
+ * `decay` with every call.  Attention adds to it on its way, and eviction keeps the
+ * rows of the largest mass.  A cache starts with len 0 and any other contents; rows
+ * that a program writes by itself (viscache_prune's outputs) need a mass of their own. */
+typedef struct {
+  void *k_pool, *v_pool;   /* bf16 rows of d values, 16-byte aligned */
+  float *mass;             /* [pool rows] */
+  const int64_t *row_off;  /* as in vc_cache: unit u owns rows [row_off, row_off + cap) and holds len */
+  const int32_t *cap;
+  int32_t *len;            /* (lengths past 2^31 - 1025 count as that) */
+} vc_mass_cache;
+
+/* Host only.  Workspace bytes viscache_mass_attend needs for n queries a sequence over
+ * caches of at most max_rows rows; 0 where it refuses them. */
+size_t viscache_mass_attend_workspace_bytes(const vc_decode_shape *shape, int32_t n, int32_t max_rows);
+
+/* Device, asynchronous.  Attention of n queries per sequence and layer over the cache.
+ * c = count[b] clamped to [0, n] (DEVICE int32 [B]; NULL: n) queries of sequence b take
+ * part; a sequence without any is left alone, its masses too.
+ * Append: with k and v (bf16, head index the kv head) their rows i < c are appended to
+ * every unit, as far as cap leaves room, with mass 0; base = len before, len grows.  With
+ * k and v NULL the cache holds the queries' rows already (or does without them), and
+ * base = len - c.
+ * Query i attends the rows t < min(base + i + 1, len, max_rows):
+ *   p = softmax_t(scale * q . K_t),  out = sum p_t V_t,
+ *   mass[t] <- decay * mass[t] + sum of p_t over the unit's queries and heads
+ * for t < min(len, max_rows) (masses behind are left as they were).  A query that sees no
+ * row gives zeros and no weight; one with a NaN gives NaN, and NaN to the masses of the
+ * rows it sees.  An infinity or a NaN among a row's values reaches the queries that see
+ * it (as NaN), no others.  Rows i >= c of out are left as they were.  q: bf16; out: bf16
+ * (out_fp32 = 0) or fp32, both indexed by the query head; the rows of q, k, v and out
+ * and the cache must not overlap.
+ * Logits, maxima, sums, weights and masses are fp32, summed in an order that follows
+ * from the shape, max_rows, the lengths and the counts.  A weight meets its value with
+ * 24 bits; with n * Hq/Hkv > 16 and bf16 outputs it is rounded to bf16 there (2^-8 of
+ * itself; a caller that needs more asks for fp32 outputs).
+ * decay: finite, not negative (1: nothing fades; 0: the last call's weights alone).
+ * max_rows bounds every len after the append.  n = 0 does nothing.  n * Hq/Hkv <= 16
+ * (single tokens, short drafts) is one launch, or two where units are cut along their
+ * rows; more take three or four.  `workspace`: DEVICE, at least
+ * viscache_mass_attend_workspace_bytes bytes, 256-byte aligned; contents do not matter and
+ * none are kept, so calls, captured ones among them, may share one as long as they do
+ * not overlap.  VC_ERR_WORKSPACE comes after all other checks.  VC_ERR_UNSUPPORTED for
+ * n * Hq/Hkv > 2^24, 2^23 or more workgroups of a launch, or 2^24 or more columns to
+ * join. */
+vc_status viscache_mass_attend(const vc_decode_shape *shape, const vc_mass_cache *cache, const vc_rows *k,
+                               const vc_rows *v, const vc_rows *q, const vc_rows *out, int32_t n,
+                               const int32_t *count, int32_t out_fp32, float scale, float decay, int32_t max_rows,
+                               void *workspace, size_t workspace_bytes, void *stream);
+
 /* Static text for a status code. */
 const char *viscache_strerror(vc_status s);
 

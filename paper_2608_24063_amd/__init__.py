@@ -75,6 +75,10 @@ class vc_norm(ctypes.Structure):
     _fields_ = [("eps", c_f32), ("weight_fp32", c_i32), ("q_weight", c_vp), ("k_weight", c_vp)]
 
 
+class vc_mass_cache(ctypes.Structure):
+    _fields_ = [("k_pool", c_vp), ("v_pool", c_vp), ("mass", c_vp), ("row_off", c_vp), ("cap", c_vp), ("len", c_vp)]
+
+
 class VisCacheError(RuntimeError):
     def __init__(self, status: int, what: str):
         super().__init__(f"{what}: {strerror(status)} (status {status})")
@@ -137,6 +141,10 @@ def lib() -> ctypes.CDLL:
         L.viscache_norm_rope_grad_workspace_bytes.argtypes = [c_vp, c_i32]
         L.viscache_norm_rope_grad_workspace_bytes.restype = ctypes.c_size_t
         L.viscache_norm_rope_grad.argtypes = [c_vp, c_vp, c_vp, c_i32] + [c_vp] * 11 + [ctypes.c_size_t, c_vp]
+        L.viscache_mass_attend_workspace_bytes.argtypes = [c_vp, c_i32, c_i32]
+        L.viscache_mass_attend_workspace_bytes.restype = ctypes.c_size_t
+        L.viscache_mass_attend.argtypes = [c_vp] * 6 + [c_i32, c_vp, c_i32, c_f32, c_f32, c_i32, c_vp, ctypes.c_size_t,
+                                                        c_vp]
         L.viscache_strerror.argtypes = [c_i32]
         L.viscache_strerror.restype = ctypes.c_char_p
         for name in ("viscache_budget", "viscache_out_rows", "viscache_prune", "viscache_prune_score_offsets",
@@ -145,7 +153,7 @@ def lib() -> ctypes.CDLL:
                      "viscache_decode_step_q4", "viscache_decode_step_noalloc", "viscache_decode_plan",
                      "viscache_decode_step_planned", "viscache_quantize_rows", "viscache_q8_append",
                      "viscache_q8_read", "viscache_q8_attend", "viscache_q8_step", "viscache_rope",
-                     "viscache_norm_rope", "viscache_norm_rope_grad"):
+                     "viscache_norm_rope", "viscache_norm_rope_grad", "viscache_mass_attend"):
             getattr(L, name).restype = c_i32
         _lib = L
     return _lib
@@ -419,6 +427,19 @@ def viscache_norm_rope_grad(shape: vc_decode_shape, rope: vc_rope, norm: vc_norm
     _check(st, "viscache_norm_rope_grad")
 
 
+def viscache_mass_attend_workspace_bytes(shape: vc_decode_shape, n: int, max_rows: int) -> int:
+    return int(lib().viscache_mass_attend_workspace_bytes(_ref(shape), _int32(n), _int32(max_rows)))
+
+
+def viscache_mass_attend(shape: vc_decode_shape, cache: vc_mass_cache, k, v, q: vc_rows, out: vc_rows, n: int, count: int,
+                         out_fp32: int, scale: float, decay: float, max_rows: int, workspace: int, workspace_bytes: int,
+                         stream: int) -> None:
+    """k, v: vc_rows, or None where nothing is appended."""
+    st = lib().viscache_mass_attend(_ref(shape), _ref(cache), _ref(k), _ref(v), _ref(q), _ref(out), _int32(n), count,
+                                    out_fp32, scale, decay, _int32(max_rows), workspace, workspace_bytes, stream)
+    _check(st, "viscache_mass_attend")
+
+
 def viscache_strerror(status: int) -> str:
     return strerror(status)
 
@@ -432,4 +453,4 @@ EXPORTED = ("viscache_default_params", "viscache_budget", "viscache_out_rows",
             "viscache_quantize_rows", "viscache_q8_append", "viscache_q8_read",
             "viscache_q8_attend_workspace_bytes", "viscache_q8_attend", "viscache_rope", "viscache_q8_step",
             "viscache_norm_rope", "viscache_norm_rope_grad_workspace_bytes", "viscache_norm_rope_grad",
-            "viscache_strerror")
+            "viscache_mass_attend_workspace_bytes", "viscache_mass_attend", "viscache_strerror")

@@ -78,7 +78,10 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt8(Q8Attn p) {
   __shared__ Values<D> tv[2] __attribute__((aligned(16)));
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int ln = lane & 31, hf = lane >> 5;
-  const Share sh = share_of(p, blockIdx.x, lane);
+  const Share sh = share_of(p, blockIdx.x, lane, [&](int u) {
+    return Held{rows_held(ldg(p.c.len + u), ldg(p.c.cap + u)),
+                p.count ? min(max(ldg(p.count + u / p.Hkv % p.B), 0), p.n) : p.n, ldg(p.c.row_off + u)};
+  });
   const int u = sh.u, qt = sh.qt, sp = sh.sp, ns = sh.ns;
   if (u < 0) return;
   const int len = sh.len, cnt = sh.cnt, cols = cnt * p.G;
@@ -94,7 +97,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt8(Q8Attn p) {
   const int end = rows_seen(min(col, cl));
   const int wmin = rows_seen(min(c0 + 32 * w, cl));  // fewest rows a column of the wave sees
   const bool live = c0 + 32 * w <= cl;  // the wave has columns (the others only stage)
-  const int64_t blk0 = sh.blk0;
+  const int64_t blk0 = sh.off / kQ8Block;
   const int nsealed = len / kQ8Block;
   const int g = u % p.Hkv, lb = u / p.Hkv;
   auto row_of = [&](const RowsDesc &r, int cc) {

@@ -1,0 +1,54 @@
+// vc_mass.h -- plans and host launchers of the cache that keeps its rows' attention
+// weight: attention (single tokens, prompts) and eviction.  Internal.
+#pragma once
+#include "vc_q8.h"
+
+namespace vc {
+
+constexpr int kMassTile = 32;         // rows of a single token's tile
+constexpr int kMassChunk = 1024;      // rows of a workgroup of k_finish
+constexpr int kMassKeys = 256;        // rows of a workgroup of k_mass_cols
+constexpr int kMassMaxRows = INT32_MAX - 1024;  // so that the end of a row's tile is a row index
+
+// The cache, as in vc_mass_cache.
+struct MassPool {
+  uint16_t *kp, *vp;
+  float *mass;
+  const int64_t *row_off;
+  const int32_t *cap;
+  int32_t *len;
+};
+
+struct MassAttn {
+  MassPool c;
+  RowsDesc q, out, k, v;  // k, v: the rows to append
+  const int32_t *count;   // queries per sequence; null: n
+  int32_t L, B, Hq, Hkv, G, d, units;
+  int32_t wgs;            // workgroups of the attention launch
+  int32_t n, cols;        // queries per sequence; cols = n * G
+  int32_t append, fp32, causal;  // causal: always 1
+  int32_t max_rows;
+  float sc, decay;        // sc = scale * log2(e)
+  // Single tokens (cols <= 16): pieces of `piece` tiles, at most npmax a unit; the
+  // logits of every column and row wait in [unit][cols][ldr] for its maximum and sum.
+  int32_t piece, npmax, ldr;
+  float *logits;
+  // Prompts (npmax 1): nqt column tiles of qcols columns, each in as many key splits
+  // as the launch's workgroups allow (ns 1: whole).
+  int32_t qcols, nqt, ns;
+  float *part_o;          // partial results: [part][qcols][d], [part][qcols]
+  float2 *part_ml;
+  float2 *stat;           // prompts: [unit][cols] maximum and 1 / sum of the weights
+  // Per unit (rows before the call, rows now, queries, pieces): of single tokens in
+  // several pieces, and of prompts that append.
+  int4 *state;
+  int32_t *np;            // prompts: first part and number of parts of each tile
+};
+
+// launch_mass_token: attention (and append) in one launch, or two where units are cut.
+// launch_mass_prompt: append, attention, join where tiles are cut, and the rows' weights.
+hipError_t launch_mass_token(const MassAttn &p, hipStream_t st);
+hipError_t launch_mass_prompt(const MassAttn &p, hipStream_t st);
+hipError_t launch_mass_cols(const MassAttn &p, hipStream_t st);  // called by launch_mass_prompt
+
+}  // namespace vc

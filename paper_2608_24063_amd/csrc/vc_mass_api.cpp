@@ -1,0 +1,150 @@
+// vc_mass_api.cpp -- the C ABI of the cache that keeps its rows' attention weight
+// (include/viscache.h): argument checks, workspace layout and how a call is cut into
+// workgroups.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "../../include/viscache.h"
+#include "vc_host.h"
+#include "vc_mass.h"
+
+using namespace vc;
+
+namespace {
+
+constexpr int kTokenCols = 16;  // columns of the single-token kernel
+
+vc_status check_cache(const vc_mass_cache *c) {
+  if (!c || !c->k_pool || !c->v_pool || !c->mass || !c->row_off || !c->cap || !c->len) return VC_ERR_ARG;
+  if ((reinterpret_cast<uintptr_t>(c->k_pool) | reinterpret_cast<uintptr_t>(c->v_pool)) % 16 != 0 ||
+      reinterpret_cast<uintptr_t>(c->mass) % 4 != 0)
+    return VC_ERR_ARG;
+  return VC_OK;
+}
+
+MassPool bind(const vc_mass_cache *c) {
+  return MassPool{static_cast<uint16_t *>(c->k_pool), static_cast<uint16_t *>(c->v_pool), c->mass, c->row_off, c->cap,
+                  c->len};
+}
+
+// How an attention call is cut, and the parts of its workspace.
+struct Cut {
+  int32_t piece = 0, npmax = 1, ldr = 0, qcols = 0, nqt = 0, ns = 1;
+  int64_t wgs = 0, slots = 0;  // workgroups; columns of partial results
+  size_t ml = 0, stat = 0, state = 0, np = 0, logits = 0, total = 0;
+};
+
+bool attend_cut(const vc_decode_shape *s, int32_t n, int32_t max_rows, Cut &c) {
+  const int64_t units = (int64_t)s->L * s->B * s->Hkv;
+  const int64_t G = s->Hq / s->Hkv, cols = n * G;
+  max_rows = std::min(max_rows, kMassMaxRows);  // no unit holds more
+  if (cols > (int64_t(1) << 24)) return false;
+  if (cols <= kTokenCols) {
+    const int64_t nt = std::max<int64_t>(1, ((int64_t)max_rows + kMassTile - 1) / kMassTile);
+    // Pieces of a multiple of four tiles (one per wave and turn).
+    const int64_t want = units * nt / 512;
+    c.qcols = kTokenCols;
+    c.piece = (int32_t)std::max<int64_t>(8, (want + 3) / 4 * 4);
+    if (nt <= std::max<int64_t>(2 * (int64_t)c.piece, 16)) c.piece = (int32_t)nt;
+    c.npmax = (int32_t)((nt + c.piece - 1) / c.piece);
+    c.wgs = units * c.npmax;
+    c.slots = c.npmax > 1 ? c.wgs * kTokenCols : 0;
+    c.ldr = (int32_t)(nt * kMassTile);
+    // The second launch's workgroups.
+    if (c.npmax > 1 && units * (((int64_t)max_rows + kMassChunk - 1) / kMassChunk) >= kMaxWg) return false;
+  } else {
+    const int64_t nt = std::max<int64_t>(1, ((int64_t)max_rows + kQ8Block - 1) / kQ8Block);
+    c.qcols = cols > 128 ? 256 : 128;
+    const int64_t nqt = (cols + c.qcols - 1) / c.qcols, tiles = units * nqt;
+    if (tiles >= kMaxWg) return false;
+    const int64_t resident = c.qcols == 256 ? 256 : 512;
+    c.nqt = (int32_t)nqt;
+    // Workgroups that the card holds at once share the tiles' rows where that is two
+    // a tile or more (attention over the 8-bit cache was measured on both sides of it).
+    c.ns = tiles * 2 <= resident && nt >= 2 * kQ8SplitBlocks ? 2 : 1;
+    c.wgs = c.ns > 1 ? std::min(resident, tiles * (nt / kQ8SplitBlocks)) : tiles;
+    c.slots = c.ns > 1 ? c.wgs * c.qcols : 0;
+    // The other launches' workgroups: the append's, the join's, the masses'.
+    if (units * (((int64_t)n + kQ8Block - 1) / kQ8Block) >= kMaxWg || (c.slots && units * cols >= 2 * kMaxWg) ||
+        units * (((int64_t)max_rows + kMassKeys - 1) / kMassKeys) >= kMaxWg)
+      return false;
+  }
+  if (c.wgs >= kMaxWg) return false;
+  const bool token = cols <= kTokenCols;
+  c.ml = align_up(sizeof(float) * (size_t)c.slots * (size_t)s->d);
+  c.stat = c.ml + align_up(sizeof(float2) * (size_t)c.slots);
+  c.state = c.stat + (token ? 0 : align_up(sizeof(float2) * (size_t)(units * cols)));
+  c.np = c.state + align_up(sizeof(int4) * (size_t)units);
+  c.logits = c.np + (token || c.ns == 1 ? 0 : align_up(sizeof(int32_t) * 2 * (size_t)(units * c.nqt)));
+  c.total = c.logits + (token ? align_up(sizeof(float) * (size_t)(units * cols) * (size_t)c.ldr) : 0);
+  return true;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t viscache_mass_attend_workspace_bytes(const vc_decode_shape *s, int32_t n, int32_t max_rows) {
+  if (check_shape(s) != VC_OK || n < 0 || max_rows < 0) return 0;
+  Cut c;
+  return attend_cut(s, std::max(n, 1), max_rows, c) ? c.total : 0;
+}
+
+vc_status viscache_mass_attend(const vc_decode_shape *s, const vc_mass_cache *c, const vc_rows *k, const vc_rows *v,
+                               const vc_rows *q, const vc_rows *out, int32_t n, const int32_t *count, int32_t out_fp32,
+                               float scale, float decay, int32_t max_rows, void *workspace, size_t workspace_bytes,
+                               void *stream) {
+  vc_status st = check_shape(s);
+  if (st != VC_OK) return st;
+  if ((st = check_cache(c)) != VC_OK) return st;
+  if (n < 0 || max_rows < 0 || (out_fp32 != 0 && out_fp32 != 1) || !k != !v) return VC_ERR_ARG;
+  if (!(scale > 0.f) || !std::isfinite(scale) || !(decay >= 0.f) || !std::isfinite(decay)) return VC_ERR_ARG;
+  if (n == 0) return VC_OK;
+  if (!rows_ok(q, 2, s->L, s->B, n, s->Hq, s->d, false, false) ||
+      !rows_ok(out, out_fp32 ? 4 : 2, s->L, s->B, n, s->Hq, s->d, true, false))
+    return VC_ERR_ARG;
+  if (k && (!rows_ok(k, 2, s->L, s->B, n, s->Hkv, s->d, false, false) ||
+            !rows_ok(v, 2, s->L, s->B, n, s->Hkv, s->d, false, false)))
+    return VC_ERR_ARG;
+  Cut cut;
+  if (!attend_cut(s, n, max_rows, cut)) return VC_ERR_UNSUPPORTED;
+  if (!workspace || workspace_bytes < cut.total || reinterpret_cast<uintptr_t>(workspace) % kAlign != 0)
+    return VC_ERR_WORKSPACE;
+  MassAttn p{};
+  p.c = bind(c);
+  p.q = desc(q);
+  p.out = desc(out);
+  if (k) {
+    p.k = desc(k);
+    p.v = desc(v);
+    if (n == 1) p.k.token = p.v.token = 0;  // (not checked)
+  }
+  p.count = count;
+  p.L = s->L; p.B = s->B; p.Hq = s->Hq; p.Hkv = s->Hkv; p.G = s->Hq / s->Hkv; p.d = s->d;
+  p.units = s->L * s->B * s->Hkv;
+  p.wgs = (int32_t)cut.wgs;
+  p.n = n;
+  p.cols = n * p.G;
+  p.append = k != nullptr;
+  p.fp32 = out_fp32;
+  p.causal = 1;
+  p.max_rows = std::min(max_rows, kMassMaxRows);
+  p.sc = scale * 1.4426950408889634f;
+  p.decay = decay;
+  p.piece = cut.piece; p.npmax = cut.npmax; p.ldr = cut.ldr;
+  p.qcols = cut.qcols; p.nqt = cut.nqt; p.ns = cut.ns;
+  uint8_t *ws = static_cast<uint8_t *>(workspace);
+  p.part_o = reinterpret_cast<float *>(ws);
+  p.part_ml = reinterpret_cast<float2 *>(ws + cut.ml);
+  p.stat = reinterpret_cast<float2 *>(ws + cut.stat);
+  p.state = reinterpret_cast<int4 *>(ws + cut.state);
+  p.np = reinterpret_cast<int32_t *>(ws + cut.np);
+  p.logits = reinterpret_cast<float *>(ws + cut.logits);
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  const hipError_t e = p.cols <= kTokenCols ? launch_mass_token(p, hs) : launch_mass_prompt(p, hs);
+  return e == hipSuccess ? VC_OK : VC_ERR_HIP;
+}
+
+}  // extern "C"

@@ -276,16 +276,22 @@ __device__ __forceinline__ float wave_sum(float x) {
   return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), 63));
 }
 
+// What a prompt's workgroups have to know of a unit.
+struct Held {
+  int rows, cnt;  // rows held, queries
+  int64_t off;    // its first pool row
+};
+
 // Which column tile and key split a prompt's workgroup takes, of how many, and
 // what the tile's unit is.
 struct Share {
   int u, qt, sp, ns;  // unit (-1: nothing to do), tile, split of ns
   int id;             // where its partial results go
   int len, cnt;       // rows held, queries
-  int64_t blk0;       // the unit's first block
+  int64_t off;        // the unit's first pool row
 };
 
-// Workgroup `bid` of a prompt: tiles in the order of their units, splits
+// Workgroup `bid` of a prompt, by info(u) of its units: tiles in the order of their units, splits
 // innermost, those of a unit on one XCD (they share its L2); every lane of the
 // wave takes part.  Where few tiles are cut along
 // their rows, as many blocks go to each workgroup as make no more splits than
@@ -294,12 +300,12 @@ struct Share {
 // rows with 40 queries each 56.5, 47.8, with up to 40 44.6, 36.5; three of 9001 to
 // 12801 with up to 65 51.6, 48.9; one of 12544 with 30 23.7, 24.0, with 1024 202,
 // 205.)
-__device__ __forceinline__ Share share_of(const Q8Attn &p, uint32_t bid, int lane) {
-  auto queries = [&](int u) { return p.count ? min(max(ldg(p.count + u / p.Hkv % p.B), 0), p.n) : p.n; };
+template <typename Plan, typename Info>
+__device__ __forceinline__ Share share_of(const Plan &p, uint32_t bid, int lane, Info info) {
   if (p.ns == 1) {
     const int id = (int)xcd_block(bid, (uint32_t)p.wgs), u = id / p.nqt;
-    return Share{u, id % p.nqt, 0, 1, id, rows_held(ldg(p.c.len + u), ldg(p.c.cap + u)), queries(u),
-                 ldg(p.c.row_off + u) / kQ8Block};
+    const Held h = info(u);
+    return Share{u, id % p.nqt, 0, 1, id, h.rows, h.cnt, h.off};
   }
   // Lane: tiles K lane .. K lane + K - 1, by their blocks.  Of 256 columns no more
   // than 128, a wave a SIMD, take three quarters of the time (1.4 to 1.6 us a
@@ -313,9 +319,10 @@ __device__ __forceinline__ Share share_of(const Q8Attn &p, uint32_t bid, int lan
   for (int k = 0; k < KM; ++k) {
     if (k >= K) break;  // uniform
     const int t = K * lane + k, u = (int)((uint32_t)min(t, tiles - 1) / (uint32_t)p.nqt);
-    held[k] = rows_held(ldg(p.c.len + u), ldg(p.c.cap + u));
-    cnt[k] = queries(u);
-    off[k] = ldg(p.c.row_off + u);
+    const Held h = info(u);
+    held[k] = h.rows;
+    cnt[k] = h.cnt;
+    off[k] = h.off;
     const int c0 = (t - u * p.nqt) * p.qcols, cl = min(c0 + p.qcols, cnt[k] * p.G) - 1;
     const int seen = min(p.causal ? held[k] - cnt[k] + 1 + (int)((uint32_t)max(cl, 0) / (uint32_t)p.G) : held[k], p.max_rows);
     nb[k] = t < tiles && cl >= c0 ? max((seen + kQ8Block - 1) / kQ8Block, 1) : 0;
@@ -360,8 +367,8 @@ __device__ __forceinline__ Share share_of(const Q8Attn &p, uint32_t bid, int lan
   const int src = __builtin_ctzll(hit);
   auto of = [&](int x) { return __builtin_amdgcn_readlane(x, src); };
   t = of(t);
-  const uint64_t at = (uint32_t)of((int)s.blk0) | (uint64_t)(uint32_t)of((int)(s.blk0 >> 32)) << 32;
-  return Share{t / p.nqt, t % p.nqt, of(s.sp), of(s.ns), id, of(s.len), of(s.cnt), (int64_t)at / kQ8Block};
+  const uint64_t at = (uint32_t)of((int)s.off) | (uint64_t)(uint32_t)of((int)(s.off >> 32)) << 32;
+  return Share{t / p.nqt, t % p.nqt, of(s.sp), of(s.ns), id, of(s.len), of(s.cnt), (int64_t)at};
 }
 
 }  // namespace vc

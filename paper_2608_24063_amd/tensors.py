@@ -9,11 +9,11 @@ import struct
 import torch
 
 from . import (VC_ERR_WORKSPACE, VC_PRUNE_EVENTS, VC_Q8_BLOCK, VisCacheError, _int32, lib, VC_Q8_E4M3, VC_Q8_INT8, VC_RANK_GLOBAL, make_params, make_prune_io, make_shape, prune_with_io, vc_cache,
-               vc_decode_shape, vc_norm, vc_q8cache, vc_qcache, vc_rope, vc_rows, viscache_append_kv, viscache_budget, viscache_decode_attn,
+               vc_decode_shape, vc_mass_cache, vc_norm, vc_q8cache, vc_qcache, vc_rope, vc_rows, viscache_append_kv, viscache_budget, viscache_decode_attn,
                viscache_decode_plan, viscache_decode_step, viscache_decode_step_noalloc,
                viscache_decode_step_planned, viscache_decode_step_q4,
                viscache_decode_step_workspace_bytes,
-               viscache_decode_workspace_bytes, viscache_out_rows, viscache_prune_workspace_bytes,
+               viscache_decode_workspace_bytes, viscache_mass_attend_workspace_bytes, viscache_out_rows, viscache_prune_workspace_bytes,
                viscache_q8_append, viscache_q8_attend_workspace_bytes, viscache_quantize_rows)
 
 
@@ -485,10 +485,60 @@ class NormRope:
         return (*out, *dw)
 
 
-_Q8_BUFFERS = ("k_codes", "v_codes", "k_scale", "v_scale", "k_tail", "v_tail", "row_off", "cap", "len")
+class _Attends:
+    """What caches share whose attention takes a workspace: shape, device, row bound."""
+
+    def _shaped(self, L, B, Hq, Hkv, d, caps, device) -> list:
+        self.L, self.B, self.Hq, self.Hkv, self.d = L, B, Hq, Hkv, d
+        self.shape = vc_decode_shape(B, L, Hq, Hkv, d)
+        self.device = torch.device(device)
+        if self.device.type == "cuda" and self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self._index = self.device.index if self.device.type == "cuda" else -1
+        self.units = L * B * Hkv
+        caps = [int(c) for c in caps]
+        if len(caps) != self.units or min(caps, default=0) < 0:
+            raise ValueError(f"{len(caps)} capacities, need {self.units}, none negative")
+        self.max_cap = max(caps)
+        self._ws, self._ws_of, self._kept = None, {}, []
+        self._shape_at = ctypes.addressof(self.shape)
+        self._lib = lib()
+        return caps
+
+    def _bind(self, need, buffers) -> list:
+        """The buffers by the names and (shape, type) of `need`, as attributes; their addresses."""
+        for name, (shape, t) in need.items():
+            b = buffers[name]
+            if b.shape != shape or b.dtype is not t or b.device != self.device or not b.is_contiguous():
+                _refuse(b, name, shape, f"contiguous {t}", self._index)
+            setattr(self, name, b)
+        return [buffers[name].data_ptr() for name in need]
+
+    def _workspace(self, n: int, max_rows: int):
+        """(address, bytes) of the workspace, grown when a call needs more than any
+        before it (a call that is captured into a graph must have run once)."""
+        ws = self._ws_of.get((n, max_rows))
+        if ws is None:
+            need = self._needs(n, max_rows)
+            had = 0 if self._ws is None else self._ws.numel()
+            if self._ws is None or had < need:
+                if torch.cuda.is_current_stream_capturing():
+                    raise RuntimeError("the workspace is too small: run the call once before it is captured")
+                # By half at least, so that all that are kept come to three times the largest.
+                self._ws = torch.empty((max(need, had + had // 2),), dtype=torch.uint8, device=self.device)
+                self._kept.append(self._ws)  # a graph captured before this goes on using the one it knows
+                self._ws_of.clear()
+            elif len(self._ws_of) >= 4096:  # bounds that change with every call
+                self._ws_of.clear()
+            ws = self._ws_of[n, max_rows] = self._ws.data_ptr(), self._ws.numel()
+        return ws
+
+    def _bound(self, max_rows) -> int:
+        """The row bound of a call: no unit holds more rows than it has room for."""
+        return self.max_cap if max_rows is None else min(_int32(max_rows), self.max_cap)
 
 
-class Q8Cache:
+class Q8Cache(_Attends):
     """A decode cache in 8 bits (viscache_q8_*) over L layers x B sequences x
     Hkv heads: unit u = (l*B + b)*Hkv + g has room for caps[u] rows.  format:
     "int8" or "e4m3".  `buffers`: the cache's tensors by name (k_codes, v_codes,
@@ -512,19 +562,9 @@ class Q8Cache:
     FORMATS = {"int8": (VC_Q8_INT8, torch.int8), "e4m3": (VC_Q8_E4M3, torch.float8_e4m3fn)}
 
     def __init__(self, L, B, Hq, Hkv, d, caps, device, format: str = "e4m3", buffers=None):
-        self.L, self.B, self.Hq, self.Hkv, self.d = L, B, Hq, Hkv, d
-        self.shape = vc_decode_shape(B, L, Hq, Hkv, d)
-        self.device = torch.device(device)
-        if self.device.type == "cuda" and self.device.index is None:
-            self.device = torch.device("cuda", torch.cuda.current_device())
-        self._index = self.device.index if self.device.type == "cuda" else -1
-        self.units = L * B * Hkv
-        caps = [int(c) for c in caps]
-        if len(caps) != self.units or min(caps, default=0) < 0:
-            raise ValueError(f"{len(caps)} capacities, need {self.units}, none negative")
+        caps = self._shaped(L, B, Hq, Hkv, d, caps, device)
         code, typ = self.FORMATS[format]
         self.format = format
-        self.max_cap = max(caps)
         offs, o = [], 0
         for c in caps:
             offs.append(o)
@@ -540,42 +580,15 @@ class Q8Cache:
             buffers = {name: torch.zeros(shape, dtype=t, device=self.device) for name, (shape, t) in need.items()}
             buffers["row_off"] = torch.tensor(offs, dtype=torch.int64, device=self.device) * VC_Q8_BLOCK
             buffers["cap"] = torch.tensor(caps, dtype=torch.int32, device=self.device)
-        for name, (shape, t) in need.items():
-            b = buffers[name]
-            if b.shape != shape or b.dtype is not t or b.device != self.device or not b.is_contiguous():
-                _refuse(b, name, shape, f"contiguous {t}", self._index)
-            setattr(self, name, b)
+        at = self._bind(need, buffers)
         # Attention starts on the units with the most room first.
         order = sorted(range(self.units), key=lambda u: -caps[u])
         self.order = torch.tensor(order, dtype=torch.int32, device=self.device) if len(set(caps)) > 1 else None
-        self.c = vc_q8cache(code, *[buffers[name].data_ptr() for name in _Q8_BUFFERS],
-                            0 if self.order is None else self.order.data_ptr())
-        self._ws, self._ws_of, self._kept = None, {}, []
-        self._shape_at, self._cache_at = ctypes.addressof(self.shape), ctypes.addressof(self.c)
-        self._lib = lib()
+        self.c = vc_q8cache(code, *at, 0 if self.order is None else self.order.data_ptr())
+        self._cache_at = ctypes.addressof(self.c)
 
-    def _workspace(self, n: int, max_rows: int):
-        """(address, bytes) of the workspace, grown when a call needs more than any
-        before it (a call that is captured into a graph must have run once)."""
-        ws = self._ws_of.get((n, max_rows))
-        if ws is None:
-            need = viscache_q8_attend_workspace_bytes(self.shape, n, max_rows)
-            had = 0 if self._ws is None else self._ws.numel()
-            if self._ws is None or had < need:
-                if torch.cuda.is_current_stream_capturing():
-                    raise RuntimeError("the workspace is too small: run the call once before it is captured")
-                # By half at least, so that all that are kept come to three times the largest.
-                self._ws = torch.empty((max(need, had + had // 2),), dtype=torch.uint8, device=self.device)
-                self._kept.append(self._ws)  # a graph captured before this goes on using the one it knows
-                self._ws_of.clear()
-            elif len(self._ws_of) >= 4096:  # bounds that change with every call
-                self._ws_of.clear()
-            ws = self._ws_of[n, max_rows] = self._ws.data_ptr(), self._ws.numel()
-        return ws
-
-    def _bound(self, max_rows) -> int:
-        """The row bound of a call: no unit holds more rows than it has room for."""
-        return self.max_cap if max_rows is None else min(_int32(max_rows), self.max_cap)
+    def _needs(self, n: int, max_rows: int) -> int:
+        return viscache_q8_attend_workspace_bytes(self.shape, n, max_rows)
 
     def append(self, k, v, count=None, head_major: bool = False) -> None:
         """Appends k, v bf16 [L, B, n, Hkv, d] ([L, B, Hkv, n, d] with
@@ -715,4 +728,68 @@ class Q8Cache:
                  int(fp32), scale, most, ws[0], ws[1])
 
 
-__all__ = ["PruneCall", "DecodeCache", "Q8Cache", "Rope", "NormRope", "make_params"]
+class MassCache(_Attends):
+    """A bf16 decode cache that keeps what its rows were given (viscache_mass_*) over L
+    layers x B sequences x Hkv heads: unit u = (l*B + b)*Hkv + g has room for caps[u]
+    rows, and `mass` holds for each row the attention weight it got so far.  `buffers`:
+    the cache's tensors by name (k_pool, v_pool [rows, d], mass [rows], row_off, cap,
+    len), where a program keeps them itself; row_off and cap have to hold the units'
+    first rows, one unit after the other, and caps (they are not read back to be
+    checked).
+
+    How a call's rows go to workgroups follows from the capacities, not from the
+    lengths, which only the device knows; a program that knows a bound well below the
+    capacities passes it as max_rows.
+
+    Calls go to the current stream of the cache's device.  Calls on one cache share a
+    workspace and must not overlap."""
+
+    def __init__(self, L, B, Hq, Hkv, d, caps, device, buffers=None):
+        caps = self._shaped(L, B, Hq, Hkv, d, caps, device)
+        offs, o = [], 0
+        for c in caps:
+            offs.append(o)
+            o += c
+        rows, units = max(o, 1), self.units
+        need = {"k_pool": ((rows, d), _BF16), "v_pool": ((rows, d), _BF16), "mass": ((rows,), _FP32),
+                "row_off": ((units,), torch.int64), "cap": ((units,), torch.int32), "len": ((units,), torch.int32)}
+        if buffers is None:
+            buffers = {name: torch.zeros(shape, dtype=t, device=self.device) for name, (shape, t) in need.items()}
+            buffers["row_off"] = torch.tensor(offs, dtype=torch.int64, device=self.device)
+            buffers["cap"] = torch.tensor(caps, dtype=torch.int32, device=self.device)
+        self.c = vc_mass_cache(*self._bind(need, buffers))
+        self._cache_at = ctypes.addressof(self.c)
+
+    def _needs(self, n: int, max_rows: int) -> int:
+        return viscache_mass_attend_workspace_bytes(self.shape, n, max_rows)
+
+    def attend(self, q, out, scale: float, k=None, v=None, count=None, decay: float = 1.0, max_rows=None) -> None:
+        """Attention of q bf16 [L, B, n, Hq, d] over the cache into out (bf16 or fp32,
+        the same shape), every row's mass fading by `decay` and growing by what the row
+        was given.  With k and v bf16 [L, B, n, Hkv, d] their rows are appended first (a
+        serving step); without them the cache's newest rows are the queries' own.  count
+        int32 [B]: the tokens of each sequence.  max_rows: rows past it are not attended
+        (by default, and at most, the largest capacity)."""
+        was = q.shape
+        n, index = was[2], self._index
+        want = (self.L, self.B, n, self.Hq, self.d)
+        if was != want:
+            _refuse(q, "q", want, _BF16, index)
+        fp32 = out.dtype is _FP32
+        qr, outr = _take(q, "q", None, _BF16, index), _take(out, "out", want, _FP32 if fp32 else _BF16, index)
+        if (k is None) != (v is None):
+            raise ValueError("keys without values, or values without keys")
+        kr = vr = None
+        if k is not None:
+            kv = (self.L, self.B, n, self.Hkv, self.d)
+            kr, vr = _take(k, "k", kv, _BF16, index), _take(v, "v", kv, _BF16, index)
+        cnt = _ints(count, "count", (self.B,), index)
+        if n == 0:
+            return
+        rows = self._bound(max_rows)
+        ws = self._workspace(n, rows)
+        _enqueue("viscache_mass_attend", self._lib.viscache_mass_attend, index, self._shape_at, self._cache_at, kr, vr,
+                 qr, outr, n, cnt, int(fp32), scale, decay, rows, ws[0], ws[1])
+
+
+__all__ = ["PruneCall", "DecodeCache", "Q8Cache", "Rope", "NormRope", "MassCache", "make_params"]

@@ -1,0 +1,263 @@
+"""GPU parity of attention that adds up its rows' weights (viscache_mass_attend) against 64
+bits; tolerances are derived in tests/mass_ref.py.  Rows that no unit holds are NaN."""
+import numpy as np
+import pytest
+
+from tests import mass_ref, q8_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+MARK = 77.0
+
+
+@pytest.fixture(scope="module")
+def dev():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2608_24063_amd as vc
+    vc.lib()
+    return torch.device("cuda:0")
+
+
+def _bf16(x, dev):
+    return torch.from_numpy(np.ascontiguousarray(x)).to(dev).to(torch.bfloat16)
+
+
+def _np(t):
+    return t.float().cpu().numpy().astype(np.float64)
+
+
+class Pair:
+    """A MassCache and its units in 64 bits."""
+
+    def __init__(self, seed, dev, L, B, Hq, Hkv, d, lens, caps, loud=1.0):
+        from paper_2608_24063_amd.tensors import MassCache
+        self.rng, self.dev, self.dims = np.random.default_rng(seed), dev, (L, B, Hq, Hkv, d)
+        self.c = MassCache(L, B, Hq, Hkv, d, caps, dev)
+        rows = max(sum(caps), 1)
+        K, V = np.full((rows, d), np.nan, np.float32), np.full((rows, d), np.nan, np.float32)
+        mass = np.full((rows,), MARK, np.float32)
+        self.units, self.off, o = [], [], 0
+        for n, cap in zip(lens, caps):
+            K[o:o + n] = ref.bf16(loud * self.rng.standard_normal((n, d)))
+            V[o:o + n] = ref.bf16(self.rng.standard_normal((n, d)) + 0.3)
+            mass[o:o + n] = np.exp(self.rng.standard_normal(n)).astype(np.float32)
+            self.units.append(mass_ref.Unit(K[o:o + n].copy(), V[o:o + n].copy(), mass[o:o + n].copy(), cap))
+            self.off.append(o)
+            o += cap
+        self.c.k_pool.copy_(_bf16(K, dev))
+        self.c.v_pool.copy_(_bf16(V, dev))
+        self.c.mass.copy_(torch.from_numpy(mass))
+        self.c.len.copy_(torch.tensor(lens, dtype=torch.int32))
+
+    def inputs(self, n):
+        L, B, Hq, Hkv, d = self.dims
+        r = lambda H: ref.bf16(self.rng.standard_normal((L, B, n, H, d)))  # noqa: E731
+        return r(Hq), r(Hkv), r(Hkv)
+
+    def attend(self, q, k=None, v=None, count=None, fp32=True, decay=1.0, max_rows=None, put=None, out=None):
+        """The call, and the units' own; every output, mass, row and length compared."""
+        L, B, Hq, Hkv, d = self.dims
+        n, G, scale = q.shape[2], Hq // Hkv, d ** -0.5
+        put = put or (lambda x: _bf16(x, self.dev))
+        if out is None:
+            out = torch.full((L, B, n, Hq, d), MARK, dtype=torch.float32 if fp32 else torch.bfloat16, device=self.dev)
+        cnt = None if count is None else torch.tensor(count, dtype=torch.int32, device=self.dev)
+        self.c.attend(put(q), out, scale, k=None if k is None else put(k), v=None if v is None else put(v), count=cnt,
+                      decay=decay, max_rows=max_rows)
+        torch.cuda.synchronize()
+        got = _np(out)
+        for u, unit in enumerate(self.units):
+            l, b, g = u // (B * Hkv), u // Hkv % B, u % Hkv
+            c = n if count is None else max(min(count[b], n), 0)
+            heads = slice(g * G, (g + 1) * G)
+            want, tol, size = unit.attend(q[l, b, :c, heads], scale, None if k is None else k[l, b, :, g],
+                                          None if v is None else v[l, b, :, g], decay, max_rows)
+            bad = np.abs(got[l, b, :c, heads] - want) > mass_ref.out_tol(want, tol, size, fp32, n * G > 16)
+            assert not bad.any(), (u, len(unit.K), np.argwhere(bad)[0], want[tuple(np.argwhere(bad)[0])],
+                                   got[l, b, :c, heads][tuple(np.argwhere(bad)[0])])
+            assert (got[l, b, c:, heads] == MARK).all(), u
+        self.check_cache()
+        return out
+
+    def check_cache(self):
+        K, V, mass, lens = _np(self.c.k_pool), _np(self.c.v_pool), _np(self.c.mass), self.c.len.tolist()
+        for u, (unit, o) in enumerate(zip(self.units, self.off)):
+            r = len(unit.K)
+            assert lens[u] == r, u
+            assert np.array_equal(K[o:o + r], unit.K) and np.array_equal(V[o:o + r], unit.V), u
+            assert np.isnan(K[o + r:o + unit.cap]).all() and np.isnan(V[o + r:o + unit.cap]).all(), u
+            bad = np.abs(mass[o:o + r] - unit.mass) > unit.mass_tol
+            assert not bad.any(), (u, r, np.argwhere(bad)[0], mass[o:o + r][bad][0], unit.mass[bad][0], unit.mass_tol[bad][0])
+            assert (mass[o + r:o + unit.cap] == MARK).all(), u
+
+
+SHAPES = [(2, 2, 8, 2, 64), (1, 3, 28, 4, 128), (1, 2, 16, 1, 128), (2, 1, 3, 3, 64)]
+ODD = [0, 1, 31, 32, 33, 63, 64, 65, 127, 129, 200, 511, 700]
+
+
+def _lens(rng, units, most=None):
+    lens = [int(x) for x in rng.choice(ODD, units)]
+    if most:
+        lens[int(rng.integers(0, units))] = most
+    return lens
+
+
+@pytest.mark.parametrize("L,B,Hq,Hkv,d", SHAPES)
+@pytest.mark.parametrize("n", [1, 2, 5, 17, 64, 65, 130])
+@pytest.mark.parametrize("fp32", [True, False])
+def test_calls_after_one_another(dev, L, B, Hq, Hkv, d, n, fp32):
+    """Appending calls, then one over rows that are there, with decay, counts and little room."""
+    rng = np.random.default_rng(n + d)
+    lens = _lens(rng, L * B * Hkv)
+    caps = [x + n + int(rng.integers(0, 2 * n + 3)) for x in lens]  # the second call finds little room
+    caps[0] = lens[0]
+    p = Pair(n, dev, L, B, Hq, Hkv, d, lens, caps)
+    for decay in (1.0, 0.9):
+        p.attend(*p.inputs(n), fp32=fp32, decay=decay)
+    count = [int(x) for x in rng.integers(0, n + 1, B)]
+    count[B - 1] = 0 if B > 1 else n
+    p.attend(*p.inputs(n), count=count, fp32=fp32, decay=0.0)
+    p.attend(p.inputs(n)[0], count=[x + 5 for x in count], fp32=fp32, decay=0.5)  # (clamped to n)
+    p.attend(p.inputs(n)[0], fp32=fp32)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n,Hq,Hkv", [(1, 7, 1), (1, 28, 4), (3, 8, 2), (4, 8, 1), (40, 7, 1), (300, 8, 2)])
+def test_long_units_in_pieces(dev, d, n, Hq, Hkv):
+    """Units that are cut along their rows beside short and empty ones."""
+    lens = [5000, 0, 37, 2100][:Hkv] if Hkv > 1 else [9001]
+    lens = (lens * 2)[:2 * Hkv]
+    p = Pair(7, dev, 1, 2, Hq, Hkv, d, lens, [x + 2 * n + 3 for x in lens])
+    p.attend(*p.inputs(n))
+    p.attend(*p.inputs(n), fp32=False, decay=0.75, count=[n, n // 2])
+    p.attend(p.inputs(n)[0], count=[0, 1])
+
+
+@pytest.mark.parametrize("n", [1, 2, 40])
+def test_row_bound(dev, n):
+    p = Pair(11, dev, 1, 2, 8, 2, 64, [100, 400, 64, 0], [200, 1500, 64 + n, n])
+    for most in (0, 1, 64, 101, 300):
+        p2 = Pair(11, dev, 1, 2, 8, 2, 64, [100, 400, 64, 0], [200, 1500, 64 + n, n])
+        p2.attend(*p2.inputs(n), max_rows=most)
+    p.attend(*p.inputs(n), max_rows=2 ** 40)
+
+
+@pytest.mark.parametrize("n", [1, 3, 33])
+def test_strides(dev, n):
+    """Head-major inputs and outputs, rows inside larger ones, a token stride of its own."""
+    p = Pair(13, dev, 2, 2, 8, 2, 64, [70, 5, 200, 33, 64, 1, 90, 40], [400] * 8)
+
+    def wide(x):
+        L, B, m, H, d = x.shape
+        t = torch.full((L, B, H, m, 2 * d), float("nan"), dtype=torch.bfloat16, device=dev)[..., :d].permute(0, 1, 3, 2, 4)
+        t.copy_(_bf16(x, dev))
+        return t
+    for fp32 in (True, False):
+        out = torch.full((2, 8, 2, n, 80), MARK, dtype=torch.float32 if fp32 else torch.bfloat16, device=dev)
+        view = out[..., :64].permute(0, 2, 3, 1, 4)
+        p.attend(*p.inputs(n), fp32=fp32, put=wide, out=view, count=[n, max(n - 1, 0)])
+        assert (out[..., 64:] == MARK).all()
+
+
+@pytest.mark.parametrize("n", [2, 4, 20, 70])
+@pytest.mark.parametrize("long", [False, True])
+def test_rows_without_finite_values(dev, n, long):
+    """An infinity or a NaN in a row reaches the queries that see the row, and no others."""
+    lens = [3000, 4001] if long else [50, 64]
+    lens[1] += 60 - n % 7
+    make = lambda: Pair(17, dev, 1, 1, 8, 2, 64, lens, [x + n for x in lens])  # noqa: E731
+    for fp32 in (True, False):
+        clean, p = make(), make()
+        q, k, v = clean.inputs(n)
+        want = clean.attend(q, k, v, fp32=fp32)
+        r = n // 2
+        v = v.copy()
+        v[0, 0, r, 0, 3], v[0, 0, r, 1, 9], v[0, 0, n - 1, 1, 3] = np.inf, np.nan, -np.inf
+        out = torch.zeros_like(want)
+        p.c.attend(_bf16(q, dev), out, 64 ** -0.5, k=_bf16(k, dev), v=_bf16(v, dev))
+        bad = torch.isfinite(out).logical_not()
+        expect = torch.zeros_like(bad)
+        expect[0, 0, r:, :4, 3] = True
+        expect[0, 0, r:, 4:, 9] = True
+        expect[0, 0, n - 1, 4:, 3] = True
+        assert torch.equal(bad, expect)
+        assert torch.equal(out[~bad], want[~bad])
+        assert torch.equal(p.c.mass, clean.c.mass)  # weights are the keys' affair
+        # a key that later queries see, and a query
+        p, k2, q2 = make(), k.copy(), q.copy()
+        k2[0, 0, r, 0, 5] = np.nan
+        q2[0, 0, 0, 7, 0] = np.nan
+        p.c.attend(_bf16(q2, dev), out, 64 ** -0.5, k=_bf16(k2, dev), v=_bf16(clean.inputs(n)[2] * 0 + 1, dev))
+        nan = torch.isnan(out).any(dim=-1)
+        expect = torch.zeros_like(nan)
+        expect[0, 0, r:, :4] = True
+        expect[0, 0, 0, 7] = True
+        assert torch.equal(nan, expect)
+        m = torch.isnan(p.c.mass)
+        a, b = lens[0], lens[0] + n  # rows of unit 0; unit 1's rows that query 0 sees
+        assert m[:a + n].all() and m[b:b + lens[1] + 1].all() and not m[b + lens[1] + 1:].any()
+
+
+def test_masses_of_many_calls(dev):
+    """Sixty steps of one token: the masses of a whole answer, every row and query counted once."""
+    p = Pair(19, dev, 1, 2, 8, 2, 128, [40, 300, 0, 7], [400] * 4)
+    before = [u.mass.sum() for u in p.units]
+    for i in range(60):
+        p.attend(*p.inputs(1))
+    for u, b in zip(p.units, before):
+        assert abs(u.mass.sum() - b - 60 * 4) < 1e-6  # every query's weights sum to one
+
+
+@pytest.mark.parametrize("n", [1, 30])
+def test_streams_and_graphs(dev, n):
+    """A step captured once and replayed gives the eager steps' bits; another stream too."""
+    make = lambda: Pair(23, dev, 2, 2, 8, 2, 64, [300, 20, 2000, 64, 0, 1, 500, 90], [2600] * 8)  # noqa: E731
+    a, b = make(), make()
+    ins = [a.inputs(n) for _ in range(4)]
+    q, k, v = (_bf16(x, dev) for x in ins[0])
+    outs = [torch.zeros(q.shape, device=dev) for _ in range(2)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    b.c.attend(q, outs[1], 0.125, k=k, v=v)  # grows the workspace
+    a.c.attend(q, outs[0], 0.125, k=k, v=v)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        b.c.attend(q, outs[1], 0.125, k=k, v=v, decay=0.5)
+    for x in ins[1:]:
+        for t, y in zip((q, k, v), x):
+            t.copy_(_bf16(y, dev))
+        graph.replay()
+        with torch.cuda.stream(side):
+            side.wait_stream(torch.cuda.current_stream())
+            a.c.attend(q, outs[0], 0.125, k=k, v=v, decay=0.5)
+        torch.cuda.synchronize()
+        assert torch.equal(*outs) and torch.equal(a.c.mass, b.c.mass) and torch.equal(a.c.len, b.c.len)
+        assert torch.equal(a.c.k_pool.view(torch.int16), b.c.k_pool.view(torch.int16))
+        assert torch.equal(a.c.v_pool.view(torch.int16), b.c.v_pool.view(torch.int16))
+
+
+def test_refusals(dev):
+    p = Pair(29, dev, 1, 2, 8, 2, 64, [10] * 4, [20] * 4)
+    c, (q, k, v) = p.c, (_bf16(x, dev) for x in p.inputs(3))
+    out = torch.zeros(q.shape, device=dev)
+    cnt = torch.ones((2,), dtype=torch.int32, device=dev)
+    for f in (lambda: c.attend(q[:, :1], out, 0.1), lambda: c.attend(q.float(), out, 0.1),
+              lambda: c.attend(q, out[:, :, :2], 0.1), lambda: c.attend(q, out.half(), 0.1),
+              lambda: c.attend(q, out, 0.1, k=k), lambda: c.attend(q, out, 0.1, v=v),
+              lambda: c.attend(q, out, 0.1, k=k[:, :, :2], v=v), lambda: c.attend(q, out, 0.1, k=k, v=v.float()),
+              lambda: c.attend(q, out, 0.1, count=cnt.long()), lambda: c.attend(q, out, 0.1, count=cnt[:1]),
+              lambda: c.attend(q.cpu(), out, 0.1), lambda: c.attend(q, out.transpose(3, 4), 0.1)):
+        with pytest.raises(ValueError):
+            f()
+    from paper_2608_24063_amd import VisCacheError
+    for kw in (dict(scale=0.0), dict(scale=float("nan")), dict(scale=0.1, decay=-1.0), dict(scale=0.1, decay=float("inf")),
+               dict(scale=0.1, max_rows=-1)):
+        with pytest.raises(VisCacheError):
+            c.attend(q, out, **kw)
+    c.attend(q[:, :, :0], out[:, :, :0], 0.1, k=k[:, :, :0], v=v[:, :, :0])
+    p.check_cache()
+    assert not out.any()
