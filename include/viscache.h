@@ -684,6 +684,29 @@ vc_status viscache_mass_attend(const vc_decode_shape *shape, const vc_mass_cache
                                const int32_t *count, int32_t out_fp32, float scale, float decay, int32_t max_rows,
                                void *workspace, size_t workspace_bytes, void *stream);
 
+/* Host only.  Workspace bytes viscache_mass_evict needs for caches of at most max_rows
+ * rows; 0 where it refuses them. */
+size_t viscache_mass_evict_workspace_bytes(const vc_decode_shape *shape, int32_t max_rows);
+
+/* Device, asynchronous.  Eviction by mass: unit u of n = min(len, max_rows) rows keeps k =
+ * min(keep[u], n) of them (keep: DEVICE int32 [L*B*Hkv]; less than 0 counts as 0), the
+ * first a = min(sinks, k), the last z = min(recent, k - a), and of the others the k - a -
+ * z of the largest mass, ties to the lower index, NaN after all numbers.  Kept rows stay
+ * in order and move together with their masses, to rows 0 .. k - 1 of the same unit (to
+ * NULL: in place) or of another cache of the same shape, whose cap bounds k and whose
+ * pools must not overlap; len (of `to`, where there is one) becomes k, and a source
+ * that is not moved within is left as it was.  Rows and masses behind the k are left as
+ * they were, except that in place they may be any of the unit's old ones.  index: DEVICE
+ * int32 [L*B*Hkv][index_rows], or NULL with index_rows 0: entry j < min(k, index_rows) of
+ * a unit is the row that became row j; the others are left as they were.  Shape as for
+ * attention (Hq is checked, not used).  max_rows bounds every len (rows past it are
+ * evicted).  Two launches.  `workspace` as for viscache_mass_attend.  VC_ERR_ARG also
+ * for a `to` that shares its pools, masses or lengths with the cache; VC_ERR_UNSUPPORTED
+ * for 2^22 or more units or 2^23 or more chunks of 16 KB of keys. */
+vc_status viscache_mass_evict(const vc_decode_shape *shape, const vc_mass_cache *cache, const vc_mass_cache *to,
+                              const int32_t *keep, int32_t sinks, int32_t recent, int32_t max_rows, int32_t *index,
+                              int32_t index_rows, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Static text for a status code. */
 const char *viscache_strerror(vc_status s);
 

@@ -145,6 +145,9 @@ def lib() -> ctypes.CDLL:
         L.viscache_mass_attend_workspace_bytes.restype = ctypes.c_size_t
         L.viscache_mass_attend.argtypes = [c_vp] * 6 + [c_i32, c_vp, c_i32, c_f32, c_f32, c_i32, c_vp, ctypes.c_size_t,
                                                         c_vp]
+        L.viscache_mass_evict_workspace_bytes.argtypes = [c_vp, c_i32]
+        L.viscache_mass_evict_workspace_bytes.restype = ctypes.c_size_t
+        L.viscache_mass_evict.argtypes = [c_vp] * 4 + [c_i32] * 3 + [c_vp, c_i32, c_vp, ctypes.c_size_t, c_vp]
         L.viscache_strerror.argtypes = [c_i32]
         L.viscache_strerror.restype = ctypes.c_char_p
         for name in ("viscache_budget", "viscache_out_rows", "viscache_prune", "viscache_prune_score_offsets",
@@ -153,7 +156,8 @@ def lib() -> ctypes.CDLL:
                      "viscache_decode_step_q4", "viscache_decode_step_noalloc", "viscache_decode_plan",
                      "viscache_decode_step_planned", "viscache_quantize_rows", "viscache_q8_append",
                      "viscache_q8_read", "viscache_q8_attend", "viscache_q8_step", "viscache_rope",
-                     "viscache_norm_rope", "viscache_norm_rope_grad", "viscache_mass_attend"):
+                     "viscache_norm_rope", "viscache_norm_rope_grad", "viscache_mass_attend",
+                     "viscache_mass_evict"):
             getattr(L, name).restype = c_i32
         _lib = L
     return _lib
@@ -440,6 +444,19 @@ def viscache_mass_attend(shape: vc_decode_shape, cache: vc_mass_cache, k, v, q: 
     _check(st, "viscache_mass_attend")
 
 
+def viscache_mass_evict_workspace_bytes(shape: vc_decode_shape, max_rows: int) -> int:
+    return int(lib().viscache_mass_evict_workspace_bytes(_ref(shape), _int32(max_rows)))
+
+
+def viscache_mass_evict(shape: vc_decode_shape, cache: vc_mass_cache, to, keep: int, sinks: int, recent: int,
+                        max_rows: int, index: int, index_rows: int, workspace: int, workspace_bytes: int,
+                        stream: int) -> None:
+    """to: vc_mass_cache, or None for in place."""
+    st = lib().viscache_mass_evict(_ref(shape), _ref(cache), _ref(to), keep, _int32(sinks), _int32(recent),
+                                   _int32(max_rows), index, _int32(index_rows), workspace, workspace_bytes, stream)
+    _check(st, "viscache_mass_evict")
+
+
 def viscache_strerror(status: int) -> str:
     return strerror(status)
 
@@ -453,4 +470,5 @@ EXPORTED = ("viscache_default_params", "viscache_budget", "viscache_out_rows",
             "viscache_quantize_rows", "viscache_q8_append", "viscache_q8_read",
             "viscache_q8_attend_workspace_bytes", "viscache_q8_attend", "viscache_rope", "viscache_q8_step",
             "viscache_norm_rope", "viscache_norm_rope_grad_workspace_bytes", "viscache_norm_rope_grad",
-            "viscache_mass_attend_workspace_bytes", "viscache_mass_attend", "viscache_strerror")
+            "viscache_mass_attend_workspace_bytes", "viscache_mass_attend",
+            "viscache_mass_evict_workspace_bytes", "viscache_mass_evict", "viscache_strerror")

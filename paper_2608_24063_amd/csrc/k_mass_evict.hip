@@ -1,0 +1,215 @@
+// k_mass_evict.hip -- eviction by mass: unit u keeps k = keep[u] of its n rows, the first
+// `sinks`, the last `recent` and of the others those of the largest mass (ties to the
+// lower index, NaN behind every number), in order, in place or into another cache.
+//
+// k_choose, a workgroup a unit, finds the threshold exactly: a most-significant-digit radix
+// select over the masses' bits (digits of 11, 11 and 10 bits, counted in LDS), then one
+// pass that gives every kept row its place by ballots and prefix sums.  A chain of LDS
+// round trips bounds it.  k_move copies the rows, a workgroup 16 KB of keys and 16 of
+// values, and is bound by memory.
+//
+// In place a row's new place may hold a row that has yet to move.  Rows only move down and
+// keep their order, so the rows of a chunk of new places come from that chunk or later
+// ones, and what a chunk writes over is read by itself and by earlier chunks of its unit
+// alone.  So a workgroup reads its rows into registers, says so, waits until all earlier
+// chunks of the unit have said so, and writes.  Chunks are handed out by a counter: a
+// workgroup that waits was handed a later chunk than those it waits for, which were
+// handed to workgroups that run already and say so without waiting for anything.
+#include <algorithm>
+
+#include "vc_mass_device.h"
+
+namespace vc {
+
+namespace {
+
+// A mass as a key that orders like it: NaN lowest, -0 as 0.
+__device__ __forceinline__ uint32_t key_of(float m) {
+  if (m != m) return 0u;
+  const uint32_t x = __float_as_uint(m + 0.f);
+  return (x & 0x80000000u) ? ~x : x | 0x80000000u;
+}
+
+template <int NT>
+__global__ __launch_bounds__(NT) void k_choose(EvictPlan p) {
+  constexpr int kWaves = NT / 64, kBins = 2048;
+  __shared__ __attribute__((aligned(16))) uint32_t hist[kBins];
+  __shared__ uint32_t found[2], tot[2][kWaves][2];
+  const int u = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int len_ = ldg(p.c.len + u), cap_ = ldg(p.c.cap + u), keep_ = ldg(p.keep + u);
+  const int room = p.inplace ? INT32_MAX : ldg(p.to.cap + u);
+  const float *mass = p.c.mass + ldg(p.c.row_off + u);
+  const int n = max(min(min(len_, cap_), p.max_rows), 0);
+  const int k = max(min(min(keep_, n), room), 0);
+  const int a = min(p.sinks, k), z = min(p.recent, k - a), mid = n - z;  // rows a .. mid - 1 compete
+  uint32_t T = 0u, left = (uint32_t)(k - a - z);  // the threshold; rows wanted among those equal to it
+  if (left == 0u) T = ~0u;  // above every key
+  // For the launch after this one: nobody has read a row, no chunk is handed out.
+  if (p.inplace) {
+    for (int i = tid; i < p.chunks; i += NT) stg(p.flags + (int64_t)u * p.chunks + i, 0u);
+    if (u == 0 && tid == 0) stg(p.ticket, 0u);
+  }
+  if (left > 0u && left < (uint32_t)(mid - a)) {  // uniform
+#pragma unroll 1
+    for (int pass = 0; pass < 3; ++pass) {
+      const int sh = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+      const uint32_t bins = pass == 2 ? 1024u : 2048u, known = pass == 0 ? 0u : ~0u << (pass == 1 ? 21 : 10);
+      for (int i = 4 * tid; i < kBins; i += 4 * NT) *reinterpret_cast<u32x4 *>(hist + i) = u32x4{0u, 0u, 0u, 0u};
+      __syncthreads();
+      for (int t = a + tid; t < mid; t += NT) {
+        const uint32_t x = key_of(ldg(mass + t));
+        if ((x & known) == T) atomicAdd(&hist[x >> sh & (bins - 1u)], 1u);
+      }
+      __syncthreads();
+      if (w == 0) {  // the bin that holds rank `left` from the top: lane l sums bins of 32 in descending order
+        uint32_t sum = 0u;
+        for (int i = 0; i < kBins / 64; i += 4) {
+          const u32x4 h = *reinterpret_cast<const u32x4 *>(hist + kBins - kBins / 64 * (lane + 1) + i);
+          sum += (h.x + h.y) + (h.z + h.w);
+        }
+        const uint32_t incl = wave_incl_scan(sum);
+        const int src = __builtin_ctzll(__builtin_amdgcn_ballot_w64(incl - sum < left && left <= incl));
+        const uint32_t before = (uint32_t)__builtin_amdgcn_readlane((int)(incl - sum), src);
+        const int bin = kBins - 1 - kBins / 64 * src - lane;
+        const uint32_t h = lane < kBins / 64 ? hist[max(bin, 0)] : 0u;
+        const uint32_t in2 = wave_incl_scan(h) + before;
+        const uint64_t hit = __builtin_amdgcn_ballot_w64(in2 - h < left && left <= in2);
+        if (lane == __builtin_ctzll(hit)) {
+          found[0] = (uint32_t)bin;
+          found[1] = left - (in2 - h);
+        }
+      }
+      __syncthreads();
+      T |= found[0] << sh;
+      left = found[1];
+    }
+  }
+  // Every kept row's place.  A wave takes 256 rows of a tile, by four ballots of 64.
+  int32_t *list = p.list + (int64_t)u * p.ldl;
+  int32_t *index = p.index ? p.index + (int64_t)u * p.index_rows : nullptr;
+  uint32_t kept = 0u, equal = 0u;  // before the tile
+  for (int t0 = 0, it = 0; t0 < n; t0 += 4 * NT, it ^= 1) {
+    uint64_t sure[4], tie[4];
+    uint32_t ns = 0u, ne = 0u;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int t = t0 + 256 * w + 64 * j + lane;
+      const uint32_t x = key_of(ldg(mass + min(t, n - 1)));
+      const bool in = t >= a && t < mid;
+      sure[j] = __builtin_amdgcn_ballot_w64(t < n && (!in || x > T));
+      tie[j] = __builtin_amdgcn_ballot_w64(in && x == T);
+      ns += (uint32_t)__builtin_popcountll(sure[j]);
+      ne += (uint32_t)__builtin_popcountll(tie[j]);
+    }
+    if (lane == 0) tot[it][w][0] = ns, tot[it][w][1] = ne;
+    __syncthreads();
+    uint32_t bs = kept, be = equal;
+#pragma unroll
+    for (int y = 0; y < kWaves; ++y) {
+      const uint32_t s = tot[it][y][0], e = tot[it][y][1];
+      if (y < w) bs += s, be += e;
+      kept += s, equal += e;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint64_t below = ((uint64_t)1 << lane) - 1;
+      const uint32_t s = bs + (uint32_t)__builtin_popcountll(sure[j] & below);
+      const uint32_t e = be + (uint32_t)__builtin_popcountll(tie[j] & below);
+      const bool is = sure[j] >> lane & 1, ie = (tie[j] >> lane & 1) && e < left;
+      const uint32_t at = s + min(e, left);
+      if ((is || ie) && at < (uint32_t)k) {
+        const int t = t0 + 256 * w + 64 * j + lane;
+        stg(list + at, t);
+        if (index && at < (uint32_t)p.index_rows) stg(index + at, t);
+      }
+      bs += (uint32_t)__builtin_popcountll(sure[j]);
+      be += (uint32_t)__builtin_popcountll(tie[j]);
+    }
+  }
+  if (tid == 0) {
+    stg(p.count + u, k);
+    stg((p.inplace ? p.c.len : p.to.len) + u, k);
+  }
+}
+
+template <int D, bool INPLACE>
+__global__ __launch_bounds__(256) void k_move(EvictPlan p) {
+  constexpr int CPR = D / 8, R = kEvictBytes / (2 * D), IT = R * CPR / 256;  // rows of a chunk
+  __shared__ uint32_t mine;
+  __shared__ int32_t from[R];
+  const int tid = threadIdx.x;
+  uint32_t id = blockIdx.x;
+  if (INPLACE) {
+    if (tid == 0) mine = __hip_atomic_fetch_add(p.ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    id = mine;
+  }
+  const int u = (int)(id / (uint32_t)p.chunks), c = (int)(id % (uint32_t)p.chunks);
+  if (u >= p.units) return;
+  const int k = ldg(p.count + u), j0 = c * R;
+  if (j0 >= k) return;  // (nobody waits for it: waiting chunks come before it)
+  const int nr = min(R, k - j0);
+  const int64_t src = ldg(p.c.row_off + u), dst = INPLACE ? src : ldg(p.to.row_off + u);
+  for (int i = tid; i < R; i += 256) from[i] = ldg(p.list + (int64_t)u * p.ldl + j0 + min(i, nr - 1));
+  __syncthreads();
+  u32x4 kr[IT], vr[IT];
+  float m = 0.f;
+#pragma unroll
+  for (int it = 0; it < IT; ++it) {
+    const int e = tid + 256 * it;
+    const int64_t at = (src + from[e / CPR]) * D + 8 * (e % CPR);
+    kr[it] = ld16_stream(p.c.kp + at);
+    vr[it] = ld16_stream(p.c.vp + at);
+  }
+  if (tid < nr) m = ldg(p.c.mass + src + from[tid]);
+  if (INPLACE) {
+    // The rows are in registers before the barrier: what uses them here waits for them.
+#pragma unroll
+    for (int it = 0; it < IT; ++it) asm volatile("" : "+v"(kr[it]), "+v"(vr[it]) : : "memory");
+    asm volatile("" : "+v"(m) : : "memory");
+    __syncthreads();
+    uint32_t *flag = p.flags + (int64_t)u * p.chunks;
+    if (tid == 0) __hip_atomic_store(flag + c, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for (int i = tid; i < c; i += 256)
+      while (__hip_atomic_load(flag + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == 0u) __builtin_amdgcn_s_sleep(1);
+    __syncthreads();
+  }
+  const MassPool &to = INPLACE ? p.c : p.to;
+#pragma unroll
+  for (int it = 0; it < IT; ++it) {
+    const int e = tid + 256 * it, i = e / CPR;
+    if (i >= nr || (INPLACE && from[i] == j0 + i)) continue;
+    const int64_t at = (dst + j0 + i) * D + 8 * (e % CPR);
+    st16_stream(to.kp + at, kr[it]);
+    st16_stream(to.vp + at, vr[it]);
+  }
+  if (tid < nr) stg(to.mass + dst + j0 + tid, m);
+}
+
+template <int D>
+void launch_move(const EvictPlan &p, hipStream_t st) {
+  const dim3 grid((uint32_t)(p.units * p.chunks));
+  if (p.inplace)
+    hipLaunchKernelGGL((k_move<D, true>), grid, dim3(256), 0, st, p);
+  else
+    hipLaunchKernelGGL((k_move<D, false>), grid, dim3(256), 0, st, p);
+}
+
+}  // namespace
+
+hipError_t launch_mass_evict(const EvictPlan &p, hipStream_t st) {
+  if (p.max_rows <= 2048)
+    hipLaunchKernelGGL((k_choose<256>), dim3((uint32_t)p.units), dim3(256), 0, st, p);
+  else
+    hipLaunchKernelGGL((k_choose<1024>), dim3((uint32_t)p.units), dim3(1024), 0, st, p);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.chunks == 0) return e;
+  if (p.d == 128)
+    launch_move<128>(p, st);
+  else
+    launch_move<64>(p, st);
+  return hipGetLastError();
+}
+
+}  // namespace vc

@@ -8,6 +8,7 @@ namespace vc {
 constexpr int kMassTile = 32;         // rows of a single token's tile
 constexpr int kMassChunk = 1024;      // rows of a workgroup of k_finish
 constexpr int kMassKeys = 256;        // rows of a workgroup of k_mass_cols
+constexpr int kEvictBytes = 16384;    // keys (and as many values) of a workgroup of k_move
 constexpr int kMassMaxRows = INT32_MAX - 1024;  // so that the end of a row's tile is a row index
 
 // The cache, as in vc_mass_cache.
@@ -45,10 +46,25 @@ struct MassAttn {
   int32_t *np;            // prompts: first part and number of parts of each tile
 };
 
+struct EvictPlan {
+  MassPool c, to;  // to: not read in place
+  const int32_t *keep;
+  int32_t units, d, inplace, sinks, recent, max_rows;
+  int32_t chunks;    // workgroups of a unit's move
+  int32_t ldl;       // rows of a unit's list
+  int32_t *list;     // [unit][ldl] kept rows, ascending
+  int32_t *count;    // [unit] how many
+  uint32_t *flags;   // [unit][chunks]: the chunk's rows are read (in place)
+  uint32_t *ticket;  // chunks handed out (in place)
+  int32_t *index;    // the caller's: [unit][index_rows], or null
+  int32_t index_rows;
+};
+
 // launch_mass_token: attention (and append) in one launch, or two where units are cut.
 // launch_mass_prompt: append, attention, join where tiles are cut, and the rows' weights.
 hipError_t launch_mass_token(const MassAttn &p, hipStream_t st);
 hipError_t launch_mass_prompt(const MassAttn &p, hipStream_t st);
 hipError_t launch_mass_cols(const MassAttn &p, hipStream_t st);  // called by launch_mass_prompt
+hipError_t launch_mass_evict(const EvictPlan &p, hipStream_t st);
 
 }  // namespace vc

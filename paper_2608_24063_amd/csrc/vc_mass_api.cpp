@@ -82,6 +82,25 @@ bool attend_cut(const vc_decode_shape *s, int32_t n, int32_t max_rows, Cut &c) {
   return true;
 }
 
+// The parts of an eviction's workspace.
+struct EvictCut {
+  int32_t chunks = 0, ldl = 0;
+  size_t count = 0, flags = 0, ticket = 0, total = 0;
+};
+
+bool evict_cut(const vc_decode_shape *s, int32_t max_rows, EvictCut &c) {
+  max_rows = std::min(max_rows, kMassMaxRows);
+  const int64_t units = (int64_t)s->L * s->B * s->Hkv, rows = kEvictBytes / (2 * s->d);
+  c.chunks = (int32_t)((max_rows + rows - 1) / rows);
+  if (units * c.chunks >= kMaxWg || units >= kMaxWg / 2) return false;  // (1024 threads a unit)
+  c.ldl = (int32_t)(c.chunks * rows);
+  c.count = align_up(sizeof(int32_t) * (size_t)units * (size_t)c.ldl);
+  c.flags = c.count + align_up(sizeof(int32_t) * (size_t)units);
+  c.ticket = c.flags + align_up(sizeof(uint32_t) * (size_t)units * (size_t)c.chunks);
+  c.total = c.ticket + kAlign;
+  return true;
+}
+
 }  // namespace
 
 extern "C" {
@@ -145,6 +164,51 @@ vc_status viscache_mass_attend(const vc_decode_shape *s, const vc_mass_cache *c,
   hipStream_t hs = static_cast<hipStream_t>(stream);
   const hipError_t e = p.cols <= kTokenCols ? launch_mass_token(p, hs) : launch_mass_prompt(p, hs);
   return e == hipSuccess ? VC_OK : VC_ERR_HIP;
+}
+
+size_t viscache_mass_evict_workspace_bytes(const vc_decode_shape *s, int32_t max_rows) {
+  if (check_shape(s) != VC_OK || max_rows < 0) return 0;
+  EvictCut c;
+  return evict_cut(s, max_rows, c) ? c.total : 0;
+}
+
+vc_status viscache_mass_evict(const vc_decode_shape *s, const vc_mass_cache *c, const vc_mass_cache *to,
+                              const int32_t *keep, int32_t sinks, int32_t recent, int32_t max_rows, int32_t *index,
+                              int32_t index_rows, void *workspace, size_t workspace_bytes, void *stream) {
+  vc_status st = check_shape(s);
+  if (st != VC_OK) return st;
+  if ((st = check_cache(c)) != VC_OK) return st;
+  if (to) {
+    if ((st = check_cache(to)) != VC_OK) return st;
+    if (to->k_pool == c->k_pool || to->v_pool == c->v_pool || to->mass == c->mass || to->len == c->len)
+      return VC_ERR_ARG;
+  }
+  if (!keep || sinks < 0 || recent < 0 || max_rows < 0 || index_rows < 0 || (index_rows > 0 && !index))
+    return VC_ERR_ARG;
+  EvictCut cut;
+  if (!evict_cut(s, max_rows, cut)) return VC_ERR_UNSUPPORTED;
+  if (!workspace || workspace_bytes < cut.total || reinterpret_cast<uintptr_t>(workspace) % kAlign != 0)
+    return VC_ERR_WORKSPACE;
+  EvictPlan p{};
+  p.c = bind(c);
+  if (to) p.to = bind(to);
+  p.keep = keep;
+  p.units = s->L * s->B * s->Hkv;
+  p.d = s->d;
+  p.inplace = to == nullptr;
+  p.sinks = sinks;
+  p.recent = recent;
+  p.max_rows = std::min(max_rows, kMassMaxRows);
+  p.chunks = cut.chunks;
+  p.ldl = cut.ldl;
+  uint8_t *ws = static_cast<uint8_t *>(workspace);
+  p.list = reinterpret_cast<int32_t *>(ws);
+  p.count = reinterpret_cast<int32_t *>(ws + cut.count);
+  p.flags = reinterpret_cast<uint32_t *>(ws + cut.flags);
+  p.ticket = reinterpret_cast<uint32_t *>(ws + cut.ticket);
+  p.index = index_rows > 0 ? index : nullptr;
+  p.index_rows = index_rows;
+  return launch_mass_evict(p, static_cast<hipStream_t>(stream)) == hipSuccess ? VC_OK : VC_ERR_HIP;
 }
 
 }  // extern "C"

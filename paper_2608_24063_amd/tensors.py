@@ -13,7 +13,8 @@ from . import (VC_ERR_WORKSPACE, VC_PRUNE_EVENTS, VC_Q8_BLOCK, VisCacheError, _i
                viscache_decode_plan, viscache_decode_step, viscache_decode_step_noalloc,
                viscache_decode_step_planned, viscache_decode_step_q4,
                viscache_decode_step_workspace_bytes,
-               viscache_decode_workspace_bytes, viscache_mass_attend_workspace_bytes, viscache_out_rows, viscache_prune_workspace_bytes,
+               viscache_decode_workspace_bytes, viscache_mass_attend_workspace_bytes,
+               viscache_mass_evict_workspace_bytes, viscache_out_rows, viscache_prune_workspace_bytes,
                viscache_q8_append, viscache_q8_attend_workspace_bytes, viscache_quantize_rows)
 
 
@@ -260,11 +261,11 @@ def _take(t: torch.Tensor, name: str, shape, typ, index: int, head_major: bool =
 
 
 def _ints(t, name: str, shape, index: int) -> int:
-    """Address of a contiguous int32 tensor (0 for None)."""
+    """Address of a contiguous int32 tensor of this shape, unless that is known (0 for None)."""
     if t is None:
         return 0
-    if t.shape != shape or t.dtype is not torch.int32 or t.get_device() != index or not t.is_contiguous():
-        _refuse(t, name, shape, "contiguous int32", index)
+    if (shape is not None and t.shape != shape) or t.dtype is not torch.int32 or t.get_device() != index or not t.is_contiguous():
+        _refuse(t, name, t.shape if shape is None else shape, "contiguous int32", index)
     return t.data_ptr()
 
 
@@ -761,6 +762,9 @@ class MassCache(_Attends):
         self._cache_at = ctypes.addressof(self.c)
 
     def _needs(self, n: int, max_rows: int) -> int:
+        """Of n queries, or (-1) of an eviction."""
+        if n < 0:
+            return viscache_mass_evict_workspace_bytes(self.shape, max_rows)
         return viscache_mass_attend_workspace_bytes(self.shape, n, max_rows)
 
     def attend(self, q, out, scale: float, k=None, v=None, count=None, decay: float = 1.0, max_rows=None) -> None:
@@ -790,6 +794,28 @@ class MassCache(_Attends):
         ws = self._workspace(n, rows)
         _enqueue("viscache_mass_attend", self._lib.viscache_mass_attend, index, self._shape_at, self._cache_at, kr, vr,
                  qr, outr, n, cnt, int(fp32), scale, decay, rows, ws[0], ws[1])
+
+    def evict(self, keep, sinks: int = 0, recent: int = 0, to: "MassCache | None" = None, index=None,
+              max_rows=None) -> None:
+        """Every unit keeps keep[u] (int32 [units]) of its rows: the first `sinks`, the
+        last `recent` and of the others those of the largest mass (ties to the lower
+        index), in order, with their masses; in place, or into `to`, a cache of the
+        same shape with rows of its own, which bounds keep by its capacities and leaves
+        this one as it was.  index int32 [units, rows]: where the kept rows came from
+        (entries past them are left as they were).  max_rows: rows past it are evicted
+        (by default, and at most, the largest capacity)."""
+        at, idx = _ints(keep, "keep", (self.units,), self._index), _ints(index, "index", None, self._index)
+        if keep is None:
+            raise ValueError("keep: the rows that each unit keeps")
+        if index is not None and (index.dim() != 2 or index.shape[0] != self.units):
+            _refuse(index, "index", (self.units, "rows"), "contiguous int32", self._index)
+        if to is not None and (to.L, to.B, to.Hkv, to.d, to.device) != (self.L, self.B, self.Hkv, self.d, self.device):
+            raise ValueError("the other cache has another shape or device")
+        wide = 0 if index is None else index.shape[1]
+        rows = self._bound(max_rows)
+        ws = self._workspace(-1, rows)
+        _enqueue("viscache_mass_evict", self._lib.viscache_mass_evict, self._index, self._shape_at, self._cache_at,
+                 None if to is None else to._cache_at, at, _int32(sinks), _int32(recent), rows, idx, wide, ws[0], ws[1])
 
 
 __all__ = ["PruneCall", "DecodeCache", "Q8Cache", "Rope", "NormRope", "MassCache", "make_params"]
