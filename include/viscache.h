@@ -644,6 +644,11 @@ typedef struct {
   const int64_t *row_off;  /* as in vc_cache: unit u owns rows [row_off, row_off + cap) and holds len */
   const int32_t *cap;
   int32_t *len;            /* (lengths past 2^31 - 1025 count as that) */
+  const int32_t *order;    /* [L*B*Hkv] or NULL: the units in the order in which attention of n * Hq/Hkv
+                              <= 16 starts on them (longest first evens out units of different
+                              lengths).  No unit may appear twice; one that it leaves out (entries
+                              outside [0, L*B*Hkv) are passed over) is left alone by such calls.
+                              More columns and eviction take all units and do not read it. */
 } vc_mass_cache;
 
 /* Host only.  Workspace bytes viscache_mass_attend needs for n queries a sequence over

@@ -76,7 +76,8 @@ class vc_norm(ctypes.Structure):
 
 
 class vc_mass_cache(ctypes.Structure):
-    _fields_ = [("k_pool", c_vp), ("v_pool", c_vp), ("mass", c_vp), ("row_off", c_vp), ("cap", c_vp), ("len", c_vp)]
+    _fields_ = [("k_pool", c_vp), ("v_pool", c_vp), ("mass", c_vp), ("row_off", c_vp), ("cap", c_vp), ("len", c_vp),
+                ("order", c_vp)]
 
 
 class VisCacheError(RuntimeError):

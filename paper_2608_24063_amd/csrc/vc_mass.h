@@ -6,6 +6,8 @@
 namespace vc {
 
 constexpr int kMassTile = 32;         // rows of a single token's tile
+constexpr int kMassHeld4 = 10112;     // logits that a workgroup of four waves keeps in LDS
+constexpr int kMassHeld8 = 30720;     // one of eight
 constexpr int kMassChunk = 1024;      // rows of a workgroup of k_finish
 constexpr int kMassKeys = 256;        // rows of a workgroup of k_mass_cols
 constexpr int kEvictBytes = 16384;    // keys (and as many values) of a workgroup of k_move
@@ -30,9 +32,12 @@ struct MassAttn {
   int32_t append, fp32, causal;  // causal: always 1
   int32_t max_rows;
   float sc, decay;        // sc = scale * log2(e)
-  // Single tokens (cols <= 16): pieces of `piece` tiles, at most npmax a unit; the
-  // logits of every column and row wait in [unit][cols][ldr] for its maximum and sum.
-  int32_t piece, npmax, ldr;
+  // Single tokens (cols <= 16): workgroups of `waves` waves take the units in `order`
+  // (null: as they are), in pieces of `piece` tiles, at most npmax a unit.  The logits of
+  // every column wait for its maximum and sum: of a unit in one piece those of rows below
+  // `here` in LDS, all others in [unit][cols][ldr], from row `here` on.
+  const int32_t *order;
+  int32_t waves, piece, npmax, here, ldr;
   float *logits;
   // Prompts (npmax 1): nqt column tiles of qcols columns, each in as many key splits
   // as the launch's workgroups allow (ns 1: whole).

@@ -31,7 +31,7 @@ MassPool bind(const vc_mass_cache *c) {
 
 // How an attention call is cut, and the parts of its workspace.
 struct Cut {
-  int32_t piece = 0, npmax = 1, ldr = 0, qcols = 0, nqt = 0, ns = 1;
+  int32_t waves = 0, piece = 0, npmax = 1, here = 0, ldr = 0, qcols = 0, nqt = 0, ns = 1;
   int64_t wgs = 0, slots = 0;  // workgroups; columns of partial results
   size_t ml = 0, stat = 0, state = 0, np = 0, logits = 0, total = 0;
 };
@@ -43,15 +43,32 @@ bool attend_cut(const vc_decode_shape *s, int32_t n, int32_t max_rows, Cut &c) {
   if (cols > (int64_t(1) << 24)) return false;
   if (cols <= kTokenCols) {
     const int64_t nt = std::max<int64_t>(1, ((int64_t)max_rows + kMassTile - 1) / kMassTile);
-    // Pieces of a multiple of four tiles (one per wave and turn).
-    const int64_t want = units * nt / 512;
+    // Units are cut into pieces of a multiple of four tiles (one per wave and turn), as
+    // many as make about 256 workgroups, one a CU, but no more than 24 a unit, which the
+    // second launch has to join; not where the rows that a piece saves cost less than
+    // that launch, nor where the units fill the chip by themselves.  A CU reads 51 GB/s, however
+    // many its waves.  (us, 7 columns and 128 channels, in pieces of 4, 8, 16, 32 tiles and
+    // whole: 4 units of 1000 rows 11.3 12.7 14.7 15.9 15.9, of 4000 13.2 12.1 13.5 17.8 45,
+    // of 12000 21.7 15.7 15.6 19.1 124; 32 of 1000 11.4 12.7 14.8 16.0 16.2, of 4000 25.7
+    // 20.8 19.4 20.3 46.5; 64 of 1000 15.4 14.2 16.3 16.8 17.2, of 4000 39.8 31.3 28.8 28.6
+    // 47.0; 112 of 1000 24.3 21.1 19.7 17.8 18.1, of 2000 37.1 30.8 27.6 26.9 28.5, of 12000
+    // 217 188 179 175 199.  A unit of 400 rows takes 10.7 whole.)
+    const auto fours = [](int64_t x) { return (x + 3) / 4 * 4; };
     c.qcols = kTokenCols;
-    c.piece = (int32_t)std::max<int64_t>(8, (want + 3) / 4 * 4);
-    if (nt <= std::max<int64_t>(2 * (int64_t)c.piece, 16)) c.piece = (int32_t)nt;
+    c.piece = (int32_t)std::max<int64_t>({4, fours((units * nt + 255) / 256), fours((nt + 23) / 24)});
+    if (nt <= 12 || units > 128 || (units > 96 && nt <= 48)) c.piece = (int32_t)nt;
     c.npmax = (int32_t)((nt + c.piece - 1) / c.piece);
     c.wgs = units * c.npmax;
     c.slots = c.npmax > 1 ? c.wgs * kTokenCols : 0;
-    c.ldr = (int32_t)(nt * kMassTile);
+    // Eight waves where four would leave more than a third of a whole unit's logits to the
+    // workspace.  (us, four and eight waves: 896 units of 200 rows and 7 columns 23.2 36.4,
+    // of 1000 74 87, of 1500 110 120; 640 of 1000 rows and 8 columns 46 55, of 3000 175 157;
+    // 320 of 3000 104 87; 2000 of 2500 rows, 4 columns and 64 channels 208 215.)
+    const int64_t pitch = cols | 1;
+    c.waves = c.npmax == 1 && nt * kMassTile * pitch > kMassHeld4 * 3 / 2 ? 8 : 4;
+    const int64_t room = (c.waves == 8 ? kMassHeld8 : kMassHeld4) / pitch / kMassTile * kMassTile;
+    c.here = (int32_t)(c.npmax > 1 ? 0 : std::min(room, nt * kMassTile));
+    c.ldr = (int32_t)(nt * kMassTile - c.here);
     // The second launch's workgroups.
     if (c.npmax > 1 && units * (((int64_t)max_rows + kMassChunk - 1) / kMassChunk) >= kMaxWg) return false;
   } else {
@@ -152,7 +169,8 @@ vc_status viscache_mass_attend(const vc_decode_shape *s, const vc_mass_cache *c,
   p.max_rows = std::min(max_rows, kMassMaxRows);
   p.sc = scale * 1.4426950408889634f;
   p.decay = decay;
-  p.piece = cut.piece; p.npmax = cut.npmax; p.ldr = cut.ldr;
+  p.order = c->order;
+  p.waves = cut.waves; p.piece = cut.piece; p.npmax = cut.npmax; p.here = cut.here; p.ldr = cut.ldr;
   p.qcols = cut.qcols; p.nqt = cut.nqt; p.ns = cut.ns;
   uint8_t *ws = static_cast<uint8_t *>(workspace);
   p.part_o = reinterpret_cast<float *>(ws);

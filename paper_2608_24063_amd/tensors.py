@@ -738,9 +738,9 @@ class MassCache(_Attends):
     first rows, one unit after the other, and caps (they are not read back to be
     checked).
 
-    How a call's rows go to workgroups follows from the capacities, not from the
-    lengths, which only the device knows; a program that knows a bound well below the
-    capacities passes it as max_rows.
+    How a call's rows go to workgroups, and which units single tokens start with, follow
+    from the capacities, not from the lengths, which only the device knows; a program
+    that knows a bound well below the capacities passes it as max_rows.
 
     Calls go to the current stream of the cache's device.  Calls on one cache share a
     workspace and must not overlap."""
@@ -758,7 +758,11 @@ class MassCache(_Attends):
             buffers = {name: torch.zeros(shape, dtype=t, device=self.device) for name, (shape, t) in need.items()}
             buffers["row_off"] = torch.tensor(offs, dtype=torch.int64, device=self.device)
             buffers["cap"] = torch.tensor(caps, dtype=torch.int32, device=self.device)
-        self.c = vc_mass_cache(*self._bind(need, buffers))
+        at = self._bind(need, buffers)
+        # Attention of single tokens starts on the units with the most room first.
+        order = sorted(range(units), key=lambda u: -caps[u])
+        self.order = torch.tensor(order, dtype=torch.int32, device=self.device) if len(set(caps)) > 1 else None
+        self.c = vc_mass_cache(*at, 0 if self.order is None else self.order.data_ptr())
         self._cache_at = ctypes.addressof(self.c)
 
     def _needs(self, n: int, max_rows: int) -> int:
