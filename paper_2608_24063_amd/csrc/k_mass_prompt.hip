@@ -183,9 +183,24 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt(MassAttn p) {
         for (int y = 0; y < NP; ++y) O[cb] = mfma32(a, as_bf16x8(P[y][s]), O[cb]);
       }
   };
+  // The matrix part of block i: the block before it into O, and its logits; the operands'
+  // reads (two a product of V, one of K) run kAhead products ahead.
   auto products = [&](int i) {
     outputs(tv[(i & 1) ^ 1]);
     logits(tk[i & 1]);
+    if (!F32) {
+      constexpr int kPV = 4 * CB, kAll = 2 * KS + kPV, kAhead = 4;
+      __builtin_amdgcn_sched_group_barrier(0x100, 2 * kAhead, 0);
+#pragma unroll
+      for (int k = 0; k < kAll - kAhead; ++k) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        if (k + kAhead < kPV)
+          __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        else
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x8, kAhead, 0);
+    }
   };
   // The weights of block t0 + i from its logits.
   auto weights = [&](int i) {

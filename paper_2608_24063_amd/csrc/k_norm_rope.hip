@@ -15,20 +15,6 @@ namespace vc {
 
 namespace {
 
-// x over the lane (lane & ~(PER - 1)) .. + PER - 1, in each of them.
-template <int PER>
-__device__ __forceinline__ float sum_lanes(float x) {
-  const auto dpp = [&](auto c) {
-    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), decltype(c)::value, 0xF,
-                                                                 0xF, false));
-  };
-  x += dpp(std::integral_constant<int, 0xB1>{});                  // lane ^ 1
-  x += dpp(std::integral_constant<int, 0x4E>{});                  // lane ^ 2
-  if (PER >= 8) x += dpp(std::integral_constant<int, 0x141>{});   // mirrored in 8: the other quad
-  if (PER >= 16) x += dpp(std::integral_constant<int, 0x140>{});  // mirrored in 16: the other 8
-  return x;
-}
-
 // A lane's place in the rows: chunks at elements o1 and o2, frequencies N c ...
 template <bool F32, bool ADJ, int D>
 struct Place {

@@ -31,9 +31,9 @@ MassPool bind(const vc_mass_cache *c) {
 
 // How an attention call is cut, and the parts of its workspace.
 struct Cut {
-  int32_t waves = 0, piece = 0, npmax = 1, here = 0, ldr = 0, qcols = 0, nqt = 0, ns = 1;
+  int32_t waves = 0, piece = 0, npmax = 1, here = 0, ldr = 0, qcols = 0, nqt = 0, ns = 1, keys = 0, ktiles = 1, csplit = 1;
   int64_t wgs = 0, slots = 0;  // workgroups; columns of partial results
-  size_t ml = 0, stat = 0, state = 0, np = 0, logits = 0, total = 0;
+  size_t ml = 0, stat = 0, state = 0, np = 0, logits = 0, mass = 0, total = 0;
 };
 
 bool attend_cut(const vc_decode_shape *s, int32_t n, int32_t max_rows, Cut &c) {
@@ -84,9 +84,17 @@ bool attend_cut(const vc_decode_shape *s, int32_t n, int32_t max_rows, Cut &c) {
     c.wgs = c.ns > 1 ? std::min(resident, tiles * (nt / kQ8SplitBlocks)) : tiles;
     c.slots = c.ns > 1 ? c.wgs * c.qcols : 0;
     // The other launches' workgroups: the append's, the join's, the masses'.
+    c.keys = 256;
+    c.ktiles = (int32_t)std::max<int64_t>(1, ((int64_t)max_rows + c.keys - 1) / c.keys);
+    const int64_t key_tiles = units * c.ktiles;
     if (units * (((int64_t)n + kQ8Block - 1) / kQ8Block) >= kMaxWg || (c.slots && units * cols >= 2 * kMaxWg) ||
-        units * (((int64_t)max_rows + kMassKeys - 1) / kMassKeys) >= kMaxWg)
+        key_tiles >= kMaxWg)
       return false;
+    // Columns of a row tile's masses are split where tiles are few against the 256
+    // workgroups that the card holds, eight blocks of columns at least together.
+    const int64_t blocks = (cols + 63) / 64;
+    c.csplit = (int32_t)std::max<int64_t>(1, std::min<int64_t>(blocks / 8, (2048 + key_tiles - 1) / key_tiles));
+    if (key_tiles * c.csplit >= kMaxWg) c.csplit = 1;
   }
   if (c.wgs >= kMaxWg) return false;
   const bool token = cols <= kTokenCols;
@@ -95,7 +103,10 @@ bool attend_cut(const vc_decode_shape *s, int32_t n, int32_t max_rows, Cut &c) {
   c.state = c.stat + (token ? 0 : align_up(sizeof(float2) * (size_t)(units * cols)));
   c.np = c.state + align_up(sizeof(int4) * (size_t)units);
   c.logits = c.np + (token || c.ns == 1 ? 0 : align_up(sizeof(int32_t) * 2 * (size_t)(units * c.nqt)));
-  c.total = c.logits + (token ? align_up(sizeof(float) * (size_t)(units * cols) * (size_t)c.ldr) : 0);
+  c.mass = c.logits + (token ? align_up(sizeof(float) * (size_t)(units * cols) * (size_t)c.ldr) : 0);
+  c.total = c.mass;
+  if (c.csplit > 1)
+    c.total += align_up(sizeof(float) * (size_t)units * (size_t)c.ktiles * (size_t)c.csplit * (size_t)c.keys);
   return true;
 }
 
@@ -179,6 +190,8 @@ vc_status viscache_mass_attend(const vc_decode_shape *s, const vc_mass_cache *c,
   p.state = reinterpret_cast<int4 *>(ws + cut.state);
   p.np = reinterpret_cast<int32_t *>(ws + cut.np);
   p.logits = reinterpret_cast<float *>(ws + cut.logits);
+  p.keys = cut.keys; p.ktiles = cut.ktiles; p.csplit = cut.csplit;
+  p.part_mass = reinterpret_cast<float *>(ws + cut.mass);
   hipStream_t hs = static_cast<hipStream_t>(stream);
   const hipError_t e = p.cols <= kTokenCols ? launch_mass_token(p, hs) : launch_mass_prompt(p, hs);
   return e == hipSuccess ? VC_OK : VC_ERR_HIP;

@@ -2,6 +2,8 @@
 // and their values as fp32 and fp16 (int8 and e4m3 codes are exact in both).
 // Internal to libviscache.
 #pragma once
+#include <type_traits>
+
 #include "vc_device.h"
 #include "vc_q8.h"
 
@@ -261,6 +263,20 @@ __device__ __forceinline__ int64_t unit_base(const RowsDesc &r, const int64_t *u
   if (unit_off) return ldg(unit_off + u);
   const int g = u % Hkv, lb = u / Hkv;
   return (int64_t)(lb / B) * r.layer + (int64_t)(lb % B) * r.seq + (int64_t)g * r.head;
+}
+
+// x over the lanes (lane & ~(PER - 1)) .. + PER - 1 (PER 4, 8 or 16), in each of them.
+template <int PER>
+__device__ __forceinline__ float sum_lanes(float x) {
+  const auto dpp = [&](auto c) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), decltype(c)::value, 0xF,
+                                                                 0xF, false));
+  };
+  x += dpp(std::integral_constant<int, 0xB1>{});                  // lane ^ 1
+  x += dpp(std::integral_constant<int, 0x4E>{});                  // lane ^ 2
+  if (PER >= 8) x += dpp(std::integral_constant<int, 0x141>{});   // mirrored in 8: the other quad
+  if (PER >= 16) x += dpp(std::integral_constant<int, 0x140>{});  // mirrored in 16: the other 8
+  return x;
 }
 
 // Sum over a wave.
