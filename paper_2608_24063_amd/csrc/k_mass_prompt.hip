@@ -38,24 +38,23 @@ __device__ __forceinline__ MassUnit unit_now(const MassAttn &p, int u) {
   return MassUnit{ldg(p.c.row_off + u), (int)s.x, (int)s.y, (int)s.x, (int)s.z};
 }
 
-// Workgroup (unit, 64 new rows): keys and values into the pools, masses of zero.  The
-// length itself follows in the last launch, since every workgroup here reads it.
+// Workgroup (unit, 256 chunks of 16 bytes of its new rows): keys and values into the pools,
+// masses of zero.  The length itself follows in the last launch, since every workgroup
+// here reads it.
 __global__ __launch_bounds__(256) void k_append_mass(MassAttn p) {
   const int u = (int)(blockIdx.x % (uint32_t)p.units), j = (int)(blockIdx.x / (uint32_t)p.units);
   const int tid = threadIdx.x, cpr = p.d / 8;
   const MassUnit x = mass_unit(p, u);
+  const int i = j * (256 / cpr) + tid / cpr, c = tid % cpr;
+  const uint16_t *kn = new_rows(p, p.k, u), *vn = new_rows(p, p.v, u);
   if (j == 0 && tid == 0)
     st16(p.state + u, u32x4{(uint32_t)x.len0, (uint32_t)x.held, (uint32_t)x.cnt, 0u});
-  const int n = min(x.held - x.len0, (j + 1) * kBlock);
-  const uint16_t *kn = new_rows(p, p.k, u), *vn = new_rows(p, p.v, u);
-  for (int e = j * kBlock * cpr + tid; e < n * cpr; e += 256) {
-    const int i = e / cpr, c = e % cpr;
-    const int64_t row = x.off + x.len0 + i, to = row * p.d + 8 * c;
-    const u32x4 a = ld16(kn + i * p.k.token + 8 * c), b = ld16(vn + i * p.v.token + 8 * c);
-    st16(p.c.kp + to, a);
-    st16(p.c.vp + to, b);
-    if (c == 0) stg(p.c.mass + row, 0.f);
-  }
+  if (i >= x.held - x.len0) return;
+  const int64_t row = x.off + x.len0 + i, to = row * p.d + 8 * c;
+  const u32x4 a = ld16(kn + i * p.k.token + 8 * c), b = ld16(vn + i * p.v.token + 8 * c);
+  st16(p.c.kp + to, a);
+  st16(p.c.vp + to, b);
+  if (c == 0) stg(p.c.mass + row, 0.f);
 }
 
 // Pitches: 16-byte reads of 32 rows, and transposing reads of 4 rows x 64 bytes, without conflicts.
@@ -86,10 +85,17 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt(MassAttn p) {
   __shared__ int32_t bad[D];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int ln = lane & 31, hf = lane >> 5;
-  const Share sh = share_of(p, blockIdx.x, lane, [&](int u) {
-    const MassUnit x = unit_now(p, u);
-    return Held{x.held, x.cnt, x.off};
-  });
+  Share sh;
+  if (p.append)  // (two copies, so that no load in them is under a condition)
+    sh = share_of(p, blockIdx.x, lane, [&](int u) {
+      const u32x4 s = ld16(p.state + u);
+      return Held{(int)s.y, (int)s.z, ldg(p.c.row_off + u)};
+    });
+  else
+    sh = share_of(p, blockIdx.x, lane, [&](int u) {
+      const MassUnit x = mass_unit(p, u);
+      return Held{x.held, x.cnt, x.off};
+    });
   const int u = sh.u, qt = sh.qt, sp = sh.sp, ns = sh.ns;
   if (u < 0) return;
   const int cols = sh.cnt * p.G, c0 = qt * p.qcols;
@@ -106,9 +112,16 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt(MassAttn p) {
   const bool live = c0 + 32 * w <= cl;  // the wave has columns (the others only stage)
   for (int c = tid; c < D; c += NT) bad[c] = INT32_MAX;
 
-  const uint16_t *kp = p.c.kp + sh.off * D, *vp = p.c.vp + sh.off * D;
+  const uint16_t *kp = uniform(p.c.kp + sh.off * D), *vp = uniform(p.c.vp + sh.off * D);
   u32x4 rk[IT], rv[IT];
+  const int whole = uniform(most / kBlock);
   auto fetch = [&](const uint16_t *from, int t, u32x4 (&r)[IT]) {
+    if (t < whole) {  // uniform
+      const uint16_t *src = from + (int64_t)t * (kBlock * D);
+#pragma unroll
+      for (int it = 0; it < IT; ++it) r[it] = ld16(src + 8 * (tid + NT * it));
+      return;
+    }
 #pragma unroll
     for (int it = 0; it < IT; ++it) {
       const int e = tid + NT * it, row = min(t * kBlock + e / CPR, most - 1);
@@ -203,6 +216,8 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt(MassAttn p) {
     }
   };
   // The weights of block t0 + i from its logits.
+  float inf = __builtin_inff();
+  asm("" : "+s"(inf));  // (else the compiler makes med3 a maximum of quieted inputs)
   auto weights = [&](int i) {
     const int t = t0 + i;
     if ((t + 1) * kBlock > wmin) {  // wave-uniform
@@ -217,7 +232,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt(MassAttn p) {
     // (med3 with infinity is a maximum that needs no quieted inputs.)
     float x[16];
 #pragma unroll
-    for (int k = 0; k < 16; ++k) x[k] = __builtin_amdgcn_fmed3f(S[0][k], S[1][k], __builtin_inff());
+    for (int k = 0; k < 16; ++k) x[k] = __builtin_amdgcn_fmed3f(S[0][k], S[1][k], inf);
     float mx = fmaxf(x[0], x[1]);
 #pragma unroll
     for (int k = 2; k < 16; ++k) mx = fmaxf(mx, x[k]);
@@ -349,7 +364,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt(MassAttn p) {
 // A column's parts, four channels a thread: the output and the column's maximum and sum.
 template <int D>
 __global__ __launch_bounds__(256) void k_join_mass(MassAttn p) {
-  constexpr int TPC = D / 4, CPW = 256 / TPC, U = 4;  // threads a column, columns a workgroup
+  constexpr int TPC = D / 4, CPW = 256 / TPC, U = 8;  // threads a column, columns a workgroup, parts in flight
   const int tid = threadIdx.x, ch = tid % TPC * 4;
   const int64_t cg = (int64_t)blockIdx.x * CPW + tid / TPC;
   if (cg >= (int64_t)p.units * p.cols) return;
@@ -413,7 +428,7 @@ template <int D>
 hipError_t launch(const MassAttn &p, hipStream_t st) {
   hipError_t e;
   if (p.append) {
-    const int64_t nj = ((int64_t)p.n + kBlock - 1) / kBlock;
+    const int64_t rows = 2048 / D, nj = (p.n + rows - 1) / rows;
     hipLaunchKernelGGL(k_append_mass, dim3((uint32_t)(p.units * nj)), dim3(256), 0, st, p);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }

@@ -87,7 +87,7 @@ bool attend_cut(const vc_decode_shape *s, int32_t n, int32_t max_rows, Cut &c) {
     c.keys = 256;
     c.ktiles = (int32_t)std::max<int64_t>(1, ((int64_t)max_rows + c.keys - 1) / c.keys);
     const int64_t key_tiles = units * c.ktiles;
-    if (units * (((int64_t)n + kQ8Block - 1) / kQ8Block) >= kMaxWg || (c.slots && units * cols >= 2 * kMaxWg) ||
+    if (units * (((int64_t)n * s->d + 2047) / 2048) >= kMaxWg || (c.slots && units * cols >= 2 * kMaxWg) ||
         key_tiles >= kMaxWg)
       return false;
     // Columns of a row tile's masses are split where tiles are few against the 256
