@@ -12,9 +12,11 @@
 // keep their order, so the rows of a chunk of new places come from that chunk or later
 // ones, and what a chunk writes over is read by itself and by earlier chunks of its unit
 // alone.  So a workgroup reads its rows into registers, says so, waits until all earlier
-// chunks of the unit have said so, and writes.  Chunks are handed out by a counter: a
-// workgroup that waits was handed a later chunk than those it waits for, which were
-// handed to workgroups that run already and say so without waiting for anything.
+// chunks of the unit have said so, and writes.  A unit's chunks are handed out by a counter
+// of its own: a workgroup that waits was handed a later chunk than those it waits for,
+// which were handed to workgroups that run already and say so without waiting for
+// anything.  (One counter for all units takes 14 ns a workgroup, which follow one another:
+// 83 us against 45 for 112 units of 2400 to 3136 rows cut to 1880 on average.)
 #include <algorithm>
 
 #include "vc_mass_device.h"
@@ -22,6 +24,8 @@
 namespace vc {
 
 namespace {
+
+constexpr int kMoveThreads = 512;
 
 // A mass as a key that orders like it: NaN lowest, -0 as 0.
 __device__ __forceinline__ uint32_t key_of(float m) {
@@ -48,7 +52,7 @@ __global__ __launch_bounds__(NT) void k_choose(EvictPlan p) {
   // For the launch after this one: nobody has read a row, no chunk is handed out.
   if (p.inplace) {
     for (int i = tid; i < p.chunks; i += NT) stg(p.flags + (int64_t)u * p.chunks + i, 0u);
-    if (u == 0 && tid == 0) stg(p.ticket, 0u);
+    if (tid == 0) stg(p.ticket + u, 0u);
   }
   if (left > 0u && left < (uint32_t)(mid - a)) {  // uniform
 #pragma unroll 1
@@ -134,30 +138,31 @@ __global__ __launch_bounds__(NT) void k_choose(EvictPlan p) {
 }
 
 template <int D, bool INPLACE>
-__global__ __launch_bounds__(256) void k_move(EvictPlan p) {
-  constexpr int CPR = D / 8, R = kEvictBytes / (2 * D), IT = R * CPR / 256;  // rows of a chunk
+__global__ __launch_bounds__(kMoveThreads) void k_move(EvictPlan p) {
+  constexpr int CPR = D / 8, R = kEvictBytes / (2 * D), IT = R * CPR / kMoveThreads;  // rows of a chunk
   __shared__ uint32_t mine;
   __shared__ int32_t from[R];
   const int tid = threadIdx.x;
-  uint32_t id = blockIdx.x;
+  const int u = (int)(blockIdx.x / (uint32_t)p.chunks);
+  int c = (int)(blockIdx.x % (uint32_t)p.chunks);
+  const int k = ldg(p.count + u);
   if (INPLACE) {
-    if (tid == 0) mine = __hip_atomic_fetch_add(p.ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (c * R >= k) return;  // as many stay as there are chunks
+    if (tid == 0) mine = __hip_atomic_fetch_add(p.ticket + u, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
-    id = mine;
+    c = (int)mine;
   }
-  const int u = (int)(id / (uint32_t)p.chunks), c = (int)(id % (uint32_t)p.chunks);
-  if (u >= p.units) return;
-  const int k = ldg(p.count + u), j0 = c * R;
-  if (j0 >= k) return;  // (nobody waits for it: waiting chunks come before it)
+  const int j0 = c * R;
+  if (j0 >= k) return;
   const int nr = min(R, k - j0);
   const int64_t src = ldg(p.c.row_off + u), dst = INPLACE ? src : ldg(p.to.row_off + u);
-  for (int i = tid; i < R; i += 256) from[i] = ldg(p.list + (int64_t)u * p.ldl + j0 + min(i, nr - 1));
+  for (int i = tid; i < R; i += kMoveThreads) from[i] = ldg(p.list + (int64_t)u * p.ldl + j0 + min(i, nr - 1));
   __syncthreads();
   u32x4 kr[IT], vr[IT];
   float m = 0.f;
 #pragma unroll
   for (int it = 0; it < IT; ++it) {
-    const int e = tid + 256 * it;
+    const int e = tid + kMoveThreads * it;
     const int64_t at = (src + from[e / CPR]) * D + 8 * (e % CPR);
     kr[it] = ld16_stream(p.c.kp + at);
     vr[it] = ld16_stream(p.c.vp + at);
@@ -171,14 +176,14 @@ __global__ __launch_bounds__(256) void k_move(EvictPlan p) {
     __syncthreads();
     uint32_t *flag = p.flags + (int64_t)u * p.chunks;
     if (tid == 0) __hip_atomic_store(flag + c, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    for (int i = tid; i < c; i += 256)
+    for (int i = tid; i < c; i += kMoveThreads)
       while (__hip_atomic_load(flag + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == 0u) __builtin_amdgcn_s_sleep(1);
     __syncthreads();
   }
   const MassPool &to = INPLACE ? p.c : p.to;
 #pragma unroll
   for (int it = 0; it < IT; ++it) {
-    const int e = tid + 256 * it, i = e / CPR;
+    const int e = tid + kMoveThreads * it, i = e / CPR;
     if (i >= nr || (INPLACE && from[i] == j0 + i)) continue;
     const int64_t at = (dst + j0 + i) * D + 8 * (e % CPR);
     st16_stream(to.kp + at, kr[it]);
@@ -191,9 +196,9 @@ template <int D>
 void launch_move(const EvictPlan &p, hipStream_t st) {
   const dim3 grid((uint32_t)(p.units * p.chunks));
   if (p.inplace)
-    hipLaunchKernelGGL((k_move<D, true>), grid, dim3(256), 0, st, p);
+    hipLaunchKernelGGL((k_move<D, true>), grid, dim3(kMoveThreads), 0, st, p);
   else
-    hipLaunchKernelGGL((k_move<D, false>), grid, dim3(256), 0, st, p);
+    hipLaunchKernelGGL((k_move<D, false>), grid, dim3(kMoveThreads), 0, st, p);
 }
 
 }  // namespace

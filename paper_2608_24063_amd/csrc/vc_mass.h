@@ -9,7 +9,7 @@ constexpr int kMassTile = 32;         // rows of a single token's tile
 constexpr int kMassHeld4 = 10112;     // logits that a workgroup of four waves keeps in LDS
 constexpr int kMassHeld8 = 30720;     // one of eight
 constexpr int kMassChunk = 1024;      // rows of a workgroup of k_finish
-constexpr int kEvictBytes = 16384;    // keys (and as many values) of a workgroup of k_move
+constexpr int kEvictBytes = 32768;    // keys (and as many values) of a workgroup of k_move
 constexpr int kMassMaxRows = INT32_MAX - 1024;  // so that the end of a row's tile is a row index
 
 // The cache, as in vc_mass_cache.
@@ -63,7 +63,7 @@ struct EvictPlan {
   int32_t *list;     // [unit][ldl] kept rows, ascending
   int32_t *count;    // [unit] how many
   uint32_t *flags;   // [unit][chunks]: the chunk's rows are read (in place)
-  uint32_t *ticket;  // chunks handed out (in place)
+  uint32_t *ticket;  // [unit]: chunks handed out (in place)
   int32_t *index;    // the caller's: [unit][index_rows], or null
   int32_t index_rows;
 };

@@ -125,7 +125,7 @@ bool evict_cut(const vc_decode_shape *s, int32_t max_rows, EvictCut &c) {
   c.count = align_up(sizeof(int32_t) * (size_t)units * (size_t)c.ldl);
   c.flags = c.count + align_up(sizeof(int32_t) * (size_t)units);
   c.ticket = c.flags + align_up(sizeof(uint32_t) * (size_t)units * (size_t)c.chunks);
-  c.total = c.ticket + kAlign;
+  c.total = c.ticket + align_up(sizeof(uint32_t) * (size_t)units);
   return true;
 }
 
