@@ -7,7 +7,10 @@
 // the means are exact products.
 //
 // Bound by memory: every value is read and written once, streamed.  A row lies over d /
-// (2N) lanes (N values in 16 bytes), which exchange its sums by DPP.
+// (2N) lanes (N values in 16 bytes), which exchange its sums by DPP.  A wave's first rows
+// are requested before the weights and the positions that it turns them by.  12608
+// tokens of 28 + 4 bf16 heads, 128 channels: 39 us (5.2 TB/s); the gradient over 16382
+// tokens of 64 + 8: 176 to 187 us (4.8 to 5.1 TB/s), 5 of them the sum of the weights'.
 #include "vc_norm.h"
 #include "vc_q8_device.h"
 
@@ -112,35 +115,46 @@ __global__ __launch_bounds__(256) void k_norm_rope(NormPlan p) {
   const int64_t g0 = bid % groups * TPW;
   const int half = p.t.rot / 2;
   const Pl pl(lane, p.t.rot);
-  float wq[2 * N], wk[2 * N];
-  pl.weights(p.qw, l, p.w_fp32, wq);
-  pl.weights(p.kw, l, p.w_fp32, wk);
-  for (int e = tid; e < TPW * kRopeMaxHalf; e += 256) {
-    const int t = e / kRopeMaxHalf, i = e % kRopeMaxHalf;
-    const int64_t g = g0 + t;
-    if (i < half && g < toks) cs[t][i] = turn_of(p.t, i, ldg(p.pos + axis_of(p.t, i) * toks + g));
-  }
-  __syncthreads();
   const int t = w / kWaves, sub = w % kWaves;
-  const int64_t g = g0 + t;
-  if (g >= toks) return;
-  const int b = (int)(g / p.n), i = (int)(g % p.n);
-  if (p.count && i >= ldg(p.count + b)) return;
-  float2 w2[N];
-#pragma unroll
-  for (int k = 0; k < N; ++k) w2[k] = pl.rotated ? cs[t][N * pl.c + k] : make_float2(1.f, 0.f);
+  const int64_t g = g0 + t, gc = g < toks ? g : toks - 1;
+  const int b = (int)(gc / p.n), i = (int)(gc % p.n);
   const int H = p.Hq + p.Hkv;
   constexpr int64_t E = F32 ? 4 : 2;
   auto row0 = [&](const RowsDesc &r) { return r.base + E * (l * r.layer + b * r.seq + i * r.token); };
   const uint64_t qi = row0(p.qi), qo = row0(p.qo), ki = row0(p.ki), ko = row0(p.ko);
   const int64_t qih = E * p.qi.head, qoh = E * p.qo.head, kih = E * p.ki.head, koh = E * p.ko.head;
-  for (int h = sub * HS + lane / Pl::PER; h < H; h += kWaves * HS) {
+  u32x4 x0, x1;
+  auto request = [&](int h) {
     const bool isq = h < p.Hq;
     const int hh = isq ? h : h - p.Hq;
     const char *src = reinterpret_cast<const char *>((isq ? qi : ki) + hh * (isq ? qih : kih));
+    x0 = ld16_stream(src + E * pl.o1);
+    x1 = ld16_stream(src + E * pl.o2);
+  };
+  // The first rows' requests, the weights' and the positions', before anything waits.
+  const int h0 = sub * HS + lane / Pl::PER;
+  request(min(h0, H - 1));
+  float wq[2 * N], wk[2 * N];
+  pl.weights(p.qw, l, p.w_fp32, wq);
+  pl.weights(p.kw, l, p.w_fp32, wk);
+  for (int e = tid; e < TPW * kRopeMaxHalf; e += 256) {
+    const int tt = e / kRopeMaxHalf, f = e % kRopeMaxHalf;
+    const int64_t gg = g0 + tt;
+    if (f < half && gg < toks) cs[tt][f] = turn_of(p.t, f, ldg(p.pos + axis_of(p.t, f) * toks + gg));
+  }
+  __syncthreads();
+  if (g >= toks) return;
+  if (p.count && i >= ldg(p.count + b)) return;
+  float2 w2[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) w2[k] = pl.rotated ? cs[t][N * pl.c + k] : make_float2(1.f, 0.f);
+  for (int h = h0; h < H; h += kWaves * HS) {
+    const bool isq = h < p.Hq;
+    const int hh = isq ? h : h - p.Hq;
     char *dst = reinterpret_cast<char *>((isq ? qo : ko) + hh * (isq ? qoh : koh));
     float x[2 * N];
-    Pl::unpack(ld16_stream(src + E * pl.o1), ld16_stream(src + E * pl.o2), x);
+    Pl::unpack(x0, x1, x);
+    request(min(h + kWaves * HS, H - 1));  // the next rows', which no output overlaps
     const float r = inv_rms<D>(Pl::squares(x), p.eps);
 #pragma unroll
     for (int k = 0; k < 2 * N; ++k) x[k] = x[k] * r * (isq ? wq[k] : wk[k]);
@@ -260,8 +274,14 @@ hipError_t launch(const NormPlan &p, bool grad, hipStream_t st) {
     hipLaunchKernelGGL((k_dweight<D>), dim3((uint32_t)(p.L * 2 * (D / 16))), dim3(1024), 0, st, p);
     return hipGetLastError();
   }
-  // Tokens of a workgroup as for the rotation alone (launch_rope).
-  if (p.Hq + p.Hkv <= 2 * Place<F32, ADJ, D>::HS && toks * p.L >= 2048)
+  // Four tokens a workgroup, a wave each, where a wave then has few passes over a token's
+  // heads and the tokens fill the chip; else a token a workgroup.  (us, one token and four:
+  // bf16, 128 channels, 10 heads, 1024, 2048, 32000 tokens 4.8 4.5, 7.6 5.4, 87 41; 32 heads
+  // (4 passes) 5.9 6.9, 9.8 9.3, 114 90; 72 heads (9) 9.3 11.4, 15.9 16.1, 193 199.  bf16, 64
+  // channels, 72 heads (5) 6.9 7.7, 12.2 11.0, 140 116.  fp32, 128 channels, 10 heads (3) 4.8
+  // 4.6, 6.9 5.6, 69 55, 32 heads (8) 172 189; 64 channels, 32 heads (4) 8.6 8.4, 85 91.)
+  constexpr int HS = Place<F32, ADJ, D>::HS;
+  if ((p.Hq + p.Hkv + HS - 1) / HS <= (F32 ? 3 : 5) && toks * p.L >= 2048)
     hipLaunchKernelGGL((k_norm_rope<F32, ADJ, D, 4>), dim3((uint32_t)((toks + 3) / 4 * p.L)), dim3(256), 0, st, p);
   else
     hipLaunchKernelGGL((k_norm_rope<F32, ADJ, D, 1>), dim3((uint32_t)(toks * p.L)), dim3(256), 0, st, p);
