@@ -15,8 +15,8 @@ namespace vc {
 
 namespace {
 
-
 constexpr int kCols = 64;  // columns of a block
+constexpr int NW = kMassKeys / 64, NT = kMassKeys;  // waves and threads of a workgroup
 
 template <int D>
 struct Smem {
@@ -24,9 +24,9 @@ struct Smem {
   float2 stat[2][kCols];
 };
 
-template <int D, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void k_mass_cols(MassAttn p) {
-  constexpr int NT = 64 * NW, KS = D / 16, CPR = D / 8, IT = kCols * CPR / NT, CS = NT / CPR;
+template <int D>
+__global__ __launch_bounds__(NT, 2) void k_mass_cols(MassAttn p) {
+  constexpr int KS = D / 16, CPR = D / 8, IT = kCols * CPR / NT, CS = NT / CPR;
   __shared__ Smem<D> sm;
   __shared__ float red[NW][64][2];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -210,10 +210,9 @@ __global__ __launch_bounds__(64 * NW, 2) void k_mass_cols(MassAttn p) {
 }
 
 // The masses of a tile from its splits, in their order.
-__global__ __launch_bounds__(256) void k_mass_sum(MassAttn p) {
-  const uint32_t tiles = gridDim.x / (uint32_t)p.units;  // of 256 rows
-  const int u = (int)(blockIdx.x / tiles);
-  const int row = (int)(blockIdx.x % tiles) * 256 + threadIdx.x;
+__global__ __launch_bounds__(kMassKeys) void k_mass_sum(MassAttn p) {
+  const int u = (int)(blockIdx.x / (uint32_t)p.ktiles);
+  const int row = (int)(blockIdx.x % (uint32_t)p.ktiles) * kMassKeys + threadIdx.x;
   MassUnit x;
   if (p.append) {  // (the launch before it has set the length)
     const u32x4 s = ld16(p.state + u);
@@ -224,21 +223,16 @@ __global__ __launch_bounds__(256) void k_mass_sum(MassAttn p) {
   if (x.cnt == 0 || row >= min(x.held, p.max_rows)) return;
   float *to = p.c.mass + x.off + row;
   const float was = ldg(to);
-  const int64_t ut = (int64_t)u * p.ktiles + row / p.keys;
-  const float *from = p.part_mass + ut * p.csplit * p.keys + row % p.keys;
+  const float *from = p.part_mass + (int64_t)blockIdx.x * p.csplit * kMassKeys + threadIdx.x;
   float got = 0.f;
 #pragma unroll 4
-  for (int sp = 0; sp < p.csplit; ++sp) got += ldg(from + (int64_t)sp * p.keys);
+  for (int sp = 0; sp < p.csplit; ++sp) got += ldg(from + (int64_t)sp * kMassKeys);
   stg(to, row < x.len0 ? fmaf(p.decay, was, got) : got);
 }
 
 template <int D>
 void launch(const MassAttn &p, hipStream_t st) {
-  const dim3 grid((uint32_t)(p.units * p.ktiles * p.csplit)), block(p.keys);
-  if (p.keys == 512)
-    hipLaunchKernelGGL((k_mass_cols<D, 8>), grid, block, 0, st, p);
-  else
-    hipLaunchKernelGGL((k_mass_cols<D, 4>), grid, block, 0, st, p);
+  hipLaunchKernelGGL((k_mass_cols<D>), dim3((uint32_t)(p.units * p.ktiles * p.csplit)), dim3(NT), 0, st, p);
 }
 
 }  // namespace
@@ -250,8 +244,7 @@ hipError_t launch_mass_cols(const MassAttn &p, hipStream_t st) {
     launch<64>(p, st);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.csplit == 1) return e;
-  const int64_t tiles = ((int64_t)p.max_rows + 255) / 256;
-  hipLaunchKernelGGL(k_mass_sum, dim3((uint32_t)(p.units * tiles)), dim3(256), 0, st, p);
+  hipLaunchKernelGGL(k_mass_sum, dim3((uint32_t)(p.units * p.ktiles)), dim3(kMassKeys), 0, st, p);
   return hipGetLastError();
 }
 

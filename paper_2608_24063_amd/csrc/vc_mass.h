@@ -9,6 +9,7 @@ constexpr int kMassTile = 32;         // rows of a single token's tile
 constexpr int kMassHeld4 = 10112;     // logits that a workgroup of four waves keeps in LDS
 constexpr int kMassHeld8 = 30720;     // one of eight
 constexpr int kMassChunk = 1024;      // rows of a workgroup of k_finish
+constexpr int kMassKeys = 256;        // rows of a workgroup of k_mass_cols
 constexpr int kEvictBytes = 32768;    // keys (and as many values) of a workgroup of k_move
 constexpr int kMassMaxRows = INT32_MAX - 1024;  // so that the end of a row's tile is a row index
 
@@ -43,9 +44,9 @@ struct MassAttn {
   int32_t qcols, nqt, ns;
   float *part_o;          // partial results: [part][qcols][d], [part][qcols]
   float2 *part_ml;
-  // Prompts' masses: `ktiles` tiles of `keys` rows a unit, each tile's columns shared by
-  // csplit workgroups, and what each of several adds: [unit][tile][csplit][keys].
-  int32_t keys, ktiles, csplit;
+  // Prompts' masses: `ktiles` tiles of kMassKeys rows a unit, each tile's columns shared by
+  // csplit workgroups, and what each of several adds: [unit][tile][csplit][row].
+  int32_t ktiles, csplit;
   float *part_mass;
   float2 *stat;           // prompts: [unit][cols] maximum and 1 / sum of the weights
   // Per unit (rows before the call, rows now, queries, pieces): of single tokens in

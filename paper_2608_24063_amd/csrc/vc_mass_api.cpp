@@ -31,7 +31,7 @@ MassPool bind(const vc_mass_cache *c) {
 
 // How an attention call is cut, and the parts of its workspace.
 struct Cut {
-  int32_t waves = 0, piece = 0, npmax = 1, here = 0, ldr = 0, qcols = 0, nqt = 0, ns = 1, keys = 0, ktiles = 1, csplit = 1;
+  int32_t waves = 0, piece = 0, npmax = 1, here = 0, ldr = 0, qcols = 0, nqt = 0, ns = 1, ktiles = 1, csplit = 1;
   int64_t wgs = 0, slots = 0;  // workgroups; columns of partial results
   size_t ml = 0, stat = 0, state = 0, np = 0, logits = 0, mass = 0, total = 0;
 };
@@ -69,8 +69,8 @@ bool attend_cut(const vc_decode_shape *s, int32_t n, int32_t max_rows, Cut &c) {
     const int64_t room = (c.waves == 8 ? kMassHeld8 : kMassHeld4) / pitch / kMassTile * kMassTile;
     c.here = (int32_t)(c.npmax > 1 ? 0 : std::min(room, nt * kMassTile));
     c.ldr = (int32_t)(nt * kMassTile - c.here);
-    // The second launch's workgroups.
-    if (c.npmax > 1 && units * (((int64_t)max_rows + kMassChunk - 1) / kMassChunk) >= kMaxWg) return false;
+    // The second launch's workgroups (of 1024 threads).
+    if (c.npmax > 1 && units * (((int64_t)max_rows + kMassChunk - 1) / kMassChunk) >= kMaxWg / 2) return false;
   } else {
     const int64_t nt = std::max<int64_t>(1, ((int64_t)max_rows + kQ8Block - 1) / kQ8Block);
     c.qcols = cols > 128 ? 256 : 128;
@@ -84,14 +84,16 @@ bool attend_cut(const vc_decode_shape *s, int32_t n, int32_t max_rows, Cut &c) {
     c.wgs = c.ns > 1 ? std::min(resident, tiles * (nt / kQ8SplitBlocks)) : tiles;
     c.slots = c.ns > 1 ? c.wgs * c.qcols : 0;
     // The other launches' workgroups: the append's, the join's, the masses'.
-    c.keys = 256;
-    c.ktiles = (int32_t)std::max<int64_t>(1, ((int64_t)max_rows + c.keys - 1) / c.keys);
+    c.ktiles = (int32_t)std::max<int64_t>(1, ((int64_t)max_rows + kMassKeys - 1) / kMassKeys);
     const int64_t key_tiles = units * c.ktiles;
     if (units * (((int64_t)n * s->d + 2047) / 2048) >= kMaxWg || (c.slots && units * cols >= 2 * kMaxWg) ||
         key_tiles >= kMaxWg)
       return false;
-    // Columns of a row tile's masses are split where tiles are few against the 256
-    // workgroups that the card holds, eight blocks of columns at least together.
+    // A row tile's columns are split over workgroups (the card holds 512 of them) until
+    // there are 2048, eight blocks of columns at least together: tiles of later rows are
+    // seen by fewer columns, and many small workgroups even that out.  (us of the masses,
+    // columns in 1, 2 and 5 parts: 8 units of 25088 rows and 16384 columns 883 850 874; 12
+    // units of 9000 to 12900 rows and 455 columns, which stay whole, 35 38 50.)
     const int64_t blocks = (cols + 63) / 64;
     c.csplit = (int32_t)std::max<int64_t>(1, std::min<int64_t>(blocks / 8, (2048 + key_tiles - 1) / key_tiles));
     if (key_tiles * c.csplit >= kMaxWg) c.csplit = 1;
@@ -106,7 +108,7 @@ bool attend_cut(const vc_decode_shape *s, int32_t n, int32_t max_rows, Cut &c) {
   c.mass = c.logits + (token ? align_up(sizeof(float) * (size_t)(units * cols) * (size_t)c.ldr) : 0);
   c.total = c.mass;
   if (c.csplit > 1)
-    c.total += align_up(sizeof(float) * (size_t)units * (size_t)c.ktiles * (size_t)c.csplit * (size_t)c.keys);
+    c.total += align_up(sizeof(float) * (size_t)units * (size_t)c.ktiles * (size_t)c.csplit * kMassKeys);
   return true;
 }
 
@@ -190,7 +192,7 @@ vc_status viscache_mass_attend(const vc_decode_shape *s, const vc_mass_cache *c,
   p.state = reinterpret_cast<int4 *>(ws + cut.state);
   p.np = reinterpret_cast<int32_t *>(ws + cut.np);
   p.logits = reinterpret_cast<float *>(ws + cut.logits);
-  p.keys = cut.keys; p.ktiles = cut.ktiles; p.csplit = cut.csplit;
+  p.ktiles = cut.ktiles; p.csplit = cut.csplit;
   p.part_mass = reinterpret_cast<float *>(ws + cut.mass);
   hipStream_t hs = static_cast<hipStream_t>(stream);
   const hipError_t e = p.cols <= kTokenCols ? launch_mass_token(p, hs) : launch_mass_prompt(p, hs);
