@@ -166,7 +166,10 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt(MassAttn p) {
   for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
     for (int i = 0; i < 16; ++i) O[cb][i] = 0.f;
-  float m = kNegInf, l = 0.f;
+  // The sum of the weights, block by block: small weights added one at a time to the sum of
+  // thousands would be lost one at a time (7e-6 of the masses over 25000 rows), and what a
+  // block's addition rounds off is kept.
+  float m = kNegInf, l = 0.f, lost = 0.f;
   constexpr int NP = F32 ? 3 : 1;  // parts of P
   u32x4 P[NP][4];
 
@@ -242,17 +245,19 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt(MassAttn p) {
       const float alpha = mn == kNegInf ? 0.f : fast_exp2(m - mn);
       m = mn;
       l *= alpha;
+      lost *= alpha;
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb) O[cb] *= alpha;
     }
     const float off = m == kNegInf ? 0.f : -m;
+    float sum[4];
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
       float pr[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         pr[k] = fast_exp2(fmaf(S[s / 2][8 * (s % 2) + k], p.sc, off));
-        l += pr[k];
+        sum[s] = k == 0 ? pr[0] : sum[s] + pr[k];
       }
       if (F32) {
 #pragma unroll
@@ -265,6 +270,9 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt(MassAttn p) {
         P[0][s] = u32x4{pack_bf16(pr[0], pr[1]), pack_bf16(pr[2], pr[3]), pack_bf16(pr[4], pr[5]), pack_bf16(pr[6], pr[7])};
       }
     }
+    const float b = (sum[0] + sum[1]) + (sum[2] + sum[3]), to = l + b, was = to - b;
+    lost += (l - was) + (b - (to - was));
+    l = to;
   };
   // Keys of block i + 1 and values of block i into LDS, and the requests of the ones
   // after them.  Past the last block the last one again: under a condition the
@@ -317,7 +325,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt(MassAttn p) {
       if (live) outputs(tv[(T - 1) & 1]);
     }
   }
-  l = sum_halves(l);
+  l = sum_halves(l + lost);
   __syncthreads();  // (the last of bad)
   if ((t0 + T) * kBlock > fewest) {  // uniform
 #pragma unroll

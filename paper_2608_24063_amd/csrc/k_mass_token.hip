@@ -305,10 +305,9 @@ __global__ __launch_bounds__(64 * NW, 2) void k_token(MassAttn p) {
     m = mn;
     float pr[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      pr[i] = fast_exp2(fmaf(S[i / 4][i % 4], p.sc, -ref));
-      l += pr[i];
-    }
+    for (int i = 0; i < 8; ++i) pr[i] = fast_exp2(fmaf(S[i / 4][i % 4], p.sc, -ref));
+    // (Together first: small weights added one at a time to a long sum would be lost.)
+    l += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
     u32x4 part[3];
 #pragma unroll
     for (int y = 0; y < 3; ++y) {

@@ -136,7 +136,7 @@ def test_long_units_in_pieces(dev, d, n, Hq, Hkv):
     p.attend(p.inputs(n)[0], count=[0, 1])
 
 
-@pytest.mark.parametrize("n", [1, 2, 40])
+@pytest.mark.parametrize("n", [1, 2, 40, 300])
 def test_row_bound(dev, n):
     p = Pair(11, dev, 1, 2, 8, 2, 64, [100, 400, 64, 0], [200, 1500, 64 + n, n])
     for most in (0, 1, 64, 101, 300):
@@ -261,3 +261,59 @@ def test_refusals(dev):
     c.attend(q[:, :, :0], out[:, :, :0], 0.1, k=k[:, :, :0], v=v[:, :, :0])
     p.check_cache()
     assert not out.any()
+
+
+@pytest.mark.parametrize("n,rows", [(1, 200), (1, 6000), (4, 300), (3, 5000)])
+def test_order_of_units(dev, n, rows):
+    """Units in another order give the same bits; those that an order leaves out are left alone."""
+    lens = [rows, 7, rows // 2, 0, 33, rows - 1, 64, 1]
+    make = lambda: Pair(37, dev, 2, 2, 8, 2, 64, lens, [x + 2 * n + i for i, x in enumerate(lens)])  # noqa: E731
+    a, b, c = make(), make(), make()
+    q, k, v = (_bf16(x, dev) for x in a.inputs(n))
+    outs = [torch.full(q.shape, MARK, dtype=torch.float32, device=dev) for _ in range(3)]
+    orders = [a.c.order, torch.tensor([3, 1, 7, 0, 2, 6, 5, 4], dtype=torch.int32, device=dev),
+              torch.tensor([5, -1, 0, 8, 2 ** 31 - 1, 3, -2 ** 31, 1], dtype=torch.int32, device=dev)]
+    for x, o, out in zip((a, b, c), orders, outs):
+        x.c.c.order = o.data_ptr()
+        x.c.attend(q, out, 0.125, k=k, v=v, decay=0.5)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], outs[1]) and torch.equal(a.c.mass, b.c.mass) and torch.equal(a.c.len, b.c.len)
+    was, taken = make(), {0, 1, 3, 5}
+    for u, o in enumerate(a.off):
+        rows_, l, s, g = slice(o, o + a.units[u].cap), u // 4, u // 2 % 2, u % 2
+        like = a if u in taken else was
+        assert torch.equal(c.c.mass[rows_], like.c.mass[rows_]) and c.c.len[u] == like.c.len[u]
+        assert torch.equal(c.c.k_pool[rows_].view(torch.int16), like.c.k_pool[rows_].view(torch.int16))
+        heads = outs[2][l, s, :, 4 * g:4 * g + 4]
+        assert torch.equal(heads, outs[0][l, s, :, 4 * g:4 * g + 4]) if u in taken else (heads == MARK).all()
+
+
+@pytest.mark.parametrize("n", [1, 2, 40, 200])
+@pytest.mark.parametrize("fp32", [True, False])
+def test_sums_of_many_small_weights(dev, n, fp32):
+    """A row that takes a third of every query's weight and 30000 that share the rest: each of
+    them is 2^-13.7 of the first, so that a sum that takes them one after another rounds every
+    one to the same side (2^-24 in 2^-13.7), which adds up to some 2^-12 of the whole.
+    Tolerances: a logit in units of log 2 is 13.7, rounded once there and once in its factor
+    (2^-20 of a weight together), 2^-22 for the exponential; a sum of 1 / l adds at most 64 rows
+    or blocks one after another, a mass a thirty-second of the columns (2^-24 each).  An output
+    adds up 16 rows a product one product after another."""
+    from paper_2608_24063_amd.tensors import MassCache
+    rows, d, Hq = 30000, 64, 8
+    c = MassCache(1, 1, Hq, 1, d, [rows + n], dev)
+    c.k_pool.zero_()
+    c.v_pool.fill_(1.0)
+    q = torch.zeros((1, 1, n, Hq, d), dtype=torch.bfloat16, device=dev)
+    q[..., 0] = 1.0
+    c.k_pool[17, 0] = 9.5  # its weight is exp(9.5), that of the others 1
+    c.len.fill_(rows + n)
+    out = torch.zeros(q.shape, dtype=torch.float32 if fp32 else torch.bfloat16, device=dev)
+    c.attend(q, out, 1.0, decay=0.0)
+    mass = _np(c.mass)
+    total, tol = n * Hq, 2.0 ** -20 + 2.0 ** -22 + (64 + n * Hq / 32) * 2.0 ** -24
+    assert abs(mass.sum() - total) <= total * tol
+    want = np.array([np.exp(9.5) / (np.exp(9.5) + rows + i) for i in range(n)])
+    assert abs(mass[17] - Hq * want.sum()) <= mass[17] * tol
+    assert abs(mass[100] - Hq * (want / np.exp(9.5)).sum()) <= mass[100] * tol
+    most = 2.0 ** -20 + (rows / 16 + 64) * 2.0 ** -24
+    assert (out.float() - 1).abs().max() <= (most if fp32 else most + 2.0 ** -7 * 1.01)
