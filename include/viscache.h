@@ -678,7 +678,8 @@ size_t viscache_mass_attend_workspace_bytes(const vc_decode_shape *shape, int32_
  * decay: finite, not negative (1: nothing fades; 0: the last call's weights alone).
  * max_rows bounds every len after the append.  n = 0 does nothing.  n * Hq/Hkv <= 16
  * (single tokens, short drafts) is one launch, or two where units are cut along their
- * rows; more take three or four.  `workspace`: DEVICE, at least
+ * rows; more take two, and one each for an append, for outputs and for masses that are
+ * joined from parts.  `workspace`: DEVICE, at least
  * viscache_mass_attend_workspace_bytes bytes, 256-byte aligned; contents do not matter and
  * none are kept, so calls, captured ones among them, may share one as long as they do
  * not overlap.  VC_ERR_WORKSPACE comes after all other checks.  VC_ERR_UNSUPPORTED for
@@ -707,7 +708,7 @@ size_t viscache_mass_evict_workspace_bytes(const vc_decode_shape *shape, int32_t
  * attention (Hq is checked, not used).  max_rows bounds every len (rows past it are
  * evicted).  Two launches.  `workspace` as for viscache_mass_attend.  VC_ERR_ARG also
  * for a `to` that shares its pools, masses or lengths with the cache; VC_ERR_UNSUPPORTED
- * for 2^22 or more units or 2^23 or more chunks of 16 KB of keys. */
+ * for 2^22 or more units or 2^23 or more chunks of 32 KB of keys. */
 vc_status viscache_mass_evict(const vc_decode_shape *shape, const vc_mass_cache *cache, const vc_mass_cache *to,
                               const int32_t *keep, int32_t sinks, int32_t recent, int32_t max_rows, int32_t *index,
                               int32_t index_rows, void *workspace, size_t workspace_bytes, void *stream);

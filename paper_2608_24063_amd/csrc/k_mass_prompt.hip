@@ -10,6 +10,12 @@
 // a lane's logits are the k-elements of its own P^T operand; P never leaves the
 // registers, and V's operands are transposing reads of its row-major block.
 //
+// 16384 columns over 8 units of 25088 rows, 128 channels: 1480 to 1560 us (1.05 to 1.1
+// PFLOP/s, the matrix cores busy for 0.54 of the time, at the clock that they leave).
+// Without the operands' reads and the weights it takes 1049, products and supply without
+// weights 1250, weights and supply without products 892.  455 columns over 12 units of
+// 9000 to 12900 rows: append 5, attention 40, join 8.
+//
 // With bf16 outputs a weight is rounded to bf16 before it meets its value (2^-8 of
 // itself): a choice of speed, since the errors of a column's weights average out and
 // stay under the half step of the output unless its values cancel, and a second part
