@@ -5,10 +5,12 @@
 // k_choose, a workgroup a unit, finds the threshold exactly: a most-significant-digit radix
 // select over the masses' bits (digits of 11, 11 and 10 bits, counted in LDS), then one
 // pass that gives every kept row its place by ballots and prefix sums.  A chain of LDS
-// round trips bounds it (us: 8 units of 200 rows 6, 112 of 2400 to 3136 rows 9.4, 896 of 2300
-// to 5800 42).  k_move copies the rows, a workgroup 32 KB of keys and 32 of values, and is
-// bound by memory: half of those 896 units into another cache 446 us (5.7 TB/s read and
-// written); 0.6 of the 112 in place 47 (4.5 TB/s).
+// round trips bounds it (us: 8 units of 200 rows 6, 112 of 2400 to 3136 rows 7.4, 896 of
+// 2300 to 5800 19.5; with every pass reading the masses again 6, 9.4, 43).
+//
+// k_move copies the rows, a workgroup 32 KB of keys and 32 of values, and is bound by
+// memory: half of those 896 units into another cache 446 us (5.7 TB/s read and written);
+// 0.6 of the 112 in place 47 (4.5 TB/s).
 //
 // In place a row's new place may hold a row that has yet to move.  Rows only move down and
 // keep their order, so the rows of a chunk of new places come from that chunk or later
@@ -58,6 +60,18 @@ __global__ __launch_bounds__(NT) void k_choose(EvictPlan p) {
     for (int i = tid; i < p.chunks; i += NT) stg(p.flags + (int64_t)u * p.chunks + i, 0u);
     if (tid == 0) stg(p.ticket + u, 0u);
   }
+  // A wave takes 256 rows of a tile of 4 NT, 64 at a time.  The keys of two tiles stay in
+  // registers, further ones are read again in each pass.
+  constexpr int kTile = 4 * NT, kHeld = 2;
+  const int mine = 256 * w + lane;  // the lane's first row in a tile
+  uint32_t held[kHeld][4];
+  auto keys = [&](int t0, uint32_t (&x)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = key_of(ldg(mass + min(t0 + mine + 64 * j, n - 1)));
+  };
+#pragma unroll
+  for (int h = 0; h < kHeld; ++h)
+    if (h * kTile < n) keys(h * kTile, held[h]);  // uniform
   if (left > 0u && left < (uint32_t)(mid - a)) {  // uniform
 #pragma unroll 1
     for (int pass = 0; pass < 3; ++pass) {
@@ -65,9 +79,20 @@ __global__ __launch_bounds__(NT) void k_choose(EvictPlan p) {
       const uint32_t bins = pass == 2 ? 1024u : 2048u, known = pass == 0 ? 0u : ~0u << (pass == 1 ? 21 : 10);
       for (int i = 4 * tid; i < kBins; i += 4 * NT) *reinterpret_cast<u32x4 *>(hist + i) = u32x4{0u, 0u, 0u, 0u};
       __syncthreads();
-      for (int t = a + tid; t < mid; t += NT) {
-        const uint32_t x = key_of(ldg(mass + t));
-        if ((x & known) == T) atomicAdd(&hist[x >> sh & (bins - 1u)], 1u);
+      auto count = [&](int t0, const uint32_t (&x)[4]) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int t = t0 + mine + 64 * j;
+          if (t >= a && t < mid && (x[j] & known) == T) atomicAdd(&hist[x[j] >> sh & (bins - 1u)], 1u);
+        }
+      };
+#pragma unroll
+      for (int h = 0; h < kHeld; ++h)
+        if (h * kTile < n) count(h * kTile, held[h]);
+      for (int t0 = kHeld * kTile; t0 < n; t0 += kTile) {
+        uint32_t x[4];
+        keys(t0, x);
+        count(t0, x);
       }
       __syncthreads();
       if (w == 0) {  // the bin that holds rank `left` from the top: lane l sums bins of 32 in descending order
@@ -93,20 +118,19 @@ __global__ __launch_bounds__(NT) void k_choose(EvictPlan p) {
       left = found[1];
     }
   }
-  // Every kept row's place.  A wave takes 256 rows of a tile, by four ballots of 64.
+  // Every kept row's place.
   int32_t *list = p.list + (int64_t)u * p.ldl;
   int32_t *index = p.index ? p.index + (int64_t)u * p.index_rows : nullptr;
   uint32_t kept = 0u, equal = 0u;  // before the tile
-  for (int t0 = 0, it = 0; t0 < n; t0 += 4 * NT, it ^= 1) {
+  auto places = [&](int t0, int it, const uint32_t (&x)[4]) {
     uint64_t sure[4], tie[4];
     uint32_t ns = 0u, ne = 0u;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int t = t0 + 256 * w + 64 * j + lane;
-      const uint32_t x = key_of(ldg(mass + min(t, n - 1)));
+      const int t = t0 + mine + 64 * j;
       const bool in = t >= a && t < mid;
-      sure[j] = __builtin_amdgcn_ballot_w64(t < n && (!in || x > T));
-      tie[j] = __builtin_amdgcn_ballot_w64(in && x == T);
+      sure[j] = __builtin_amdgcn_ballot_w64(t < n && (!in || x[j] > T));
+      tie[j] = __builtin_amdgcn_ballot_w64(in && x[j] == T);
       ns += (uint32_t)__builtin_popcountll(sure[j]);
       ne += (uint32_t)__builtin_popcountll(tie[j]);
     }
@@ -127,13 +151,21 @@ __global__ __launch_bounds__(NT) void k_choose(EvictPlan p) {
       const bool is = sure[j] >> lane & 1, ie = (tie[j] >> lane & 1) && e < left;
       const uint32_t at = s + min(e, left);
       if ((is || ie) && at < (uint32_t)k) {
-        const int t = t0 + 256 * w + 64 * j + lane;
+        const int t = t0 + mine + 64 * j;
         stg(list + at, t);
         if (index && at < (uint32_t)p.index_rows) stg(index + at, t);
       }
       bs += (uint32_t)__builtin_popcountll(sure[j]);
       be += (uint32_t)__builtin_popcountll(tie[j]);
     }
+  };
+#pragma unroll
+  for (int h = 0; h < kHeld; ++h)
+    if (h * kTile < n) places(h * kTile, h & 1, held[h]);
+  for (int t0 = kHeld * kTile, it = 0; t0 < n; t0 += kTile, it ^= 1) {
+    uint32_t x[4];
+    keys(t0, x);
+    places(t0, it, x);
   }
   if (tid == 0) {
     stg(p.count + u, k);
@@ -208,10 +240,16 @@ void launch_move(const EvictPlan &p, hipStream_t st) {
 }  // namespace
 
 hipError_t launch_mass_evict(const EvictPlan &p, hipStream_t st) {
+  // More threads where few units are long.  (us, 512 and 1024 threads: 8 units of 25000 rows
+  // 34.4 28.0, 64 of 12000 17.8 14.4, 112 of 3000 7.4 7.1, 256 of 5000 10.8 11.2, 504 of 2500
+  // 10.7 13.8, 600 of 3000 13.5 19.5, 912 of 12000 43 56; 256 and 512: 112 of 3000 11.0 7.4.)
+  const dim3 grid((uint32_t)p.units);
   if (p.max_rows <= 2048)
-    hipLaunchKernelGGL((k_choose<256>), dim3((uint32_t)p.units), dim3(256), 0, st, p);
+    hipLaunchKernelGGL((k_choose<256>), grid, dim3(256), 0, st, p);
+  else if (p.max_rows <= 8192 || p.units > 256)
+    hipLaunchKernelGGL((k_choose<512>), grid, dim3(512), 0, st, p);
   else
-    hipLaunchKernelGGL((k_choose<1024>), dim3((uint32_t)p.units), dim3(1024), 0, st, p);
+    hipLaunchKernelGGL((k_choose<1024>), grid, dim3(1024), 0, st, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.chunks == 0) return e;
   if (p.d == 128)
