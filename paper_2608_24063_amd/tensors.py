@@ -457,18 +457,20 @@ class NormRope:
         if (q is None) != (q_dout is None) or (k is None) != (k_dout is None):
             raise ValueError("rows without their outputs' gradients, or gradients without rows")
         new = torch.zeros_like if count is not None else torch.empty_like
-        side, out, dw = [], [], [None, None]
-        for i, (x, g, o, name) in enumerate(((q, q_dout, q_din, "q"), (k, k_dout, k_din, "k"))):
+        side, out, dw = [], [], []
+        for x, w, g, o, name in ((q, q_weight, q_dout, q_din, "q"), (k, k_weight, k_dout, k_din, "k")):
             if x is None:
-                side += [None, None, None, 0]
+                side += (None, None, None, 0)
                 out.append(None)
+                dw.append(None)
                 continue
             xr, gr = _take(x, name, None, typ, index), _take(g, name + "_dout", x.shape, typ, index)
             if o is None:
                 o = new(x, memory_format=torch.contiguous_format)
-            dw[i] = torch.empty((L, self.d), dtype=_FP32, device=x.device)
-            side += [xr, gr, _take(o, name + "_din", x.shape, typ, index), dw[i].data_ptr()]
+            w = torch.empty_like(w, dtype=_FP32)  # contiguous, as the weights are
+            side += (xr, gr, _take(o, name + "_din", x.shape, typ, index), w.data_ptr())
             out.append(o)
+            dw.append(w)
         if L == 0:
             return (*out, *dw)
         if B == 0 or n == 0:
@@ -479,7 +481,7 @@ class NormRope:
                 self._bytes.clear()
             need = self._bytes[shape, n] = self._lib.viscache_norm_rope_grad_workspace_bytes(shape, n)
         # Of this call alone: the allocator orders its reuse after the stream's work.
-        ws = torch.empty((max(need, 1),), dtype=torch.uint8, device=dw[0 if q is not None else 1].device)
+        ws = (q if k is None else k).new_empty((max(need, 1),), dtype=torch.uint8)
         _enqueue("viscache_norm_rope_grad", self._lib.viscache_norm_rope_grad, index, shape,
                  self.rope._address[typ is _FP32][bool(inverse)], norm, n, *at, *side, ws.data_ptr(), need)
         _changed([o for o in out if o is not None])
