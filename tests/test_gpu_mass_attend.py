@@ -317,3 +317,48 @@ def test_sums_of_many_small_weights(dev, n, fp32):
     assert abs(mass[100] - Hq * (want / np.exp(9.5)).sum()) <= mass[100] * tol
     most = 2.0 ** -20 + (rows / 16 + 64) * 2.0 ** -24
     assert (out.float() - 1).abs().max() <= (most if fp32 else most + 2.0 ** -7 * 1.01)
+
+
+@pytest.mark.parametrize("n,fp32", [(1, True), (3, False), (40, False), (40, True)])
+def test_rows_past_32_bits(dev, n, fp32):
+    """A unit whose last rows are past 2^31 elements of its pools and one behind it, whose keys
+    are zero but for one of logit 20 near the end: outputs, masses, the append and an eviction
+    that leaves that row, the first and the last ones.  Tolerances as in tests/mass_ref.py, with
+    2^-18 for the logit of 20 (2^-24 of it from the scale's rounding, half a step at 28.9, its
+    value in units of log 2, in each of the maximum and the difference) and the exponentials."""
+    from paper_2608_24063_amd.tensors import MassCache
+    rows, d, far, small = 17_000_000, 128, 16_999_990, 70
+    c = MassCache(1, 1, 2, 2, d, [rows + n, small + n], dev)
+    c.v_pool.fill_(1.0)
+    first = [0, rows + n]
+    for o, r in zip(first, (far, 60)):
+        c.k_pool[o + r, 0], c.v_pool[o + r] = 20.0, 3.0
+    c.len.copy_(torch.tensor([rows, small], dtype=torch.int32))
+    q, k = (torch.zeros((1, 1, n, 2, d), dtype=torch.bfloat16, device=dev) for _ in range(2))
+    q[..., 0] = 1.0
+    k[..., 1] = 2.0  # (logit 0 too)
+    v = torch.full_like(k, 2.0)
+    out = torch.zeros(q.shape, dtype=torch.float32 if fp32 else torch.bfloat16, device=dev)
+    c.attend(q, out, 1.0, k=k, v=v)
+    assert c.len.tolist() == [rows + n, small + n]
+    e = np.exp(20.0)
+    for u, (o, r, hit) in enumerate(zip(first, (rows, small), (far, 60))):
+        i = np.arange(n)
+        total = e + r + i  # of query i: the loud row, the others and i + 1 new ones
+        want = (3 * e + (r - 1) + 2 * (i + 1)) / total
+        tol = want * ((3 * r / 32 + 128) * 2.0 ** -24 + 2.0 ** -18 + (0 if fp32 else 2.0 ** -7 * 1.01))
+        assert (np.abs(_np(out[0, 0, :, u]) - want[:, None]) <= tol[:, None]).all(), u
+        mass = c.mass[o:o + r + n]
+        near = (r / 32 + 192) * 2.0 ** -24 + 2.0 ** -18
+        for row, m in ((hit, (e / total).sum()), (0, (1 / total).sum()), (hit - 1, (1 / total).sum()),
+                       (r, (1 / total).sum()), (r + n - 1, 1 / total[-1])):
+            assert abs(float(mass[row]) - m) <= m * near, (u, row)
+        assert (c.k_pool[o + r:o + r + n, 1] == 2).all() and (c.v_pool[o + r:o + r + n] == 2).all()
+    index = torch.full((2, 4), -1, dtype=torch.int32, device=dev)
+    c.evict(torch.tensor([4, 4], dtype=torch.int32, device=dev), sinks=1, recent=2, index=index)
+    assert c.len.tolist() == [4, 4]
+    for u, (o, r, hit) in enumerate(zip(first, (rows, small), (far, 60))):
+        want = sorted({0, hit, r + n - 2, r + n - 1})
+        assert index[u].tolist() == want
+        assert c.k_pool[o:o + 4, 0].tolist() == [20.0 if x == hit else 0.0 for x in want]
+        assert c.v_pool[o:o + 4, 5].tolist() == [3.0 if x == hit else 2.0 if x >= r else 1.0 for x in want]
