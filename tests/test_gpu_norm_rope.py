@@ -281,3 +281,35 @@ def test_refusals(dev):
     for f in bad:
         with pytest.raises(ValueError):
             f()
+
+
+def test_rows_past_32_bits(dev):
+    """More than 2^31 values of queries: the first and last tokens have the bits of a call of their own."""
+    from paper_2608_24063_amd.tensors import NormRope, Rope
+    n, Hq, Hkv, d, m = 140_000, 128, 8, 128, 9
+    rope = NormRope(Rope(d, theta=1e4))
+    g = torch.Generator(device=dev)
+    g.manual_seed(3)
+    rows = lambda H: torch.randn((1, 1, n, H, d), generator=g, device=dev, dtype=torch.bfloat16)  # noqa: E731
+    q, k, dq, dk = rows(Hq), rows(Hkv), rows(Hq), rows(Hkv)
+    w = torch.randn((2, 1, d), generator=g, device=dev)
+    pos = torch.arange(n, dtype=torch.int32, device=dev).expand(3, 1, n).contiguous()
+    dq[:, :, m:-m] = 0  # (the weights' gradients are those tokens' alone)
+    dk[:, :, m:-m] = 0
+    oq, ok = rope.apply(pos, q, k, w[0], w[1], q_out=torch.empty_like(q), k_out=torch.empty_like(k))
+    gq, gk, wq, wk = rope.grad(pos, q, k, w[0], w[1], dq, dk)
+    sums = [0, 0]
+    for sl in (slice(0, m), slice(n - m, n)):
+        cut = lambda x: x[:, :, sl].clone()  # noqa: E731  (turned in place)
+        p = pos[:, :, sl].contiguous()
+        a, b = rope.apply(p, cut(q), cut(k), w[0], w[1])
+        assert torch.equal(a, oq[:, :, sl]) and torch.equal(b, ok[:, :, sl])
+        a, b, wa, wb = rope.grad(p, cut(q), cut(k), w[0], w[1], cut(dq), cut(dk))
+        assert torch.equal(a, gq[:, :, sl]) and torch.equal(b, gk[:, :, sl])
+        sums = [sums[0] + wa.double(), sums[1] + wb.double()]
+    assert not gq[:, :, m:-m].any() and not gk[:, :, m:-m].any()
+    # Two sums of the same terms in other orders: at most 2 m H + 1024 roundings of the sum of the
+    # terms' magnitudes, which are normal values' products: well below 8 sqrt 2 on average.
+    for got, want, H in ((wq, sums[0], Hq), (wk, sums[1], Hkv)):
+        terms = 2 * m * H
+        assert (got.double() - want).abs().max() <= 2 * (terms + 1024) * 2.0 ** -24 * terms * 8 * 2 ** 0.5
