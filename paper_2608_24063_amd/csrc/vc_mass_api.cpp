@@ -52,10 +52,14 @@ bool attend_cut(const vc_decode_shape *s, int32_t n, int32_t max_rows, Cut &c) {
     // of 12000 21.7 15.7 15.6 19.1 124; 32 of 1000 11.4 12.7 14.8 16.0 16.2, of 4000 25.7
     // 20.8 19.4 20.3 46.5; 64 of 1000 15.4 14.2 16.3 16.8 17.2, of 4000 39.8 31.3 28.8 28.6
     // 47.0; 112 of 1000 24.3 21.1 19.7 17.8 18.1, of 2000 37.1 30.8 27.6 26.9 28.5, of 12000
-    // 217 188 179 175 199.  A unit of 400 rows takes 10.7 whole.)
+    // 217 188 179 175 199.  A unit of 400 rows takes 10.7 whole.)  Units so long that the
+    // pieces of 1024 workgroups are, too, even out better in as many (256 and 1024
+    // workgroups: 112 units of 12000 rows 181 173, of 23000 341 320, of 4000 to 12000 132 127,
+    // of 4000 47 47; 32 of 23000 97 100, 64 of 4000 29 31).
     const auto fours = [](int64_t x) { return (x + 3) / 4 * 4; };
     c.qcols = kTokenCols;
-    c.piece = (int32_t)std::max<int64_t>({4, fours((units * nt + 255) / 256), fours((nt + 23) / 24)});
+    const int64_t want = units * nt > 32768 ? 1024 : 256;
+    c.piece = (int32_t)std::max<int64_t>({4, fours((units * nt + want - 1) / want), fours((nt + 23) / 24)});
     if (nt <= 12 || units > 128 || (units > 96 && nt <= 48)) c.piece = (int32_t)nt;
     c.npmax = (int32_t)((nt + c.piece - 1) / c.piece);
     c.wgs = units * c.npmax;
