@@ -97,9 +97,14 @@ bool attend_cut(const vc_decode_shape *s, int32_t n, int32_t max_rows, Cut &c) {
     // there are 2048, eight blocks of columns at least together: tiles of later rows are
     // seen by fewer columns, and many small workgroups even that out.  (us of the masses,
     // columns in 1, 2 and 5 parts: 8 units of 25088 rows and 16384 columns 883 850 874; 12
-    // units of 9000 to 12900 rows and 455 columns, which stay whole, 35 38 50.)
+    // units of 9000 to 12900 rows and 455 columns, which stay whole, 35 38 50.)  Down to a
+    // block each where tiles are so few that this makes no more than 256, one a CU.  (us of a
+    // call, whole and split: 455 columns, 4 units of 3000 rows 50.3 43.6, of 12000 58.6 60.1
+    // in two parts; 280 columns, 4 units of 1000 40.8 36.8; 1400 columns, 4 units of 3000
+    // 63.1 54.9; 800 columns and 64 channels, a unit of 2000 39.8 29.6.)
     const int64_t blocks = (cols + 63) / 64;
-    c.csplit = (int32_t)std::max<int64_t>(1, std::min<int64_t>(blocks / 8, (2048 + key_tiles - 1) / key_tiles));
+    c.csplit = (int32_t)std::max<int64_t>({1, std::min<int64_t>(blocks / 8, (2048 + key_tiles - 1) / key_tiles),
+                                           std::min<int64_t>(blocks, 256 / key_tiles)});
     if (key_tiles * c.csplit >= kMaxWg) c.csplit = 1;
   }
   if (c.wgs >= kMaxWg) return false;
