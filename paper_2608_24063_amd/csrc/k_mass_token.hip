@@ -440,9 +440,10 @@ __global__ __launch_bounds__(64 * NW, 2) void k_token(MassAttn p) {
 // Workgroup (unit, chunk of rows) of a unit in several pieces: the columns that fall to
 // the chunk from their pieces, 1024 / d at a time, and the chunk's masses.  Bound by
 // latency, so all that it reads is requested at once, as soon as the unit is known.
-template <int D>
+template <int D, int R>
 __global__ __launch_bounds__(kMassChunk) void k_finish(MassAttn p) {
   constexpr int NC = kMassChunk / D, U = 8;  // columns at a time, pieces in flight
+  constexpr int kRows = kMassChunk * R;      // of a chunk
   __shared__ float2 ml[16];  // maximum and 1 / sum
   const int u = unit_of(p, (int)(blockIdx.x % (uint32_t)p.units)), ch = (int)(blockIdx.x / (uint32_t)p.units);
   if (u < 0) return;  // (nothing has written what its pieces leave)
@@ -456,12 +457,12 @@ __global__ __launch_bounds__(kMassChunk) void k_finish(MassAttn p) {
   const int np = (int)st.w;
   if (ch == 0 && tid == 0 && p.append) stg(p.c.len + u, x.held);
   if (np <= 1) return;
-  const int cols = x.cnt * p.G, emax = min(x.held, p.max_rows), nch = (emax + kMassChunk - 1) / kMassChunk;
+  const int cols = x.cnt * p.G, emax = min(x.held, p.max_rows), nch = (emax + kRows - 1) / kRows;
   if (ch >= nch) return;
   const int64_t slot = (int64_t)u * p.npmax;
   const float2 *pm = p.part_ml + slot * 16;
   const float *lu = p.logits + (int64_t)u * p.cols * p.ldr;
-  const int r = ch * kMassChunk + tid, rc = min(r, emax - 1);
+  const int r = ch * kRows + R * tid, rc = min(r, (emax - 1) / R * R);
   // Column tid / 16's pieces tid % 16, + 16, ...
   const int mc = min(tid / 16, cols - 1), m0 = tid % 16;
   const float2 a = ldg(pm + min(m0, np - 1) * 16 + mc);
@@ -477,7 +478,7 @@ __global__ __launch_bounds__(kMassChunk) void k_finish(MassAttn p) {
     }
   };
   pieces(min(col0, cols - 1), 0);
-  MassRows<1> rows;
+  MassRows<R> rows;
   rows.request(p, x, lu, cols, rc, emax);
   if (tid < 256) {
     float M = m0 < np ? a.x : kNegInf, s = m0 < np ? a.y : 0.f;
@@ -520,7 +521,13 @@ hipError_t launch(const MassAttn &p, hipStream_t st) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.npmax == 1) return e;
   const int64_t chunks = ((int64_t)p.max_rows + kMassChunk - 1) / kMassChunk;
-  hipLaunchKernelGGL((k_finish<D>), dim3((uint32_t)(p.units * chunks)), dim3(kMassChunk), 0, st, p);
+  // Four rows a thread where one would take more than the 512 workgroups that the card holds.
+  // (us of both launches, one and four rows: 112 units of 23000 319 309, of 12000 172.5
+  // 168.5, of 4000 47.5 48.6; 64 of 12000 98.4 96.4, of 4000 29.0 32.4; 4 of 12000 15.6 17.5.)
+  if (p.units * chunks > 512)
+    hipLaunchKernelGGL((k_finish<D, 4>), dim3((uint32_t)(p.units * ((chunks + 3) / 4))), dim3(kMassChunk), 0, st, p);
+  else
+    hipLaunchKernelGGL((k_finish<D, 1>), dim3((uint32_t)(p.units * chunks)), dim3(kMassChunk), 0, st, p);
   return hipGetLastError();
 }
 

@@ -8,7 +8,7 @@ namespace vc {
 constexpr int kMassTile = 32;         // rows of a single token's tile
 constexpr int kMassHeld4 = 10112;     // logits that a workgroup of four waves keeps in LDS
 constexpr int kMassHeld8 = 30 * 1024; // one of eight
-constexpr int kMassChunk = 1024;      // rows of a workgroup of k_finish
+constexpr int kMassChunk = 1024;      // threads of a workgroup of k_finish, of one row or four
 constexpr int kMassKeys = 256;        // rows of a workgroup of k_mass_cols
 constexpr int kEvictBytes = 32768;    // keys (and as many values) of a workgroup of k_move
 constexpr int kMassMaxRows = INT32_MAX - 1024;  // so that the end of a row's tile is a row index

@@ -362,3 +362,15 @@ def test_rows_past_32_bits(dev, n, fp32):
         assert index[u].tolist() == want
         assert c.k_pool[o:o + 4, 0].tolist() == [20.0 if x == hit else 0.0 for x in want]
         assert c.v_pool[o:o + 4, 5].tolist() == [3.0 if x == hit else 2.0 if x >= r else 1.0 for x in want]
+
+
+@pytest.mark.parametrize("n", [1, 2])
+def test_many_long_units_in_pieces(dev, n):
+    """Units so many and long that the second launch takes four rows a thread."""
+    rng = np.random.default_rng(41)
+    lens = [int(x) for x in rng.integers(7000, 9000, 64)]
+    lens[3], lens[17], lens[40], lens[41] = 0, 5, 8191, 4097
+    p = Pair(41, dev, 4, 4, 4, 4, 64, lens, [x + 2 * n + 1 for x in lens])
+    p.attend(*p.inputs(n))
+    p.attend(*p.inputs(n), count=[n, 0, n - 1, n], decay=0.5, fp32=False)
+    p.attend(p.inputs(n)[0], max_rows=8190)
