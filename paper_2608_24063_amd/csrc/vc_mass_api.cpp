@@ -77,11 +77,15 @@ bool attend_cut(const vc_decode_shape *s, int32_t n, int32_t max_rows, Cut &c) {
     if (c.npmax > 1 && units * (((int64_t)max_rows + kMassChunk - 1) / kMassChunk) >= kMaxWg / 2) return false;
   } else {
     const int64_t nt = std::max<int64_t>(1, ((int64_t)max_rows + kQ8Block - 1) / kQ8Block);
-    // Two workgroups of 128 columns hide each other's start, which counts where rows are few.
-    // (us of a call, 256 and 128 columns: 640 units, 300 rows and 2400 columns 668 626, 595
-    // and 2840 1075 1032, 600 and 4800 1424 1435; 112 units, 500 and 2100 145.4 140.6, 900
-    // and 2100 219 222, 1065 and 455 81.4 86.5, 3300 and 2100 657 701.)
-    c.qcols = cols > 128 && nt > 8 ? 256 : 128;
+    // Two workgroups of 128 columns hide each other's start, which counts where rows are few,
+    // and make more parts where all work is little.  (us of a call, 256 and 128 columns: 640
+    // units, 300 rows and 2400 columns 668 626, 595 and 2840 1075 1032, 600 and 4800 1424
+    // 1435; 112 units, 500 and 2100 145.4 140.6, 900 and 2100 219 222, 1065 and 455 81.4 86.5,
+    // 3300 and 2100 657 701; 4 units, 600 and 4200 50.8 46.7, 1040 and 280 37.3 32.7; 8 of
+    // 1100 and 800 47.9 43.0; 20 of 1564 and 512 52.5 53.8; 12 of 4065 and 455 57.8 58.3.)
+    const int64_t wide = units * ((cols + 255) / 256);
+    const bool few = nt <= 8 || (wide <= 768 && wide * nt <= 768);
+    c.qcols = cols > 128 && !few ? 256 : 128;
     const int64_t nqt = (cols + c.qcols - 1) / c.qcols, tiles = units * nqt;
     if (tiles >= kMaxWg) return false;
     const int64_t resident = c.qcols == 256 ? 256 : 512;
