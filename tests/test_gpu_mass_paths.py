@@ -4,7 +4,8 @@ import numpy as np
 import pytest
 
 from tests import mass_paths as mp
-from tests.test_gpu_mass_attend import Pair, _bf16, dev  # noqa: F401
+from tests.test_gpu_mass_attend import _bf16, dev  # noqa: F401
+from tests.test_gpu_mass_finite import Finite
 
 pytestmark = pytest.mark.gpu
 
@@ -13,7 +14,7 @@ torch = pytest.importorskip("torch")
 
 def _pair(p, dev, d, seed=43):  # noqa: F811
     lens, caps = mp.sizes(p)
-    return Pair(seed, dev, p.L, p.B, p.Hq, p.Hkv, d, lens, caps)
+    return Finite(seed, dev, p.L, p.B, p.Hq, p.Hkv, d, lens, caps)
 
 
 @pytest.mark.parametrize("p", mp.TOKENS + mp.PROMPTS, ids=lambda p: p.name)
