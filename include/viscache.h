@@ -675,7 +675,8 @@ size_t viscache_mass_attend_workspace_bytes(const vc_decode_shape *shape, int32_
  * from the shape, max_rows, the lengths and the counts.  A weight meets its value with
  * 24 bits; with n * Hq/Hkv > 16 and bf16 outputs it is rounded to bf16 there (2^-8 of
  * itself; a caller that needs more asks for fp32 outputs).
- * decay: finite, not negative (1: nothing fades; 0: the last call's weights alone).
+ * decay: finite, not negative (1: nothing fades; 0: the last call's weights alone, whatever the
+ * masses were; any other leaves masses that are infinite or NaN so).
  * max_rows bounds every len after the append.  n = 0 does nothing.  n * Hq/Hkv <= 16
  * (single tokens, short drafts) is one launch, or two where units are cut along their
  * rows; more take two, and one each for an append, for outputs and for masses that are

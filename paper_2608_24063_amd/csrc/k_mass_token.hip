@@ -102,7 +102,7 @@ struct MassRows {
     }
 #pragma unroll
     for (int i = 0; i < R; ++i)
-      if (t + i < last) stg(p.c.mass + x.off + t + i, t + i < x.len0 ? fmaf(p.decay, was[i], got[i]) : got[i]);
+      if (t + i < last) stg(p.c.mass + x.off + t + i, mass_after(p, t + i < x.len0, was[i], got[i]));
   }
 };
 
@@ -423,7 +423,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_token(MassAttn p) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) got += weight_of(p, c0 + i < cols ? y[i] : kNegInf, sm.stat[(c0 + i) & 15]);
     }
-    stg(p.c.mass + x.off + r, r < x.len0 ? fmaf(p.decay, before, got) : got);
+    stg(p.c.mass + x.off + r, mass_after(p, r < x.len0, before, got));
   };
 #pragma unroll
   for (int i = 0; i < WAS; ++i)

@@ -25,6 +25,12 @@ __device__ __forceinline__ MassUnit mass_unit(const MassAttn &p, int u) {
   return x;
 }
 
+// A row's mass after a call that gave it `got`; `old`: it was there before.  (A decay of zero
+// takes nothing over, which a product would of a mass that is infinite or no number.)
+__device__ __forceinline__ float mass_after(const MassAttn &p, bool old, float was, float got) {
+  return old && p.decay != 0.f ? fmaf(p.decay, was, got) : got;
+}
+
 // Column col of unit u (query col / G, head col % G of its kv head) in q or out.
 __device__ __forceinline__ int64_t mass_col(const MassAttn &p, const RowsDesc &r, int u, int col) {
   const int g = u % p.Hkv, lb = u / p.Hkv;
