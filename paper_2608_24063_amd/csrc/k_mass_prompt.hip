@@ -92,7 +92,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_prompt(MassAttn p) {
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int ln = lane & 31, hf = lane >> 5;
   Share sh;
-  if (p.append)  // (two copies, so that no load in them is under a condition)
+  if (p.append)  // (two copies, so that it is not asked tile by tile)
     sh = share_of(p, blockIdx.x, lane, [&](int u) {
       const u32x4 s = ld16(p.state + u);
       return Held{(int)s.y, (int)s.z, ldg(p.c.row_off + u)};

@@ -328,22 +328,20 @@ __device__ __forceinline__ Share share_of(const Plan &p, uint32_t bid, int lane,
   // block against 2.0), and count as that.
   constexpr int KM = kQ8SplitTiles / 64;
   const int tiles = p.units * p.nqt, K = (tiles + 63) / 64;
-  // (All requests before anything waits for one.)
   int nb[KM], held[KM], cnt[KM];
   int64_t off[KM];
   float all = 0.f;
-  Held h[KM];
-#pragma unroll
-  for (int k = 0; k < KM; ++k) h[k] = info((int)((uint32_t)min(K * lane + k, tiles - 1) / (uint32_t)p.nqt));
 #pragma unroll
   for (int k = 0; k < KM; ++k) {
+    if (k >= K) break;  // uniform
     const int t = K * lane + k, u = (int)((uint32_t)min(t, tiles - 1) / (uint32_t)p.nqt);
-    held[k] = h[k].rows;
-    cnt[k] = h[k].cnt;
-    off[k] = h[k].off;
+    const Held h = info(u);
+    held[k] = h.rows;
+    cnt[k] = h.cnt;
+    off[k] = h.off;
     const int c0 = (t - u * p.nqt) * p.qcols, cl = min(c0 + p.qcols, cnt[k] * p.G) - 1;
     const int seen = min(p.causal ? held[k] - cnt[k] + 1 + (int)((uint32_t)max(cl, 0) / (uint32_t)p.G) : held[k], p.max_rows);
-    nb[k] = k < K && t < tiles && cl >= c0 ? max((seen + kQ8Block - 1) / kQ8Block, 1) : 0;
+    nb[k] = t < tiles && cl >= c0 ? max((seen + kQ8Block - 1) / kQ8Block, 1) : 0;
     if (p.qcols == 256 && cl - c0 < 128) nb[k] -= nb[k] / 4;
     all += (float)nb[k];
   }
