@@ -210,7 +210,7 @@ __global__ __launch_bounds__(NT, 2) void k_mass_cols(MassAttn p) {
   if (p.csplit > 1)
     stg(p.part_mass + ((int64_t)ut * p.csplit + sp) * NT + 64 * w + lane, got);
   else
-    stg(to, mass_after(p, row < x.len0, ldg(to), got));
+    stg(to, fmaf(p.decay, row < fading_rows(p, x) ? ldg(to) : 0.f, got));
 }
 
 // The masses of a tile from its splits, in their order.
@@ -231,7 +231,7 @@ __global__ __launch_bounds__(kMassKeys) void k_mass_sum(MassAttn p) {
   float got = 0.f;
 #pragma unroll 4
   for (int sp = 0; sp < p.csplit; ++sp) got += ldg(from + (int64_t)sp * kMassKeys);
-  stg(to, mass_after(p, row < x.len0, was, got));
+  stg(to, row < fading_rows(p, x) ? fmaf(p.decay, was, got) : got);
 }
 
 template <int D>

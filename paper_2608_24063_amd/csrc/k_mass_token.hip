@@ -100,9 +100,10 @@ struct MassRows {
         for (int i = 0; i < R; ++i) got[i] += weight_of(p, c0 + k < cols ? s[k][i] : kNegInf, st);
       }
     }
+    const int fades = fading_rows(p, x);
 #pragma unroll
     for (int i = 0; i < R; ++i)
-      if (t + i < last) stg(p.c.mass + x.off + t + i, mass_after(p, t + i < x.len0, was[i], got[i]));
+      if (t + i < last) stg(p.c.mass + x.off + t + i, t + i < fades ? fmaf(p.decay, was[i], got[i]) : got[i]);
   }
 };
 
@@ -413,6 +414,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_token(MassAttn p) {
     }
   }
   if (np > 1) return;
+  const int fades = fading_rows(p, x);
   auto row_mass = [&](int r, float before) {
     const float *s = sm.logits + r * pitch;
     float got = 0.f;
@@ -423,7 +425,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_token(MassAttn p) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) got += weight_of(p, c0 + i < cols ? y[i] : kNegInf, sm.stat[(c0 + i) & 15]);
     }
-    stg(p.c.mass + x.off + r, mass_after(p, r < x.len0, before, got));
+    stg(p.c.mass + x.off + r, r < fades ? fmaf(p.decay, before, got) : got);
   };
 #pragma unroll
   for (int i = 0; i < WAS; ++i)

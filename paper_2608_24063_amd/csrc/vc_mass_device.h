@@ -25,10 +25,11 @@ __device__ __forceinline__ MassUnit mass_unit(const MassAttn &p, int u) {
   return x;
 }
 
-// A row's mass after a call that gave it `got`; `old`: it was there before.  (A decay of zero
-// takes nothing over, which a product would of a mass that is infinite or no number.)
-__device__ __forceinline__ float mass_after(const MassAttn &p, bool old, float was, float got) {
-  return old && p.decay != 0.f ? fmaf(p.decay, was, got) : got;
+// Of a unit's rows, those whose mass from before the call fades; of the others nothing is
+// left: they are new, or decay is 0 (which takes nothing over of a mass that is infinite or no
+// number either).
+__device__ __forceinline__ int fading_rows(const MassAttn &p, const MassUnit &x) {
+  return p.decay == 0.f ? 0 : x.len0;
 }
 
 // Column col of unit u (query col / G, head col % G of its kv head) in q or out.
