@@ -20,6 +20,7 @@ namespace vc {
 namespace {
 
 constexpr int kCols = 64;  // columns of a block
+constexpr int kSum = 64;   // blocks whose weights a lane adds up in fp32
 constexpr int NW = kMassKeys / 64, NT = kMassKeys;  // waves and threads of a workgroup
 
 template <int D>
@@ -32,7 +33,8 @@ template <int D>
 __global__ __launch_bounds__(NT, 2) void k_mass_cols(MassAttn p) {
   constexpr int KS = D / 16, CPR = D / 8, IT = kCols * CPR / NT, CS = NT / CPR;
   __shared__ Smem<D> sm;
-  __shared__ float red[NW][64][2];
+  __shared__ float red[NW][64][2];   // the rows' sums, by halves of the lanes
+  __shared__ double sums[NW][64][2];  // those of all blocks but the last kSum
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int ln = lane & 31, hf = lane >> 5;
   // Splits of a tile's columns innermost, a unit's tiles on one XCD (they share its L2).
@@ -183,29 +185,46 @@ __global__ __launch_bounds__(NT, 2) void k_mass_cols(MassAttn p) {
     __syncthreads();  // the next block is there, this one's columns are read
     half(buf ^ 1, 0, Sa, b * kCols + 32, stb, Sb, what);
   };
-  const int b0 = min(max(uniform((int)min((int64_t)full + kCols - 1, (int64_t)INT32_MAX) / kCols), first), nb);
-  const int b1 = max(min(cols / kCols, nb), b0);  // blocks [b0, b1) are seen whole
-  int b = first;
-  for (; b < b0; ++b) block(b, std::integral_constant<int, 2>{});
-  for (; b < b1; ++b) block(b, std::integral_constant<int, 1>{});
-  for (; b < nb; ++b) block(b, std::integral_constant<int, 2>{});
-  // The rows' sums over the lanes.
-  float *part = &red[w][0][0];
-#pragma unroll
-  for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) acc[kb][i] = sum_lanes<16>(acc[kb][i]);
-  if ((lane & 15) == 0) {
+  // The rows' sums over the lanes: to(place in red, sum), in four lanes.
+  auto over_lanes = [&](auto to) {
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        part[2 * (32 * kb + 8 * (i / 4) + 4 * hf + i % 4) + ((lane >> 4) & 1)] = acc[kb][i];
+      for (int i = 0; i < 16; ++i) acc[kb][i] = sum_lanes<16>(acc[kb][i]);
+    if ((lane & 15) == 0) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          to(2 * (32 * kb + 8 * (i / 4) + 4 * hf + i % 4) + ((lane >> 4) & 1), acc[kb][i]);
+    }
+  };
+  // (Small weights added one at a time to the sum of thousands would be rounded one at a time:
+  // rows that got the same from each of 2^18 columns were 1.2e-4 off.)
+  double *const far = &sums[w][0][0];
+  const bool many = nb - first > kSum;  // uniform
+  if (many) far[lane] = far[lane + 64] = 0.0;
+  const int b0 = min(max(uniform((int)min((int64_t)full + kCols - 1, (int64_t)INT32_MAX) / kCols), first), nb);
+  const int b1 = max(min(cols / kCols, nb), b0);  // blocks [b0, b1) are seen whole
+  for (int b = first;;) {
+    const int e = min(b + kSum, nb), e0 = min(b0, e), e1 = min(b1, e);
+    for (; b < e0; ++b) block(b, std::integral_constant<int, 2>{});
+    for (; b < e1; ++b) block(b, std::integral_constant<int, 1>{});
+    for (; b < e; ++b) block(b, std::integral_constant<int, 2>{});
+    if (e >= nb) break;
+    over_lanes([&](int at, float x) { far[at] += (double)x; });
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[kb][i] = 0.f;
   }
+  float *const part = &red[w][0][0];
+  over_lanes([&](int at, float x) { part[at] = x; });
   __syncthreads();
   const int row = r0 + lane;
   if (row >= emax) return;
-  const float got = part[2 * lane] + part[2 * lane + 1];
+  float got = part[2 * lane] + part[2 * lane + 1];
+  if (many) got = (float)((far[2 * lane] + far[2 * lane + 1]) + (double)got);
   float *to = p.c.mass + x.off + row;
   if (p.csplit > 1)
     stg(p.part_mass + ((int64_t)ut * p.csplit + sp) * NT + 64 * w + lane, got);
@@ -228,10 +247,10 @@ __global__ __launch_bounds__(kMassKeys) void k_mass_sum(MassAttn p) {
   float *to = p.c.mass + x.off + row;
   const float was = ldg(to);
   const float *from = p.part_mass + (int64_t)blockIdx.x * p.csplit * kMassKeys + threadIdx.x;
-  float got = 0.f;
+  double got = 0.0;
 #pragma unroll 4
-  for (int sp = 0; sp < p.csplit; ++sp) got += ldg(from + (int64_t)sp * kMassKeys);
-  stg(to, row < fading_rows(p, x) ? fmaf(p.decay, was, got) : got);
+  for (int sp = 0; sp < p.csplit; ++sp) got += (double)ldg(from + (int64_t)sp * kMassKeys);
+  stg(to, row < fading_rows(p, x) ? fmaf(p.decay, was, (float)got) : (float)got);
 }
 
 template <int D>
