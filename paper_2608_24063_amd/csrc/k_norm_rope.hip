@@ -164,15 +164,18 @@ __global__ __launch_bounds__(256) void k_norm_rope(NormPlan p) {
 }
 
 // The gradient.  A wave takes every (4 groups)-th token of its layer, one at a time, the
-// queries and then the keys, and keeps its lanes' sums over all of them for dw; the
-// workgroup's sums go to `part`, and k_dweight adds those up in a fixed order.
+// queries and then the keys, and keeps its lanes' sums for dw, which go to the wave's in LDS,
+// in 64 bits, when they have kSum terms (thousands added one after another in fp32 would be
+// off by 1e-4 where they are alike); the workgroup's sums go to `part`, and k_dweight adds
+// those up in a fixed order.
+constexpr int kSum = 256;
 template <bool F32, bool ADJ, int D>
 __global__ __launch_bounds__(256) void k_norm_rope_grad(NormPlan p) {
   using Pl = Place<F32, ADJ, D>;
   constexpr int N = Pl::N, HS = Pl::HS, PER = Pl::PER;
   constexpr int64_t E = F32 ? 4 : 2;
   __shared__ float2 cs[4][kRopeMaxHalf];
-  __shared__ float sums[4][2][D];
+  __shared__ double sums[4][2][D];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t toks = (int64_t)p.B * p.n;
   const int l = (int)(blockIdx.x / (uint32_t)p.groups), grp = (int)(blockIdx.x % (uint32_t)p.groups);
@@ -183,6 +186,20 @@ __global__ __launch_bounds__(256) void k_norm_rope_grad(NormPlan p) {
   pl.weights(p.kw, l, p.w_fp32, ws[1]);
 #pragma unroll
   for (int k = 0; k < 2 * N; ++k) dw[0][k] = dw[1][k] = 0.f;
+  for (int e = lane; e < 2 * D; e += 64) (&sums[w][0][0])[e] = 0.0;
+  // A side's terms since its lanes' sums, over the lanes of the same channels, went to LDS.
+  int terms[2] = {0, 0};
+  auto close = [&](int s) {
+    terms[s] = 0;
+#pragma unroll
+    for (int k = 0; k < 2 * N; ++k) {
+      float v = dw[s][k];
+#pragma unroll
+      for (int m = PER; m < 64; m *= 2) v += shfl_xor(v, m);
+      if (lane < PER) sums[w][s][(k < N ? pl.o1 : pl.o2 - N) + k] += (double)v;
+      dw[s][k] = 0.f;
+    }
+  };
   for (int64_t g = (int64_t)grp * 4 + w; g < toks; g += 4 * (int64_t)p.groups) {
     const int b = (int)(g / p.n), i = (int)(g % p.n);
     if (p.count && i >= ldg(p.count + b)) continue;  // wave-uniform
@@ -223,22 +240,16 @@ __global__ __launch_bounds__(256) void k_norm_rope_grad(NormPlan p) {
     side(p.Hq, p.qi, p.qg, p.qo, ws[0], dw[0]);
     side(p.Hkv, p.ki, p.kg, p.ko, ws[1], dw[1]);
     __builtin_amdgcn_wave_barrier();
+    if ((terms[0] += (p.Hq + HS - 1) / HS) >= kSum) close(0);
+    if ((terms[1] += (p.Hkv + HS - 1) / HS) >= kSum) close(1);
   }
-  // The wave's lanes of the same channels, then the waves.
-#pragma unroll
-  for (int s = 0; s < 2; ++s)
-#pragma unroll
-    for (int k = 0; k < 2 * N; ++k) {
-      float v = dw[s][k];
-#pragma unroll
-      for (int m = PER; m < 64; m *= 2) v += shfl_xor(v, m);
-      if (lane < PER) sums[w][s][(k < N ? pl.o1 : pl.o2 - N) + k] = v;
-    }
+  close(0);
+  close(1);
   __syncthreads();
   float *to = p.part + (int64_t)blockIdx.x * 2 * D;
   for (int e = tid; e < 2 * D; e += 256) {
-    const float *f = &sums[0][0][0] + e;
-    stg(to + e, (f[0] + f[2 * D]) + (f[4 * D] + f[6 * D]));
+    const double *f = &sums[0][0][0] + e;
+    stg(to + e, (float)((f[0] + f[2 * D]) + (f[4 * D] + f[6 * D])));
   }
 }
 
