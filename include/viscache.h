@@ -684,8 +684,8 @@ size_t viscache_mass_attend_workspace_bytes(const vc_decode_shape *shape, int32_
  * viscache_mass_attend_workspace_bytes bytes, 256-byte aligned; contents do not matter and
  * none are kept, so calls, captured ones among them, may share one as long as they do
  * not overlap.  VC_ERR_WORKSPACE comes after all other checks.  VC_ERR_UNSUPPORTED for
- * n * Hq/Hkv > 2^24, 2^23 or more workgroups of a launch, or 2^24 or more columns to
- * join. */
+ * n * Hq/Hkv > 2^24, 2^23 or more workgroups of a launch (2^22 of the second one of single
+ * tokens, one for each 4096 rows of a unit), or 2^24 or more columns to join. */
 vc_status viscache_mass_attend(const vc_decode_shape *shape, const vc_mass_cache *cache, const vc_rows *k,
                                const vc_rows *v, const vc_rows *q, const vc_rows *out, int32_t n,
                                const int32_t *count, int32_t out_fp32, float scale, float decay, int32_t max_rows,

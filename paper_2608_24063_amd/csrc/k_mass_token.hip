@@ -459,7 +459,7 @@ __global__ __launch_bounds__(kMassChunk) void k_finish(MassAttn p) {
   const int np = (int)st.w;
   if (ch == 0 && tid == 0 && p.append) stg(p.c.len + u, x.held);
   if (np <= 1) return;
-  const int cols = x.cnt * p.G, emax = min(x.held, p.max_rows), nch = (emax + kRows - 1) / kRows;
+  const int cols = x.cnt * p.G, emax = min(x.held, p.max_rows), nch = (emax - 1) / kRows + 1;
   if (ch >= nch) return;
   const int64_t slot = (int64_t)u * p.npmax;
   const float2 *pm = p.part_ml + slot * 16;
@@ -522,14 +522,10 @@ hipError_t launch(const MassAttn &p, hipStream_t st) {
     hipLaunchKernelGGL((k_token<D, 4>), dim3((uint32_t)p.wgs), dim3(256), 0, st, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.npmax == 1) return e;
-  const int64_t chunks = ((int64_t)p.max_rows + kMassChunk - 1) / kMassChunk;
-  // Four rows a thread where one would take more than the 512 workgroups that the card holds.
-  // (us of both launches, one and four rows: 112 units of 23000 319 309, of 12000 172.5
-  // 168.5, of 4000 47.5 48.6; 64 of 12000 98.4 96.4, of 4000 29.0 32.4; 4 of 12000 15.6 17.5.)
-  if (p.units * chunks > 512)
-    hipLaunchKernelGGL((k_finish<D, 4>), dim3((uint32_t)(p.units * ((chunks + 3) / 4))), dim3(kMassChunk), 0, st, p);
+  if (p.finish == 4)
+    hipLaunchKernelGGL((k_finish<D, 4>), dim3((uint32_t)p.finish_wgs), dim3(kMassChunk), 0, st, p);
   else
-    hipLaunchKernelGGL((k_finish<D, 1>), dim3((uint32_t)(p.units * chunks)), dim3(kMassChunk), 0, st, p);
+    hipLaunchKernelGGL((k_finish<D, 1>), dim3((uint32_t)p.finish_wgs), dim3(kMassChunk), 0, st, p);
   return hipGetLastError();
 }
 

@@ -38,6 +38,7 @@ struct MassAttn {
   // `here` in LDS, all others in [unit][cols][ldr], from row `here` on.
   const int32_t *order;
   int32_t waves, piece, npmax, here, ldr;
+  int32_t finish, finish_wgs;  // the second launch, of cut units: rows a thread (1 or 4), workgroups
   float *logits;
   // Prompts (npmax 1): nqt column tiles of qcols columns, each in as many key splits
   // as the launch's workgroups allow (ns 1: whole).

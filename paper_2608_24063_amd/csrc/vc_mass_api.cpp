@@ -31,7 +31,7 @@ MassPool bind(const vc_mass_cache *c) {
 
 // How an attention call is cut, and the parts of its workspace.
 struct Cut {
-  int32_t waves = 0, piece = 0, npmax = 1, here = 0, ldr = 0, qcols = 0, nqt = 0, ns = 1, ktiles = 1, csplit = 1;
+  int32_t waves = 0, piece = 0, npmax = 1, here = 0, ldr = 0, finish = 0, finish_wgs = 0, qcols = 0, nqt = 0, ns = 1, ktiles = 1, csplit = 1;
   int64_t wgs = 0, slots = 0;  // workgroups; columns of partial results
   size_t ml = 0, stat = 0, state = 0, np = 0, logits = 0, mass = 0, total = 0;
 };
@@ -73,8 +73,17 @@ bool attend_cut(const vc_decode_shape *s, int32_t n, int32_t max_rows, Cut &c) {
     const int64_t room = (c.waves == 8 ? kMassHeld8 : kMassHeld4) / pitch / kMassTile * kMassTile;
     c.here = (int32_t)(c.npmax > 1 ? 0 : std::min(room, nt * kMassTile));
     c.ldr = (int32_t)(nt * kMassTile - c.here);
-    // The second launch's workgroups (of 1024 threads).
-    if (c.npmax > 1 && units * (((int64_t)max_rows + kMassChunk - 1) / kMassChunk) >= kMaxWg / 2) return false;
+    // The second launch's workgroups (of 1024 threads).  Four rows a thread where one would take
+    // more than the 512 workgroups that the card holds.  (us of both launches, one and four rows:
+    // 112 units of 23000 319 309, of 12000 172.5 168.5, of 4000 47.5 48.6; 64 of 12000 98.4
+    // 96.4, of 4000 29.0 32.4; 4 of 12000 15.6 17.5.)
+    if (c.npmax > 1) {
+      const int64_t chunks = ((int64_t)max_rows + kMassChunk - 1) / kMassChunk;
+      c.finish = units * chunks > 512 ? 4 : 1;
+      const int64_t wgs = units * ((chunks + c.finish - 1) / c.finish);
+      if (wgs >= kMaxWg / 2) return false;
+      c.finish_wgs = (int32_t)wgs;
+    }
   } else {
     const int64_t nt = std::max<int64_t>(1, ((int64_t)max_rows + kQ8Block - 1) / kQ8Block);
     // Two workgroups of 128 columns hide each other's start, which counts where rows are few,
@@ -201,6 +210,7 @@ vc_status viscache_mass_attend(const vc_decode_shape *s, const vc_mass_cache *c,
   p.decay = decay;
   p.order = c->order;
   p.waves = cut.waves; p.piece = cut.piece; p.npmax = cut.npmax; p.here = cut.here; p.ldr = cut.ldr;
+  p.finish = cut.finish; p.finish_wgs = cut.finish_wgs;
   p.qcols = cut.qcols; p.nqt = cut.nqt; p.ns = cut.ns;
   uint8_t *ws = static_cast<uint8_t *>(workspace);
   p.part_o = reinterpret_cast<float *>(ws);

@@ -11,7 +11,8 @@
 namespace vc {
 
 hipError_t launch_mass_token(const MassAttn &p, hipStream_t) {
-  std::printf("kind=token waves=%d piece=%d npmax=%d here=%d ldr=%d\n", p.waves, p.piece, p.npmax, p.here, p.ldr);
+  std::printf("kind=token waves=%d piece=%d npmax=%d here=%d ldr=%d finish=%d finish_wgs=%d\n", p.waves, p.piece, p.npmax,
+              p.here, p.ldr, p.finish, p.finish_wgs);
   return hipSuccess;
 }
 hipError_t launch_mass_prompt(const MassAttn &p, hipStream_t) {

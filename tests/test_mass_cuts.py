@@ -29,3 +29,8 @@ def test_paths_are_cut_as_they_say(tmp_path):
             got = dict(x.split("=") for x in line.split())
             assert got["kind"] == ("token" if p in mp.TOKENS else "prompt"), p.name
             assert {k: int(got[k]) for k in p.cut} == p.cut, (p.name, line)
+    # The second launch of units that are cut: rows a thread, workgroups.
+    for L, B, rows, finish, wgs in ((1, 1, 5000, 1, 5), (8, 8, 9000, 4, 192), (1, 7, 2 ** 31 - 1, 4, 7 << 19)):
+        line = subprocess.check_output([exe] + [str(x) for x in (L, B, 4, 1, 64, 1, rows)], text=True)
+        got = dict(x.split("=") for x in line.split())
+        assert int(got["npmax"]) > 1 and (int(got["finish"]), int(got["finish_wgs"])) == (finish, wgs), line
