@@ -7,6 +7,7 @@ import ctypes
 import struct
 
 import torch
+from torch.autograd import forward_ad as _forward
 
 from . import (VC_ERR_WORKSPACE, VC_PRUNE_EVENTS, VC_Q8_BLOCK, VisCacheError, _int32, lib, VC_Q8_E4M3, VC_Q8_INT8, VC_RANK_GLOBAL, make_params, make_prune_io, make_shape, prune_with_io, vc_cache,
                vc_decode_shape, vc_mass_cache, vc_norm, vc_q8cache, vc_qcache, vc_rope, vc_rows, viscache_append_kv, viscache_budget, viscache_decode_attn,
@@ -280,6 +281,14 @@ def _enqueue(name: str, f, index: int, *args) -> None:
         raise VisCacheError(st, name)
 
 
+def _no_tangents(*tensors) -> None:
+    """Refuses tensors that carry a tangent (forward-mode autograd, which a call through
+    addresses would leave as it was)."""
+    for t in tensors:
+        if t is not None and _forward.unpack_dual(t).tangent is not None:
+            raise ValueError("a tensor carries a tangent: forward-mode autograd does not see the rotation")
+
+
 class Rope:
     """Rotary positions with several axes (viscache_rope): head dim d, `rot`
     rotated channels (all by default), `sections` frequencies for time, height
@@ -312,13 +321,15 @@ class Rope:
         most 16 times it; other heads take a call for q and one for k.
 
         Autograd does not see the rotation, so tensors that require grad are refused
-        where it records (a program calls this in the forward and backward of an
-        autograd function of its own, or under no_grad); outputs count as changed in
-        place."""
+        where it records, and tensors with a tangent (a program calls this in the forward,
+        backward and jvp of an autograd function of its own, or under no_grad); outputs
+        count as changed in place."""
         if ((q is not None and q.requires_grad) or (k is not None and k.requires_grad) or
                 (q_out is not None and q_out.requires_grad) or (k_out is not None and k_out.requires_grad)):
             if torch.is_grad_enabled():
                 raise ValueError("a tensor requires grad: autograd does not see the rotation")
+        if _forward._current_level >= 0:
+            _no_tangents(q, k, q_out, k_out)
         return self._turn(pos, q, k, q_out, k_out, inverse, count)
 
     def _turn(self, pos, q, k, q_out, k_out, inverse=False, count=None):
@@ -412,6 +423,8 @@ class NormRope:
             for t in tensors:
                 if t is not None and t.requires_grad:
                     raise ValueError("a tensor requires grad: autograd does not see the normed rotation")
+        if _forward._current_level >= 0:
+            _no_tangents(*tensors)
 
     def apply(self, pos, q=None, k=None, q_weight=None, k_weight=None, q_out=None, k_out=None, inverse: bool = False,
               count=None):
@@ -420,8 +433,8 @@ class NormRope:
         (bf16 or fp32, both of one type) and turns them by pos int32 [3, B, n] into q_out
         and k_out, by default in place.  Every other argument, heads, streams and
         autograd as for Rope.apply: tensors that require grad are refused where it
-        records, and a program calls apply and grad in an autograd function of its
-        own.  Returns (q_out, k_out)."""
+        records, those with a tangent too, and a program calls apply and grad in an
+        autograd function of its own.  Returns (q_out, k_out)."""
         self._no_grad(q, k, q_weight, k_weight, q_out, k_out)
         shape, (L, B, n), typ, index, norm, at = self._call(pos, q, k, q_weight, k_weight, count)
         qi = qo = ki = ko = None
@@ -745,7 +758,8 @@ class MassCache(_Attends):
     that knows a bound well below the capacities passes it as max_rows.
 
     Calls go to the current stream of the cache's device.  Calls on one cache share a
-    workspace and must not overlap."""
+    workspace and must not overlap.  Autograd records nothing of them, whether their
+    tensors require grad or not: outputs and masses are numbers without a history."""
 
     def __init__(self, L, B, Hq, Hkv, d, caps, device, buffers=None):
         caps = self._shaped(L, B, Hq, Hkv, d, caps, device)
