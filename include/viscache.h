@@ -668,15 +668,16 @@ size_t viscache_mass_attend_workspace_bytes(const vc_decode_shape *shape, int32_
  * for t < min(len, max_rows) (masses behind are left as they were).  A query that sees no
  * row gives zeros and no weight; one with a NaN gives NaN, and NaN to the masses of the
  * rows it sees.  An infinity or a NaN among a row's values reaches the queries that see
- * it (as NaN), no others.  Rows i >= c of out are left as they were.  q: bf16; out: bf16
+ * it (which get an infinity or a NaN in its channel), no others.  Rows i >= c of out are left as they were.  q: bf16; out: bf16
  * (out_fp32 = 0) or fp32, both indexed by the query head; the rows of q, k, v and out
  * and the cache must not overlap.
  * Logits, maxima, sums, weights and masses are fp32, summed in an order that follows
  * from the shape, max_rows, the lengths and the counts.  A weight meets its value with
  * 24 bits; with n * Hq/Hkv > 16 and bf16 outputs it is rounded to bf16 there (2^-8 of
  * itself; a caller that needs more asks for fp32 outputs).
- * decay: finite, not negative (1: nothing fades; 0: the last call's weights alone, whatever the
- * masses were; any other leaves masses that are infinite or NaN so).
+ * scale: positive, scale * log2(e) finite.  decay: finite, not negative (1: nothing
+ * fades; 0: the last call's weights alone, whatever the masses were; any other leaves
+ * masses that are infinite or NaN so).
  * max_rows bounds every len after the append.  n = 0 does nothing.  n * Hq/Hkv <= 16
  * (single tokens, short drafts) is one launch, or two where units are cut along their
  * rows; more take two, and one each for an append, for outputs and for masses that are

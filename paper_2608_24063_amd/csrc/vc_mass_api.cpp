@@ -175,7 +175,8 @@ vc_status viscache_mass_attend(const vc_decode_shape *s, const vc_mass_cache *c,
   if (st != VC_OK) return st;
   if ((st = check_cache(c)) != VC_OK) return st;
   if (n < 0 || max_rows < 0 || (out_fp32 != 0 && out_fp32 != 1) || !k != !v) return VC_ERR_ARG;
-  if (!(scale > 0.f) || !std::isfinite(scale) || !(decay >= 0.f) || !std::isfinite(decay)) return VC_ERR_ARG;
+  const float sc = scale * 1.4426950408889634f;  // logits in powers of two
+  if (!(scale > 0.f) || !std::isfinite(sc) || !(decay >= 0.f) || !std::isfinite(decay)) return VC_ERR_ARG;
   if (n == 0) return VC_OK;
   if (!rows_ok(q, 2, s->L, s->B, n, s->Hq, s->d, false, false) ||
       !rows_ok(out, out_fp32 ? 4 : 2, s->L, s->B, n, s->Hq, s->d, true, false))
@@ -206,7 +207,7 @@ vc_status viscache_mass_attend(const vc_decode_shape *s, const vc_mass_cache *c,
   p.fp32 = out_fp32;
   p.causal = 1;
   p.max_rows = std::min(max_rows, kMassMaxRows);
-  p.sc = scale * 1.4426950408889634f;
+  p.sc = sc;
   p.decay = decay;
   p.order = c->order;
   p.waves = cut.waves; p.piece = cut.piece; p.npmax = cut.npmax; p.here = cut.here; p.ldr = cut.ldr;
