@@ -56,7 +56,8 @@ __device__ __forceinline__ float top_of(float a) { return __uint_as_float(__floa
 // Values of a row that not every column of a product sees: an infinity or a NaN, whose
 // weight is zero there, would still reach them.  Such values become zeros, and the
 // first row of each channel that had one (bad[channel], INT32_MAX: none) makes NaN of
-// the columns that do see it.
+// the columns that do see it.  (Rows that every column sees go through the product as they
+// are: an infinity stays one, or becomes NaN where a part of its weight is zero.)
 __device__ __forceinline__ bool any_nonfinite(u32x4 w) {
   const uint32_t m = max_mag(max_mag(max_mag(max_mag(0u, w.x), w.y), w.z), w.w);
   return (m & 0xFFFFu) >= 0x7F80u || (m >> 16) >= 0x7F80u;
