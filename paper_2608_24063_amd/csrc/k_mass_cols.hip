@@ -10,7 +10,8 @@
 // 16384 columns over 8 units of 25088 rows, 128 channels: 795 to 840 us (1.0 PFLOP/s of
 // products, the matrix cores busy for half of the time; 1120 before products and weights were
 // interleaved), and 5 to add up the parts.  455 columns over 12 units of 9000 to 12900 rows:
-// 35 (0.44 PFLOP/s: 600 workgroups on 512 places, each with a start that nothing hides).
+// 33 to 36 (0.44 PFLOP/s: each workgroup has a start that nothing hides, and where sequences
+// have 65, 40 and 15 queries, units on one XCD leave the XCDs 122 to 513 blocks to do).
 #include <type_traits>
 
 #include "vc_mass_device.h"

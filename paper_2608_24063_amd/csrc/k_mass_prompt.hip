@@ -10,7 +10,7 @@
 // a lane's logits are the k-elements of its own P^T operand; P never leaves the
 // registers, and V's operands are transposing reads of its row-major block.
 //
-// 16384 columns over 8 units of 25088 rows, 128 channels: 1480 to 1560 us (1.05 to 1.1
+// 16384 columns over 8 units of 25088 rows, 128 channels: 1480 to 1590 us (1.02 to 1.1
 // PFLOP/s, the matrix cores busy for 0.54 of the time, at the clock that they leave).
 // Without the operands' reads and the weights it takes 1049, products and supply without
 // weights 1250, weights and supply without products 892.  455 columns over 12 units of
@@ -19,9 +19,10 @@
 // With bf16 outputs a weight is rounded to bf16 before it meets its value (2^-8 of
 // itself): a choice of speed, since the errors of a column's weights average out and
 // stay under the half step of the output unless its values cancel, and a second part
-// would make half as many products again.  The sum of the weights is of the unrounded
-// ones.  With fp32 outputs P is cut in three bf16 parts (24 bits).  Sums, maxima, O and
-// the partial results are fp32 in both.
+// makes half as many products again (a call of those 16384 columns 2360 -> 2864 us).  The
+// sum of the weights is of the unrounded ones.  With fp32 outputs P is cut in three bf16
+// parts (24 bits; 3510 us, 2750 to 2830 of them here).  Sums, maxima, O and the partial
+// results are fp32 in both.
 #include "vc_mass_device.h"
 
 namespace vc {
