@@ -620,12 +620,12 @@ size_t viscache_norm_rope_grad_workspace_bytes(const vc_decode_shape *shape, int
  * (q, k) and the gradients of the rows that came out (q_dout, k_dout), all of the rows'
  * type, the gradients of the rows (q_din, k_din; rows of tokens i >= count[b] are left
  * as they were) and of the weights (q_dweight, k_dweight: DEVICE fp32 [L][d], written,
- * not added to; zeros where there are no tokens), summed in fp32 in an order that
- * depends on the shape alone.  A side is left out by NULL for all four of its
- * arguments.  q_din may be q or q_dout (the same data and strides), k_din likewise;
- * otherwise they must not overlap.  `workspace`: DEVICE, 256-byte aligned, its
- * contents on entry do not matter and none are kept.  Limits as for viscache_rope,
- * and L < 2^17. */
+ * not added to; zeros where there are no tokens), summed in fp32 over some 256 terms at
+ * a time and then in 64 bits, in an order that depends on the shape and the counts
+ * alone.  A side is left out by NULL for all four of its arguments.  q_din may be q or
+ * q_dout (the same data and strides), k_din likewise; otherwise they must not overlap.
+ * `workspace`: DEVICE, 256-byte aligned, its contents on entry do not matter and none
+ * are kept.  Limits as for viscache_rope, and L < 2^17. */
 vc_status viscache_norm_rope_grad(const vc_decode_shape *shape, const vc_rope *rope, const vc_norm *norm, int32_t n,
                                   const int32_t *pos, const int32_t *count, const vc_rows *q, const vc_rows *q_dout,
                                   const vc_rows *q_din, float *q_dweight, const vc_rows *k, const vc_rows *k_dout,
@@ -671,7 +671,8 @@ size_t viscache_mass_attend_workspace_bytes(const vc_decode_shape *shape, int32_
  * it (which get an infinity or a NaN in its channel), no others.  Rows i >= c of out are left as they were.  q: bf16; out: bf16
  * (out_fp32 = 0) or fp32, both indexed by the query head; the rows of q, k, v and out
  * and the cache must not overlap.
- * Logits, maxima, sums, weights and masses are fp32, summed in an order that follows
+ * Logits, maxima, sums, weights and masses are fp32 (a prompt's masses are added up in 64
+ * bits from sums over 4096 columns), summed in an order that follows
  * from the shape, max_rows, the lengths and the counts.  A weight meets its value with
  * 24 bits; with n * Hq/Hkv > 16 and bf16 outputs it is rounded to bf16 there (2^-8 of
  * itself; a caller that needs more asks for fp32 outputs).

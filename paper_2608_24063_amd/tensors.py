@@ -463,8 +463,8 @@ class NormRope:
         (the rows' type) to the rows' gradients, in q_din and k_din (by default new
         tensors; q or q_dout itself is allowed; rows of tokens past count are left as
         they were, in new tensors zeros), and the weights', new fp32 tensors [L, d].
-        Sums are formed in an order that depends on the shape alone.  Returns (q_din, k_din, q_dweight,
-        k_dweight), None for a side without rows."""
+        Sums are formed in an order that depends on the shape and count alone.
+        Returns (q_din, k_din, q_dweight, k_dweight), None for a side without rows."""
         self._no_grad(q, k, q_weight, k_weight, q_dout, k_dout, q_din, k_din)
         shape, (L, B, n), typ, index, norm, at = self._call(pos, q, k, q_weight, k_weight, count)
         if (q is None) != (q_dout is None) or (k is None) != (k_dout is None):
